@@ -251,6 +251,89 @@ int mebp_layer_recompute_backward_static(const mebp_config* cfg, int32_t layer, 
                                          float* dx, const mebp_layer_lora_grad* grads, int32_t B, int32_t T,
                                          mebp_stream_t stream);
 
+/* ---------------- operators on logits ------------------------------------------------
+ * What is trained on, or read off, a matrix of logits z [rows][vocab] beside the fused
+ * next-token loss above. Numbers per row are fp32, sums are fp32; a temperature tau divides
+ * the logits first. Logits of -inf are columns masked off: probability 0, gradient 0.
+ * All calls take rows = 0 (nothing is enqueued).                                          */
+
+/* Element type of a matrix of logits or of their gradient. */
+enum { MEBP_F32 = 0, MEBP_F16 = 1, MEBP_BF16 = 2 };
+
+typedef struct {
+  void* data;      /* [rows][ld], aligned to its element's size                            */
+  int64_t ld;      /* elements from one row to the next, >= vocab; those behind a row's     */
+                   /* vocab are neither read nor written                                   */
+  int32_t rows;    /* 0 .. 2^23                                                             */
+  int32_t vocab;   /* 1 .. 2^30                                                             */
+  int32_t dtype;   /* MEBP_F32, MEBP_F16 or MEBP_BF16                                      */
+} mebp_logits;
+
+/* Bytes of workspace that mebp_token_logprobs (with this top_k) and mebp_distill_topk (top_k
+ * = 0) need for logits of this shape. Pure host computation; 0 for an invalid one.         */
+size_t mebp_logits_workspace_bytes(int32_t rows, int32_t vocab, int32_t top_k);
+
+/* Outputs of mebp_token_logprobs, each one NULL where it is not wanted. With q = softmax(z /
+ * tau): */
+typedef struct {
+  float* logp;      /* [rows] ln q[target]; 0 where the target is < 0                       */
+  float* lse;       /* [rows] ln sum exp(z / tau)                                           */
+  float* entropy;   /* [rows] -sum q ln q                                                   */
+  int32_t* top_ids; /* [rows][top_k] the columns of the largest logits, in falling order,    */
+                    /* of equal ones the lower column first                                 */
+  float* top_logp;  /* [rows][top_k] their ln q                                             */
+} mebp_token_scores;
+
+/* Log probabilities of given tokens, with the entropy of the distribution and its top
+ * alternatives: the score of a text, or a teacher's record for mebp_distill_topk.
+ *   targets  [rows] int32 token ids; < 0: none; >= vocab: logp is NaN. NULL without logp
+ *   top_k    0 .. 64 (0: top_ids and top_logp are NULL)
+ * Logits of -inf and NaN are no alternatives: where a row has fewer than top_k others, the
+ * remaining ids are -1 and their ln q is -inf. A row of nothing but -inf has lse -inf, logp
+ * -inf and entropy 0; a NaN or +inf logit makes lse, logp, entropy and top_logp NaN.       */
+int mebp_token_logprobs(const mebp_logits* z, const int32_t* targets, float temperature, int32_t top_k,
+                        const mebp_token_scores* out, void* ws, size_t ws_bytes, mebp_stream_t stream);
+
+/* Gradient of sum_n d_logp[n] logp[n] + d_entropy[n] entropy[n] w.r.t. the logits:
+ *   dz[n][v] = (d_logp (1[v = target] - q[v]) - d_entropy q[v] (ln q[v] + entropy)) / tau.
+ *   lse, entropy   [rows] as mebp_token_logprobs wrote them for the same logits (entropy is
+ *                  read only with d_entropy)
+ *   d_logp, d_entropy  [rows] fp32; either may be NULL (0). targets may be NULL without d_logp
+ *   dz   of the logits' rows and vocab, any type and ld. May be the logits themselves (same
+ *        data, type and ld), and must not overlap them otherwise
+ * A target < 0 gives its row no d_logp term, one >= vocab makes the row NaN. A row whose lse
+ * is -inf gets zeros. No workspace.                                                        */
+int mebp_token_logprobs_backward(const mebp_logits* z, const int32_t* targets, float temperature, const float* lse,
+                                 const float* entropy, const float* d_logp, const float* d_entropy,
+                                 const mebp_logits* dz, mebp_stream_t stream);
+
+/* What a student's logits are distilled from. Per row, with p = softmax(logits / tau) over
+ * its entries, q = softmax(z / tau) and q1 = softmax(z) over the whole vocabulary:
+ *   loss = w (alpha tau^2 sum_k p_k (ln p_k - ln q[id_k]) - (1 - alpha) ln q1[target]).
+ * The teacher's top log probabilities serve as its logits as well.                         */
+typedef struct {
+  const int32_t* ids;      /* [rows][k] the teacher's token ids; < 0: no entry; an id may     */
+                           /* occur twice (its probabilities add); >= vocab: the row is NaN  */
+  const float* logits;     /* [rows][k]; -inf: no entry                                     */
+  const int32_t* targets;  /* [rows] hard labels, read if alpha < 1; < 0: no such term here;  */
+                           /* >= vocab: the row is NaN                                      */
+  const float* row_weight; /* [rows] w, e.g. 1 / rows for a mean; NULL: 1. A row of weight 0 */
+                           /* has loss and gradient 0 whatever its logits are               */
+  int32_t k;               /* 1 .. 64                                                       */
+  float temperature;       /* tau, 1e-6 .. 1e6                                              */
+  float alpha;             /* 0 .. 1                                                        */
+} mebp_distill;
+
+/* Distillation from a teacher's top logits: the loss of each row and, unless dz is NULL, the
+ * gradient of their sum w.r.t. the student's logits,
+ *   dz = w (alpha tau (q - p) + (1 - alpha) (q1 - 1[target])).
+ *   row_loss [rows] fp32 (written)
+ *   dz       as in mebp_token_logprobs_backward
+ * A row without entries has no distillation term. A row of nothing but -inf has loss +inf
+ * (0 without entries and label) and gradient 0.                                            */
+int mebp_distill_topk(const mebp_logits* z, const mebp_distill* d, float* row_loss, const mebp_logits* dz, void* ws,
+                      size_t ws_bytes, mebp_stream_t stream);
+
 /* Message for the last non-zero status returned on the calling thread ("" if none). */
 const char* mebp_last_error(void);
 

@@ -24,8 +24,12 @@ EXPORTED = (
     "mebp_dequant_q4", "mebp_workspace_offset", "mebp_workspace_slot_name", "mebp_kernel_timing",
     "mebp_kernel_timing_report", "mebp_kernel_repeat", "mebp_lora_grad_accumulate", "mebp_lora_adamw_step",
     "mebp_train_step_offload", "mebp_test_gemm", "mebp_layer_recompute_backward_static",
-    "mebp_set_workspace_guards", "mebp_workspace_guard_check",
+    "mebp_set_workspace_guards", "mebp_workspace_guard_check", "mebp_logits_workspace_bytes",
+    "mebp_token_logprobs", "mebp_token_logprobs_backward", "mebp_distill_topk",
 )
+
+MEBP_F32, MEBP_F16, MEBP_BF16 = 0, 1, 2  # element types of a matrix of logits
+MAX_TOP = 64  # most alternatives, and most entries of a teacher, per row
 
 STATIC_SCRATCH_BYTES = 64 << 20  # MEBP_STATIC_SCRATCH_BYTES
 
@@ -75,6 +79,20 @@ class MebpAdamwHparams(C.Structure):
                 ("weight_decay", C.c_float), ("grad_scale", C.c_float), ("step", C.c_int32)]
 
 
+class MebpLogits(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("ld", C.c_int64), ("rows", C.c_int32), ("vocab", C.c_int32), ("dtype", C.c_int32)]
+
+
+class MebpTokenScores(C.Structure):
+    _fields_ = [("logp", C.c_void_p), ("lse", C.c_void_p), ("entropy", C.c_void_p), ("top_ids", C.c_void_p),
+                ("top_logp", C.c_void_p)]
+
+
+class MebpDistill(C.Structure):
+    _fields_ = [("ids", C.c_void_p), ("logits", C.c_void_p), ("targets", C.c_void_p), ("row_weight", C.c_void_p),
+                ("k", C.c_int32), ("temperature", C.c_float), ("alpha", C.c_float)]
+
+
 class MebpError(RuntimeError):
     def __init__(self, code: int, msg: str):
         super().__init__(f"mebp status {code}: {msg}")
@@ -118,6 +136,13 @@ def lib() -> C.CDLL:
             "mebp_workspace_slot_name": (C.c_char_p, [I32]),
             "mebp_set_workspace_guards": (C.c_int, [I32]),
             "mebp_workspace_guard_check": (C.c_int, [cfgp, I32, I32, P, SZ, P]),
+            "mebp_logits_workspace_bytes": (SZ, [I32, I32, I32]),
+            "mebp_token_logprobs": (C.c_int, [C.POINTER(MebpLogits), P, C.c_float, I32, C.POINTER(MebpTokenScores), P,
+                                              SZ, P]),
+            "mebp_token_logprobs_backward": (C.c_int, [C.POINTER(MebpLogits), P, C.c_float, P, P, P, P,
+                                                       C.POINTER(MebpLogits), P]),
+            "mebp_distill_topk": (C.c_int, [C.POINTER(MebpLogits), C.POINTER(MebpDistill), P, C.POINTER(MebpLogits), P,
+                                            SZ, P]),
             "mebp_kernel_timing": (C.c_int, [I32, I32]),
             "mebp_kernel_timing_report": (C.c_int, [C.c_char_p, SZ]),
             "mebp_kernel_repeat": (C.c_int, [C.c_char_p, I32]),
@@ -237,6 +262,26 @@ def mebp_lora_grad_accumulate(cfg, grads, acc, scale: float, first: bool, stream
 def mebp_lora_adamw_step(cfg, params, grads, m, v, hp, stream=0, check=True):
     """params, m, v: ctypes arrays of MebpLayerLoraState; grads: of MebpLayerLoraGrad."""
     r = lib().mebp_lora_adamw_step(C.byref(cfg), params, grads, m, v, _ref(hp), stream)
+    return _check(r) if check else r
+
+
+def mebp_logits_workspace_bytes(rows: int, vocab: int, top_k: int = 0) -> int:
+    return lib().mebp_logits_workspace_bytes(rows, vocab, top_k)
+
+
+def mebp_token_logprobs(z, targets, temperature, top_k, out, ws, ws_bytes, stream=0, check=True):
+    r = lib().mebp_token_logprobs(_ref(z), targets, temperature, top_k, _ref(out), ws, ws_bytes, stream)
+    return _check(r) if check else r
+
+
+def mebp_token_logprobs_backward(z, targets, temperature, lse, entropy, d_logp, d_entropy, dz, stream=0, check=True):
+    r = lib().mebp_token_logprobs_backward(_ref(z), targets, temperature, lse, entropy, d_logp, d_entropy, _ref(dz),
+                                           stream)
+    return _check(r) if check else r
+
+
+def mebp_distill_topk(z, distill, row_loss, dz, ws, ws_bytes, stream=0, check=True):
+    r = lib().mebp_distill_topk(_ref(z), _ref(distill), row_loss, _ref(dz), ws, ws_bytes, stream)
     return _check(r) if check else r
 
 

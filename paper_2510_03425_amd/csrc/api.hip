@@ -91,6 +91,11 @@ std::atomic<int> g_guards{[] {
 constexpr size_t kGuardBytes = 256;
 constexpr int kMaxGuards = 2 * S_COUNT;
 
+// Slots of the workspaces of the operators on logits; their guards' tags follow the others'.
+enum OpSlot { OP_STATS, OP_KEYS, OP_PICKED, OP_COUNT };
+const char* kOpSlotNames[OP_COUNT] = {"logit_stats", "logit_keys", "logit_picked"};
+constexpr int kOpTag = 2 * S_COUNT;
+
 // A layer's weights as fragments: none, one product's at a time, or all at once.
 enum Frag { FRAG_NONE = 0, FRAG_EACH, FRAG_LAYER };
 
@@ -470,10 +475,48 @@ int guard_verdict(const Layout& L, void* ws, hipStream_t st) {
   uint32_t h = 0;
   HIP_TRY(hipMemcpyAsync(&h, (char*)ws + L.status_off, 4, hipMemcpyDeviceToHost, st));
   HIP_TRY(hipStreamSynchronize(st));
+  if (h >= (uint32_t)kOpTag && h < (uint32_t)(kOpTag + OP_COUNT))
+    return fail(MEBP_EWORKSPACE, "workspace guard after slot '%s' was overwritten", kOpSlotNames[h - kOpTag]);
   if (h != 0xFFFFFFFFu)
     return fail(MEBP_EWORKSPACE, "workspace guard after slot '%s'%s was overwritten", kSlotNames[h % S_COUNT],
                 h >= (uint32_t)S_COUNT ? " (second copy)" : "");
   return MEBP_OK;
+}
+
+// Slots of a workspace that is not a config's: placed one after another, guarded in the debug mode.
+struct OpLayout {
+  Layout L;
+  size_t off[OP_COUNT];
+  OpLayout() {
+    L.guards = g_guards.load() != 0;
+    L.nguard = 0;
+    L.total = 0;
+  }
+  void place(int i, size_t bytes) {
+    off[i] = L.total;
+    L.total += ((bytes + 255) & ~(size_t)255) + (L.guards ? kGuardBytes : 0);
+    if (!L.guards) return;
+    const size_t g = off[i] + ((bytes + 3) & ~(size_t)3);
+    L.g_off[L.nguard] = g;
+    L.g_len[L.nguard] = (uint32_t)(L.total - g);
+    L.g_tag[L.nguard++] = kOpTag + i;
+  }
+  void done() {
+    L.status_off = L.total;
+    if (L.guards) L.total += 256;
+  }
+  template <class Tp>
+  Tp* at(void* ws, int i) const {
+    return (Tp*)((char*)ws + off[i]);
+  }
+};
+
+template <class F>
+int guarded(const OpLayout& o, void* ws, mebp_stream_t stream, F&& body) {
+  if (!o.L.guards) return body();
+  int e = guard_launch(o.L, ws, (hipStream_t)stream, true);
+  if (e || (e = body())) return e;
+  return guard_verdict(o.L, ws, (hipStream_t)stream);
 }
 
 // Runs `body` (the launches of one entry point on `stream`) between a fill and a check of
@@ -1776,6 +1819,235 @@ int mebp_test_gemm(int32_t kind, const mebp_q4* w, int32_t n_out, int32_t n_in, 
   }
   HIP_TRY(launch_gemm_probe(kind, w->q4, w->scale, n_out, n_in, x, M, out, (hipStream_t)stream));
   return MEBP_OK;
+}
+
+}  // extern "C"
+
+namespace {
+// ------------------------------------------------------------------ operators on logits
+constexpr int kMaxTop = 64;
+
+int check_logits_shape(int rows, int vocab, int top_k) {
+  if (rows < 0 || vocab < 1) return fail(MEBP_EINVAL, "logits: rows %d < 0 or vocab %d < 1", rows, vocab);
+  if (rows > (1 << 23) || vocab > (1 << 30))
+    return fail(MEBP_EUNSUPPORTED, "logits: %d x %d above 2^23 rows or 2^30 columns", rows, vocab);
+  if (top_k < 0 || top_k > kMaxTop) return fail(MEBP_EUNSUPPORTED, "top_k %d not in [0, %d]", top_k, kMaxTop);
+  return MEBP_OK;
+}
+
+size_t logit_size(int dtype) { return dtype == MEBP_F32 ? 4 : 2; }
+
+int check_logits(const mebp_logits* z, const char* what) {
+  if (!z) return fail(MEBP_EINVAL, "%s is NULL", what);
+  int e;
+  if ((e = check_logits_shape(z->rows, z->vocab, 0))) return e;
+  if (z->dtype < MEBP_F32 || z->dtype > MEBP_BF16) return fail(MEBP_EINVAL, "%s: dtype %d unknown", what, z->dtype);
+  if (z->ld < z->vocab) return fail(MEBP_EINVAL, "%s: ld %lld < vocab %d", what, (long long)z->ld, z->vocab);
+  if (z->ld > ((int64_t)1 << 32)) return fail(MEBP_EUNSUPPORTED, "%s: ld %lld above 2^32", what, (long long)z->ld);
+  if (z->rows && !z->data) return fail(MEBP_EINVAL, "%s: data is NULL", what);
+  if (!aligned(z->data, logit_size(z->dtype))) return fail(MEBP_EINVAL, "%s: data not aligned to its elements", what);
+  return MEBP_OK;
+}
+
+int check_grad_logits(const mebp_logits* z, const mebp_logits* dz) {
+  int e;
+  if ((e = check_logits(dz, "dz"))) return e;
+  if (dz->rows != z->rows || dz->vocab != z->vocab) return fail(MEBP_EINVAL, "dz: not of the logits' rows and vocab");
+  if (!z->rows || (dz->data == z->data && dz->ld == z->ld && dz->dtype == z->dtype)) return MEBP_OK;
+  auto bytes = [](const mebp_logits* m) { return ((size_t)(m->rows - 1) * m->ld + m->vocab) * logit_size(m->dtype); };
+  const uintptr_t a = (uintptr_t)z->data, b = (uintptr_t)dz->data;
+  if (a < b + bytes(dz) && b < a + bytes(z))
+    return fail(MEBP_EINVAL, "dz overlaps the logits without being them (same data, ld and dtype)");
+  return MEBP_OK;
+}
+
+// operands of 4 bytes for each of `rows` rows, or for each of their entries
+int check_words(const void* p, int rows, const char* what) {
+  if (!rows) return MEBP_OK;
+  if (!p) return fail(MEBP_EINVAL, "%s is NULL", what);
+  if (!aligned(p, 4)) return fail(MEBP_EINVAL, "%s not 4-byte aligned", what);
+  return MEBP_OK;
+}
+
+int check_temperature(float tau) {
+  if (!(tau >= 1e-6f && tau <= 1e6f)) return fail(MEBP_EINVAL, "temperature %g not in [1e-6, 1e6]", tau);
+  return MEBP_OK;
+}
+
+OpLayout logits_layout(int rows, int vocab, int top_k, LogitSplit* s) {
+  OpLayout o;
+  *s = logit_split(rows, vocab);
+  o.place(OP_STATS, (size_t)rows * s->n * sizeof(float4));
+  o.place(OP_KEYS, (size_t)rows * s->n * top_k * 8);
+  o.place(OP_PICKED, (size_t)rows * (kMaxTop + 1) * 4);
+  o.done();
+  return o;
+}
+
+int check_op_ws(const OpLayout& o, const void* ws, size_t ws_bytes) {
+  if (!ws) return fail(MEBP_EINVAL, "workspace is NULL");
+  if (!aligned(ws, 256)) return fail(MEBP_EINVAL, "workspace not 256-byte aligned");
+  if (ws_bytes < o.L.total) return fail(MEBP_EWORKSPACE, "workspace %zu bytes < required %zu", ws_bytes, o.L.total);
+  return MEBP_OK;
+}
+
+void set_slots(const OpLayout& o, void* ws, LogitSplit* s) {
+  s->stats = o.at<float4>(ws, OP_STATS);
+  s->keys = o.at<unsigned long long>(ws, OP_KEYS);
+  s->picked = o.at<float>(ws, OP_PICKED);
+}
+
+// log2(e) / tau, and the rise of a logit in which the largest weight of the call's softmaxes grows 2^32 times
+float exp2_scale(float tau) { return (float)(1.4426950408889634 / (double)tau); }
+float reference_lift(float c, bool unit) { return 32.0f / (unit ? std::max(c, 1.4426950408889634f) : c); }
+
+int check_scores(const int32_t* targets, float tau, int rows, int top_k, const mebp_token_scores* out) {
+  int e;
+  if ((e = check_temperature(tau))) return e;
+  if (!out) return fail(MEBP_EINVAL, "out is NULL");
+  if (out->logp && (e = check_words(targets, rows, "targets"))) return e;
+  const void* p[5] = {out->logp, out->lse, out->entropy, out->top_ids, out->top_logp};
+  bool any = false;
+  for (const void* q : p) {
+    any |= q != nullptr;
+    if (q && !aligned(q, 4)) return fail(MEBP_EINVAL, "an output is not 4-byte aligned");
+  }
+  if (!any && rows) return fail(MEBP_EINVAL, "no output requested");
+  if (!top_k && (out->top_ids || out->top_logp)) return fail(MEBP_EINVAL, "top_ids or top_logp with top_k 0");
+  return MEBP_OK;
+}
+
+int check_distill(const mebp_distill* d, int rows, const float* row_loss) {
+  int e;
+  if (!d) return fail(MEBP_EINVAL, "distill is NULL");
+  if ((e = check_temperature(d->temperature))) return e;
+  if (!(d->alpha >= 0.f && d->alpha <= 1.f)) return fail(MEBP_EINVAL, "alpha %g not in [0, 1]", d->alpha);
+  if (d->k < 1 || d->k > kMaxTop) return fail(MEBP_EUNSUPPORTED, "k %d not in [1, %d]", d->k, kMaxTop);
+  if ((e = check_words(d->ids, rows, "ids")) || (e = check_words(d->logits, rows, "teacher logits"))) return e;
+  if (d->alpha < 1.f && (e = check_words(d->targets, rows, "targets"))) return e;
+  if (d->row_weight && (e = check_words(d->row_weight, rows, "row_weight"))) return e;
+  return check_words(row_loss, rows, "row_loss");
+}
+
+ScoreArgs score_args(const mebp_logits& z, const int32_t* targets, float tau, int top_k, const mebp_token_scores& out,
+                     const LogitSplit& s) {
+  ScoreArgs a{};
+  a.z = z.data;
+  a.ld = (size_t)z.ld;
+  a.rows = z.rows;
+  a.vocab = z.vocab;
+  a.top_k = out.top_ids || out.top_logp ? top_k : 0;
+  a.targets = targets;
+  a.inv_tau = 1.0f / tau;
+  a.c = exp2_scale(tau);
+  a.lift = reference_lift(a.c, false);
+  a.logp = out.logp;
+  a.lse = out.lse;
+  a.entropy = out.entropy;
+  a.top_ids = out.top_ids;
+  a.top_logp = out.top_logp;
+  a.split = s;
+  return a;
+}
+
+DistillArgs distill_args(const mebp_logits& z, const mebp_distill& d, float* row_loss, const mebp_logits* dz,
+                         const LogitSplit& s) {
+  DistillArgs a{};
+  a.z = z.data;
+  a.ld = (size_t)z.ld;
+  a.dz = dz ? dz->data : nullptr;
+  a.ldd = dz ? (size_t)dz->ld : 0;
+  a.rows = z.rows;
+  a.vocab = z.vocab;
+  a.k = d.k;
+  a.ids = d.ids;
+  a.logits = d.logits;
+  a.targets = d.targets;
+  a.weight = d.row_weight;
+  a.tau = d.temperature;
+  a.inv_tau = 1.0f / d.temperature;
+  a.alpha = d.alpha;
+  a.c = exp2_scale(d.temperature);
+  a.lift = reference_lift(a.c, d.alpha < 1.f && d.temperature != 1.f);
+  a.loss = row_loss;
+  a.split = s;
+  return a;
+}
+}  // namespace
+
+extern "C" {
+
+size_t mebp_logits_workspace_bytes(int32_t rows, int32_t vocab, int32_t top_k) {
+  std::string saved = g_last_error;
+  if (check_logits_shape(rows, vocab, top_k)) {
+    g_last_error = saved;
+    return 0;
+  }
+  LogitSplit s;
+  return std::max<size_t>(logits_layout(rows, vocab, top_k, &s).L.total, 256);
+}
+
+int mebp_token_logprobs(const mebp_logits* z, const int32_t* targets, float temperature, int32_t top_k,
+                        const mebp_token_scores* out, void* ws, size_t ws_bytes, mebp_stream_t stream) {
+  int e;
+  if ((e = check_logits(z, "logits")) || (e = check_logits_shape(z->rows, z->vocab, top_k)) ||
+      (e = check_scores(targets, temperature, z->rows, top_k, out)))
+    return e;
+  LogitSplit s;
+  const OpLayout o = logits_layout(z->rows, z->vocab, top_k, &s);
+  if ((e = check_op_ws(o, ws, ws_bytes))) return e;
+  if (!z->rows) return MEBP_OK;
+  set_slots(o, ws, &s);
+  return guarded(o, ws, stream, [&] {
+    HIP_TRY(launch_scores(score_args(*z, targets, temperature, top_k, *out, s), z->dtype, (hipStream_t)stream));
+    return (int)MEBP_OK;
+  });
+}
+
+int mebp_token_logprobs_backward(const mebp_logits* z, const int32_t* targets, float temperature, const float* lse,
+                                 const float* entropy, const float* d_logp, const float* d_entropy,
+                                 const mebp_logits* dz, mebp_stream_t stream) {
+  int e;
+  if ((e = check_logits(z, "logits")) || (e = check_temperature(temperature)) || (e = check_grad_logits(z, dz)) ||
+      (e = check_words(lse, z->rows, "lse")))
+    return e;
+  const int rows = z->rows;
+  if (rows && !d_logp && !d_entropy) return fail(MEBP_EINVAL, "neither d_logp nor d_entropy");
+  if (d_logp && ((e = check_words(d_logp, rows, "d_logp")) || (e = check_words(targets, rows, "targets")))) return e;
+  if (d_entropy && ((e = check_words(d_entropy, rows, "d_entropy")) || (e = check_words(entropy, rows, "entropy")))) return e;
+  if (!z->rows) return MEBP_OK;
+  ScoreGradArgs a{};
+  a.z = z->data;
+  a.dz = dz->data;
+  a.ld = (size_t)z->ld;
+  a.ldd = (size_t)dz->ld;
+  a.rows = z->rows;
+  a.vocab = z->vocab;
+  a.targets = targets;
+  a.lse = lse;
+  a.entropy = entropy;
+  a.d_logp = d_logp;
+  a.d_entropy = d_entropy;
+  a.inv_tau = 1.0f / temperature;
+  a.split = logit_split(z->rows, z->vocab);
+  HIP_TRY(launch_scores_grad(a, z->dtype, dz->dtype, (hipStream_t)stream));
+  return MEBP_OK;
+}
+
+int mebp_distill_topk(const mebp_logits* z, const mebp_distill* d, float* row_loss, const mebp_logits* dz, void* ws,
+                      size_t ws_bytes, mebp_stream_t stream) {
+  int e;
+  if ((e = check_logits(z, "logits")) || (e = check_distill(d, z->rows, row_loss)) || (dz && (e = check_grad_logits(z, dz))))
+    return e;
+  LogitSplit s;
+  const OpLayout o = logits_layout(z->rows, z->vocab, 0, &s);
+  if ((e = check_op_ws(o, ws, ws_bytes))) return e;
+  if (!z->rows) return MEBP_OK;
+  set_slots(o, ws, &s);
+  return guarded(o, ws, stream, [&] {
+    HIP_TRY(launch_distill(distill_args(*z, *d, row_loss, dz, s), z->dtype, dz ? dz->dtype : 0, (hipStream_t)stream));
+    return (int)MEBP_OK;
+  });
 }
 
 int mebp_kernel_timing(int32_t enable, int32_t capacity) {

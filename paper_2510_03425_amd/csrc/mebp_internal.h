@@ -383,6 +383,56 @@ hipError_t launch_ce_loss(const float* row_loss, const int32_t* tgt, int M, floa
 hipError_t launch_copy_host(const void* src, void* dst, size_t bytes, hipStream_t st);
 hipError_t launch_targets(const int32_t* ids, int B, int T, int V, int32_t* tgt, hipStream_t st);
 
+// ---------------------------------------------------------------- operators on logits
+enum { LOGIT_F32 = 0, LOGIT_F16 = 1, LOGIT_BF16 = 2 };  // as MEBP_F32 .. of the C ABI
+// A row in n parts of `cols` columns, and what the parts leave for the launch that joins them:
+// stats [rows][n] (reference, sum, weighted sum, sum at temperature 1), keys [rows][n][top_k] and
+// the student's logits at the teacher's entries and the target, picked [rows][65].
+constexpr int kLogitParts = 64;
+struct LogitSplit {
+  int n, cols;
+  float4* stats;
+  unsigned long long* keys;
+  float* picked;
+};
+LogitSplit logit_split(int rows, int vocab);  // n and cols
+struct ScoreArgs {
+  const void* z;
+  size_t ld;
+  int rows, vocab, top_k;
+  const int32_t* targets;
+  float inv_tau, c, lift;  // 1 / tau, log2(e) / tau, and the rise of a logit that moves a reference
+  float *logp, *lse, *entropy, *top_logp;
+  int32_t* top_ids;
+  LogitSplit split;
+};
+hipError_t launch_scores(ScoreArgs a, int dtype, hipStream_t st);
+struct ScoreGradArgs {
+  const void* z;
+  void* dz;                // may be z, of the same type and pitch
+  size_t ld, ldd;
+  int rows, vocab;
+  const int32_t* targets;
+  const float *lse, *entropy, *d_logp, *d_entropy;
+  float inv_tau;
+  LogitSplit split;        // (n and cols alone)
+};
+hipError_t launch_scores_grad(ScoreGradArgs a, int dtype, int gtype, hipStream_t st);
+struct DistillArgs {
+  const void* z;
+  void* dz;                // null: the loss alone; may be z, of the same type and pitch
+  size_t ld, ldd;
+  int rows, vocab, k;
+  const int32_t* ids;      // [rows][k], < 0: no entry
+  const float* logits;     // [rows][k]
+  const int32_t* targets;  // [rows], read where alpha < 1
+  const float* weight;     // [rows] or null
+  float tau, inv_tau, alpha, c, lift;
+  float* loss;             // [rows]
+  LogitSplit split;
+};
+hipError_t launch_distill(DistillArgs a, int dtype, int gtype, hipStream_t st);
+
 // ---------------------------------------------------------------- diagnostics
 // Per-kernel event timing (see timing.hip). timer_begin returns -1 when disabled.
 // count: launches bracketed by this record (a repeated burst counts as `count` launches)

@@ -8,6 +8,7 @@ training step runs inside ``libmebp.so``.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 from typing import List, Optional
 
 import numpy as np
@@ -42,6 +43,117 @@ def _dev(a: np.ndarray, device) -> torch.Tensor:
 
 def ptr(t: Optional[torch.Tensor]) -> int:
     return 0 if t is None else t.data_ptr()
+
+
+# ---------------------------------------------------------------- operators on logits
+LOGIT_TYPE = {torch.float32: L.MEBP_F32, torch.float16: L.MEBP_F16, torch.bfloat16: L.MEBP_BF16}
+
+
+def _on_device(f):
+    """Runs with the first tensor's device current: the library launches there, on torch's
+    current stream of that device."""
+    @functools.wraps(f)
+    def g(z, *a, **kw):
+        if z.device.type != "cuda":
+            raise ValueError("logits must be on the GPU")
+        if z.device.index == torch.cuda.current_device():
+            return f(z, *a, **kw)
+        with torch.cuda.device(z.device):
+            return f(z, *a, **kw)
+    return g
+
+
+def logits_struct(z: torch.Tensor) -> L.MebpLogits:
+    """[rows][vocab] logits (or their gradient) whose columns follow one another."""
+    if z.dim() != 2 or z.dtype not in LOGIT_TYPE or (z.stride(1) != 1 and z.shape[1] > 1):
+        raise ValueError("logits must be a fp32, fp16 or bf16 matrix with contiguous rows")
+    rows, vocab = z.shape
+    return L.MebpLogits(z.data_ptr(), z.stride(0) if rows > 1 else vocab, rows, vocab, LOGIT_TYPE[z.dtype])
+
+
+def _operand(t: Optional[torch.Tensor], dtype, shape, like: torch.Tensor, what: str) -> int:
+    """Address of an operand, None as NULL."""
+    if t is None:
+        return 0
+    if t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous() or t.device != like.device:
+        raise ValueError(f"{what} must be contiguous {dtype} {shape} on {like.device}")
+    return t.data_ptr()
+
+
+def _logits_ws(ws: Optional[torch.Tensor], z: torch.Tensor, top_k: int):
+    """The given workspace, or one that lives until the stream is done with it."""
+    if ws is None:
+        n = L.mebp_logits_workspace_bytes(z.shape[0], z.shape[1], top_k)
+        ws = torch.empty(max(n, 256), dtype=torch.uint8, device=z.device)
+    elif ws.device != z.device or not ws.is_contiguous():
+        raise ValueError(f"workspace must be contiguous on {z.device}")
+    return ws, ws.numel() * ws.element_size()
+
+
+@_on_device
+def token_logprobs(z: torch.Tensor, targets: Optional[torch.Tensor] = None, top_k: int = 0, temperature: float = 1.0,
+                   out: Optional[dict] = None, ws: Optional[torch.Tensor] = None) -> dict:
+    """``mebp_token_logprobs`` of logits [rows][vocab]: a dict of fp32 ``logp`` (with int32
+    ``targets``), ``lse``, ``entropy`` [rows] and, with ``top_k``, int32 ``top_ids`` and ``top_logp``
+    [rows][top_k]. ``out``: the wanted ones of these as tensors to write into."""
+    n = z.shape[0]
+    if out is None:
+        names = ["lse", "entropy"] + (["logp"] if targets is not None else [])
+        out = {k: torch.empty(n, dtype=torch.float32, device=z.device) for k in names}
+        if top_k > 0:
+            out["top_ids"] = torch.empty((n, top_k), dtype=torch.int32, device=z.device)
+            out["top_logp"] = torch.empty((n, top_k), dtype=torch.float32, device=z.device)
+    s = L.MebpTokenScores()
+    for k, t in out.items():
+        top = k.startswith("top_")
+        setattr(s, k, _operand(t, torch.int32 if k == "top_ids" else torch.float32, (n, top_k) if top else (n,), z, k))
+    zs = logits_struct(z)
+    ws, nb = _logits_ws(ws, z, top_k)
+    L.mebp_token_logprobs(zs, _operand(targets, torch.int32, (n,), z, "targets"), temperature, top_k, s, ws.data_ptr(),
+                          nb, stream_handle())
+    return out
+
+
+@_on_device
+def token_logprobs_backward(z: torch.Tensor, targets: Optional[torch.Tensor], lse: torch.Tensor,
+                            entropy: Optional[torch.Tensor], d_logp: Optional[torch.Tensor],
+                            d_entropy: Optional[torch.Tensor] = None, dz: Optional[torch.Tensor] = None,
+                            temperature: float = 1.0) -> torch.Tensor:
+    """``mebp_token_logprobs_backward``: the gradient w.r.t. the logits, into ``dz`` (any logits
+    type; ``z`` itself for one in place) or a new tensor of their type."""
+    n = (z.shape[0],)
+    if dz is None:
+        dz = torch.empty(z.shape, dtype=z.dtype, device=z.device)
+    f32 = torch.float32
+    if dz.device != z.device:
+        raise ValueError(f"dz must be on {z.device}")
+    L.mebp_token_logprobs_backward(logits_struct(z), _operand(targets, torch.int32, n, z, "targets"), temperature,
+                                   _operand(lse, f32, n, z, "lse"), _operand(entropy, f32, n, z, "entropy"),
+                                   _operand(d_logp, f32, n, z, "d_logp"), _operand(d_entropy, f32, n, z, "d_entropy"),
+                                   logits_struct(dz), stream_handle())
+    return dz
+
+
+@_on_device
+def distill_topk(z: torch.Tensor, ids: torch.Tensor, logits: torch.Tensor, row_loss: Optional[torch.Tensor] = None,
+                 dz: Optional[torch.Tensor] = None, temperature: float = 1.0, alpha: float = 1.0,
+                 targets: Optional[torch.Tensor] = None, row_weight: Optional[torch.Tensor] = None,
+                 ws: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """``mebp_distill_topk``: the loss of each row against a teacher's int32 ``ids`` and fp32
+    ``logits`` [rows][k], and its gradient into ``dz`` where that is given."""
+    n, k = z.shape[0], ids.shape[-1]
+    if row_loss is None:
+        row_loss = torch.empty(n, dtype=torch.float32, device=z.device)
+    if dz is not None and dz.device != z.device:
+        raise ValueError(f"dz must be on {z.device}")
+    d = L.MebpDistill(_operand(ids, torch.int32, (n, k), z, "ids"), _operand(logits, torch.float32, (n, k), z, "logits"),
+                      _operand(targets, torch.int32, (n,), z, "targets"),
+                      _operand(row_weight, torch.float32, (n,), z, "row_weight"), k, temperature, alpha)
+    zs = logits_struct(z)
+    ws, nb = _logits_ws(ws, z, 0)
+    L.mebp_distill_topk(zs, d, _operand(row_loss, torch.float32, (n,), z, "row_loss"),
+                        None if dz is None else logits_struct(dz), ws.data_ptr(), nb, stream_handle())
+    return row_loss
 
 
 class DeviceModel:
