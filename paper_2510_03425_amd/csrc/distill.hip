@@ -80,9 +80,7 @@ __global__ __launch_bounds__(NT) void k_distill_stats(DistillArgs p) {
   const T* z = (const T*)p.z + row * p.ld;
   const int v0 = part * p.split.cols, v1 = min(p.vocab, v0 + p.split.cols);
   Acc a = acc_empty();
-  scan<T, NT, 4, false>(z, v0, v1, [&](const float(&x)[kVec<T>], int) {
-    acc_add<false, TWO>(a, x, max_of(x), p.c, kLog2e, p.lift);
-  });
+  scan<T, NT, 4, false>(z, v0, v1, [&](const auto& g) { acc_add<false, TWO>(a, g, p.c, kLog2e, p.lift); });
   acc_block<NT, false, TWO>(a, p.c, kLog2e, red);
   if (threadIdx.x >= 64) return;
   const int l = lane_id();

@@ -79,20 +79,35 @@ DEV u64 merge64(u64 a, u64 b) {
 
 constexpr int top_buffer(int n) { return 64 + 64 * n; }  // keys of a wave's buffer, vectors of n logits
 
-// The threshold of a wave: its own k-th largest logit so far; or, where it is higher, the least of
-// the waves' ceil(k / waves)-th largest, which k logits of the row reach as well (`share`, which
-// only ever rises: an old value is a valid bound too). Columns rise from one vector of a wave to
-// the next, so a logit that equals the wave's own k-th ranks behind it; one that equals another
-// wave's may not, so that bound counts from the next value below it. 64 alternatives of 262144
-// random logits on 8 waves: about 100 logits of a wave get into its buffer.
+// The threshold that a logit has to be above to be buffered comes from the lanes' largest logits so
+// far: of each wave the ceil(k / waves)-th largest of its lanes' (to 2^-16 of it, by bisection), and
+// of the waves the least. k lanes of the row at least have reached it, so it bounds the row's k-th
+// logit from below; it is not far below, as the top logits are mostly in different lanes. `share`
+// holds each wave's bound, which only rises: an older one is valid too. Taken anew whenever the
+// groups seen have doubled, it lets about as many logits through between two of these times, some
+// 16 of a wave for 64 alternatives on 8 waves.
+//
+// A wave whose list has filled up has its own k-th as a second threshold: columns rise from one
+// vector of a wave to the next, so a logit that equals it ranks behind it. One that equals another
+// wave's bound may rank before, so that one counts from the next value below it.
 template <int NW>
 struct Top {
   u64 list;    // this lane's key of the sorted list
   float thr;   // only logits above it can be among the first k
+  float most;  // this lane's largest logit
   int cnt, k;  // buffered keys, k (both the same in all lanes)
+  int groups;  // seen
   u64* buf;
   uint32_t* share;  // [NW] order bits
 
+  __device__ __forceinline__ void start(int top_k, u64* b, uint32_t* sh) {
+    list = 0;
+    thr = most = -INFINITY;
+    cnt = groups = 0;
+    k = top_k;
+    buf = b;
+    share = sh;
+  }
   __device__ __forceinline__ void fence() const {
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
@@ -111,13 +126,15 @@ struct Top {
     fence();
     list = merge64(list, sort64(key));
   }
-  __device__ __forceinline__ void own_threshold() {
-    const uint32_t kth = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(list >> 32), k - 1);
-    if (kth) thr = fmaxf(thr, order_value(kth));
-    if (NW > 1) {
-      const uint32_t part = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(list >> 32), (k + NW - 1) / NW - 1);
-      if (lane_id() == 0) __hip_atomic_store(share + (threadIdx.x >> 6), part, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+  __device__ __forceinline__ void publish() {
+    const int part = (k + NW - 1) / NW;
+    const uint32_t o = order_bits(most);
+    uint32_t t = 0;
+    for (int bit = 31; bit >= 8; --bit) {
+      const uint32_t up = t | 1u << bit;
+      if (__popcll(__ballot(o >= up)) >= part) t = up;
     }
+    if (lane_id() == 0) __hip_atomic_store(share + (threadIdx.x >> 6), t, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
   }
   __device__ __forceinline__ void shared_threshold() {
     uint32_t least = 0xffffffffu;
@@ -126,39 +143,41 @@ struct Top {
       least = min(least, __hip_atomic_load(share + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP));
     thr = fmaxf(thr, below(least));
   }
-  // a first threshold: what the largest logits of k lanes reach, to 2^-16 of the value
-  __device__ __forceinline__ void first_threshold(float vmax) {
-    const uint32_t o = vmax == vmax ? order_bits(vmax) : 0u;
-    uint32_t t = 0;
-    for (int bit = 31; bit >= 8; --bit) {
-      const uint32_t up = t | 1u << bit;
-      if (__popcll(__ballot(o >= up)) >= k) t = up;
-    }
-    thr = below(t);
-  }
 
-  template <int N>
-  __device__ __forceinline__ void add(const float (&x)[N], float vmax, int col) {
-    if (!__any(vmax > thr)) return;
-    if (thr == -INFINITY)
-      first_threshold(vmax);
-    else if (NW > 1)
-      shared_threshold();
-    if (!__any(vmax > thr)) return;
-#pragma unroll
-    for (int j = 0; j < N; ++j) {
-      const bool p = x[j] > thr;
-      const u64 mask = __ballot(p);
-      if (!mask) continue;
-      if (p)
-        buf[cnt + (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0))] =
-            order_key(x[j], col + j);
-      cnt += __popcll(mask);
+  template <int U, int N>
+  __device__ __forceinline__ void add(const Group<U, N>& g) {
+    most = fmaxf(most, g.top);
+    const int seen = ++groups;
+    if ((seen & (seen - 1)) == 0) {
+      publish();
+      if (seen == 1) {
+        __syncthreads();  // (every wave has a first group)
+        shared_threshold();
+      }
     }
-    if (cnt < 64) return;
-    do flush(64);
-    while (cnt >= 64);
-    own_threshold();
+    if (!__any(g.top > thr)) return;
+    shared_threshold();
+    if (!__any(g.top > thr)) return;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (u >= g.n) break;
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        const float x = g.x[u][j];
+        const bool p = x > thr;
+        const u64 mask = __ballot(p);
+        if (!mask) continue;
+        if (p)
+          buf[cnt + (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0))] =
+              order_key(x, g.col + u * g.step + j);
+        cnt += __popcll(mask);
+      }
+      if (cnt < 64) continue;
+      do flush(64);
+      while (cnt >= 64);
+      const uint32_t kth = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(list >> 32), k - 1);
+      if (kth) thr = fmaxf(thr, order_value(kth));
+    }
   }
 
   // joins the waves' lists into the first wave's; lists: [NW / 2][64]
@@ -219,15 +238,11 @@ __global__ __launch_bounds__(NT) void k_scores(ScoreArgs p) {
   const T* z = (const T*)p.z + row * p.ld;
   const int v0 = part * p.split.cols, v1 = min(p.vocab, v0 + p.split.cols);
   Acc a = acc_empty();
-  Top<NW> t{0ull, -INFINITY, 0, p.top_k, buf + (threadIdx.x >> 6) * B, share};
-  if (TOP) {
-    if (threadIdx.x < NW) share[threadIdx.x] = 0u;
-    __syncthreads();
-  }
-  scan<T, NT, 4, true>(z, v0, v1, [&](const float(&x)[kVec<T>], int col) {
-    const float vmax = max_of(x);
-    acc_add<true, false>(a, x, vmax, p.c, 0.f, p.lift);
-    if constexpr (TOP) t.add(x, vmax, col);
+  Top<NW> t;
+  t.start(p.top_k, buf + (threadIdx.x >> 6) * B, share);
+  scan<T, NT, 4, true>(z, v0, v1, [&](const auto& g) {
+    acc_add<true, false>(a, g, p.c, 0.f, p.lift);
+    if constexpr (TOP) t.add(g);
   });
   acc_block<NT, true, false>(a, p.c, 0.f, red);
   if constexpr (TOP) t.join(buf);
@@ -246,7 +261,8 @@ __global__ __launch_bounds__(256) void k_scores_join(ScoreArgs p) {
   __shared__ u64 lists[2 * 64];
   const size_t row = blockIdx.x;
   const int l = lane_id(), wave = threadIdx.x >> 6;
-  Top<4> t{0ull, 0.f, 0, p.top_k, nullptr, nullptr};
+  Top<4> t;
+  t.start(p.top_k, nullptr, nullptr);
   if (p.top_k) {
     for (int i = wave; i < p.split.n; i += 4)
       t.list = merge64(t.list, l < p.top_k ? p.split.keys[(row * p.split.n + i) * p.top_k + l] : 0ull);

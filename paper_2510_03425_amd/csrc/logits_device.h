@@ -119,37 +119,41 @@ DEV void acc_move(Acc& a, float M, float c, float c1) {
   a.m = M;
 }
 
-// Adds N logits. The reference only follows where a logit lies more than `lift` above it, 2^6 times
+// The logits that scan() hands over at a time: `n` (all lanes alike) of U vectors, vector u of this
+// lane at columns col + u * step ..
+template <int U, int N>
+struct Group {
+  float x[U][N], top;  // top: the largest of them (NaN left out)
+  int n, col, step;
+};
+
+// Adds a group. The reference only follows where a logit lies more than `lift` above it, 2^6 times
 // its weight: fp32 holds the sums nearly as well with a stale one (the entropy's error grows with
-// the distance to the largest logit), and few vectors move it. A vector is summed by itself first,
+// the distance to the largest logit), and few groups move it. A vector is summed by itself first,
 // which leaves a lane an 8th (4th) of the additions in a row. NaN and +inf logits make s NaN:
 // exp(NaN), and exp(inf - inf).
-template <bool ENT, bool TWO, int N>
-DEV void acc_add(Acc& a, const float (&x)[N], float vmax, float c, float c1, float lift) {
-  if (vmax > a.m + lift) acc_move<ENT, TWO>(a, vmax, c, c1);
-  float s = 0.f, w = 0.f, s1 = 0.f;
+template <bool ENT, bool TWO, int U, int N>
+DEV void acc_add(Acc& a, const Group<U, N>& g, float c, float c1, float lift) {
+  if (g.top > a.m + lift) acc_move<ENT, TWO>(a, g.top, c, c1);
 #pragma unroll
-  for (int j = 0; j < N; ++j) {
-    const float d = x[j] - a.m;
-    const float e = exp2_fast(d * c);
-    s = j ? s + e : e;
-    // (a logit of -inf has weight 0, and 0 times -inf is not)
-    const float dw = fmaxf(d, -1e30f);
-    if (ENT) w = j ? fmaf(e, dw, w) : e * dw;
-    const float e1 = TWO ? exp2_fast(d * c1) : 0.f;
-    s1 = j ? s1 + e1 : e1;
+  for (int u = 0; u < U; ++u) {
+    if (u >= g.n) break;
+    float s = 0.f, w = 0.f, s1 = 0.f;
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      const float d = g.x[u][j] - a.m;
+      const float e = exp2_fast(d * c);
+      s = j ? s + e : e;
+      // (a logit of -inf has weight 0, and 0 times -inf is not)
+      const float dw = fmaxf(d, -1e30f);
+      if (ENT) w = j ? fmaf(e, dw, w) : e * dw;
+      const float e1 = TWO ? exp2_fast(d * c1) : 0.f;
+      s1 = j ? s1 + e1 : e1;
+    }
+    a.s += s;
+    if (ENT) a.w += w;
+    if (TWO) a.s1 += s1;
   }
-  a.s += s;
-  if (ENT) a.w += w;
-  if (TWO) a.s1 += s1;
-}
-
-template <int N>
-DEV float max_of(const float (&x)[N]) {
-  float m = x[0];
-#pragma unroll
-  for (int j = 1; j < N; ++j) m = fmaxf(m, x[j]);
-  return m;
 }
 
 template <bool ENT, bool TWO>
@@ -195,47 +199,58 @@ DEV Acc join_parts(const LogitSplit& sp, size_t row, float c, float c1) {
   return a;
 }
 
-// Hands columns v0 .. v1 of a row to add(x, col), kVec of them a time in each lane and -inf behind
-// the end, columns rising from call to call: U loads of each lane are in flight ahead of the group
-// that is worked on.
+// Hands columns v0 .. v1 of a row to add(group), -inf in the place of columns behind the end; columns
+// rise from vector to vector and from group to group. The loads of one group are in flight while
+// the one before it is worked on.
 template <class T, int NT, int U, bool ONCE, class F>
 DEV void scan(const T* row, int v0, int v1, F&& add) {
   constexpr int N = kVec<T>, step = NT * N;
   int i = v0 + (int)threadIdx.x * N, b = v0;
   uint4 next[U];
+  Group<U, N> g;
+  g.n = U;
+  g.step = step;
+  auto top = [&](int n) {
+    g.top = -INFINITY;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (u >= n) break;
+#pragma unroll
+      for (int j = 0; j < N; ++j) g.top = fmaxf(g.top, g.x[u][j]);
+    }
+  };
   if (b + U * step <= v1) {
 #pragma unroll
     for (int u = 0; u < U; ++u) next[u] = load16<ONCE>(row + i + u * step);
     for (; b + U * step <= v1; b += U * step, i += U * step) {
-      uint4 cur[U];
 #pragma unroll
-      for (int u = 0; u < U; ++u) cur[u] = next[u];
+      for (int u = 0; u < U; ++u) unpack<T>(next[u], g.x[u]);
       if (b + 2 * U * step <= v1) {
 #pragma unroll
         for (int u = 0; u < U; ++u) next[u] = load16<ONCE>(row + i + (U + u) * step);
       }
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        float x[N];
-        unpack<T>(cur[u], x);
-        add(x, i + u * step);
-      }
+      g.col = i;
+      top(U);
+      add(g);
     }
   }
+  if (b >= v1) return;
   // fewer than U vectors of each lane are left
+  g.n = (v1 - b + step - 1) / step;
+  g.col = i;
 #pragma unroll
   for (int u = 0; u < U; ++u)
     if (i + u * step + N <= v1) next[u] = load16<ONCE>(row + i + u * step);
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    if (b + u * step >= v1) break;
-    float x[N];
+    if (u >= g.n) break;
     if (i + u * step + N <= v1)
-      unpack<T>(next[u], x);
+      unpack<T>(next[u], g.x[u]);
     else
-      load_tail<T>(row, i + u * step, v1, x);
-    add(x, i + u * step);
+      load_tail<T>(row, i + u * step, v1, g.x[u]);
   }
+  top(g.n);
+  add(g);
 }
 
 // Writes f(z) over columns v0 .. v1 of a row. Every element is read before it is written, by the
