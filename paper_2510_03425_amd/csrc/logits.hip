@@ -20,32 +20,6 @@ DEV float order_value(uint32_t o) {
 }
 DEV u64 order_key(float x, int col) { return (u64)order_bits(x) << 32 | (uint32_t)~col; }
 
-// the value of lane l ^ J: moves inside rows of 16 lanes, swaps of rows and of halves
-template <int CTRL>
-DEV uint32_t dpp(uint32_t x) {
-  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xf, 0xf, true);
-}
-template <int J>
-DEV uint32_t lane_xor(uint32_t x) {
-  if constexpr (J == 1) return dpp<0xB1>(x);                 // quad [1,0,3,2]
-  else if constexpr (J == 2) return dpp<0x4E>(x);            // quad [2,3,0,1]
-  else if constexpr (J == 3) return dpp<0x1B>(x);            // quad [3,2,1,0]
-  else if constexpr (J == 4) return dpp<0x1B>(dpp<0x141>(x));  // 7 ^ 3
-  else if constexpr (J == 7) return dpp<0x141>(x);           // mirror of 8
-  else if constexpr (J == 8) return dpp<0x128>(x);           // rotation by 8 of 16
-  else if constexpr (J == 15) return dpp<0x140>(x);          // mirror of 16
-  else if constexpr (J == 16) {
-    const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
-    return threadIdx.x & 16 ? r[0] : r[1];
-  } else if constexpr (J == 31) return lane_xor<16>(lane_xor<15>(x));
-  else if constexpr (J == 32) {
-    const auto r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
-    return threadIdx.x & 32 ? r[0] : r[1];
-  } else {
-    static_assert(J == 63, "lane_xor");
-    return lane_xor<32>(lane_xor<31>(x));
-  }
-}
 template <int J>
 DEV u64 lane_xor64(u64 x) {
   return (u64)lane_xor<J>((uint32_t)(x >> 32)) << 32 | lane_xor<J>((uint32_t)x);
@@ -144,20 +118,20 @@ struct Top {
     thr = fmaxf(thr, below(least));
   }
 
+  // top: the group's largest logit. The first group's bounds are published by first(), before a
+  // barrier that every wave has to pass before the second.
+  __device__ __forceinline__ void first(float top) {
+    most = top;
+    publish();
+  }
   template <int U, int N>
-  __device__ __forceinline__ void add(const Group<U, N>& g) {
-    most = fmaxf(most, g.top);
+  __device__ __forceinline__ void add(const Group<U, N>& g, float top) {
+    most = fmaxf(most, top);
     const int seen = ++groups;
-    if ((seen & (seen - 1)) == 0) {
-      publish();
-      if (seen == 1) {
-        __syncthreads();  // (every wave has a first group)
-        shared_threshold();
-      }
-    }
-    if (!__any(g.top > thr)) return;
+    if (seen > 1 && (seen & (seen - 1)) == 0) publish();
+    if (!__any(top > thr)) return;
     shared_threshold();
-    if (!__any(g.top > thr)) return;
+    if (!__any(top > thr)) return;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       if (u >= g.n) break;
@@ -237,14 +211,29 @@ __global__ __launch_bounds__(NT) void k_scores(ScoreArgs p) {
   const int part = (int)(blockIdx.x % p.split.n);
   const T* z = (const T*)p.z + row * p.ld;
   const int v0 = part * p.split.cols, v1 = min(p.vocab, v0 + p.split.cols);
-  Acc a = acc_empty();
   Top<NW> t;
   t.start(p.top_k, buf + (threadIdx.x >> 6) * B, share);
+  Sums<true, ONE> sums;
+  bool begun = false;
   scan<T, NT, 4, true>(z, v0, v1, [&](const auto& g) {
-    acc_add<true, false>(a, g, p.c, 0.f, p.lift);
-    if constexpr (TOP) t.add(g);
+    float top = 0.f;
+    if (TOP || !begun) top = g.top();
+    if (!begun) {  // (of every thread: each has a first group)
+      if constexpr (TOP) t.first(top);
+      sums.start(block_max<NT>(top, red), p.c);
+      begun = true;
+    }
+    sums.add(g);
+    if constexpr (TOP) t.add(g, top);
   });
-  acc_block<NT, true, false>(a, p.c, 0.f, red);
+  sums.template join<NT>(red);
+  Acc a = sums.acc();
+  if (!sums.served()) {
+    a = acc_empty();
+    scan<T, NT, 1, false>(z, v0, v1, [&](const auto& g) { acc_add<true, false>(a, g, p.c, 0.f, p.lift); });
+    __syncthreads();
+    acc_block<NT, true, false>(a, p.c, 0.f, red);
+  }
   if constexpr (TOP) t.join(buf);
   if (threadIdx.x >= 64) return;
   if (p.split.n == 1) {
@@ -343,7 +332,12 @@ hipError_t launch_scores(ScoreArgs a, int dtype, hipStream_t st) {
   });
 }
 
+// The gradient goes by parts of 8192 columns whatever the rows: 4 loads of each lane of 256 in flight
+// in 16 bits, and many small workgroups leave no part of the chip waiting (1024 x 151936 bf16 110 us,
+// 5.6 TB/s; a workgroup per row 125 .. 130 us).
 hipError_t launch_scores_grad(ScoreGradArgs a, int dtype, int gtype, hipStream_t st) {
+  a.split.cols = 8192;
+  a.split.n = (a.vocab + a.split.cols - 1) / a.split.cols;
   const unsigned grid = (unsigned)((size_t)a.rows * a.split.n);
   const double bytes = (double)a.rows * a.vocab * (type_bytes(dtype) + type_bytes(gtype));
   return by_type(dtype, [&](auto* tp) {

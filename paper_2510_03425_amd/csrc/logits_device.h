@@ -3,9 +3,9 @@
 //
 // Every row is a softmax over tens of thousands of logits, and all that a row gives besides its
 // gradient is a few numbers: the floor is the logits read once and the gradient written once.
-// One pass keeps, per lane, a reference m, s = sum exp((z - m) / tau) and w = sum exp(..) (z - m);
-// lanes, waves and parts of a row are joined by rescaling to the largest reference. The order of
-// all sums is fixed by the shape alone.
+// One pass keeps a reference m, s = sum exp((z - m) / tau) and w = sum exp(..) (z - m); sums at several
+// references are joined by rescaling to the largest. The order of all sums is fixed by the shape
+// alone.
 #pragma once
 #include <float.h>
 
@@ -30,13 +30,14 @@ DEV float cvt(float x) { return x; }
 DEV float cvt(f16 x) { return (float)x; }
 DEV float cvt(bf16 x) { return (float)x; }
 
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
 template <class T>
-DEV void unpack(uint4 v, float (&x)[kVec<T>]) {
-  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+DEV void unpack(u32x4 w, float (&x)[kVec<T>]) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     if constexpr (sizeof(T) == 4) {
-      x[i] = __builtin_bit_cast(float, w[i]);
+      x[i] = __builtin_bit_cast(float, (uint32_t)w[i]);
     } else if constexpr (__is_same(T, f16)) {
       x[2 * i] = f16_lo(w[i]);
       x[2 * i + 1] = f16_hi(w[i]);
@@ -55,10 +56,9 @@ typedef uint32_t u32x2_2 __attribute__((ext_vector_type(2), aligned(2)));
 // ONCE: the logits are read by this pass alone. Non-temporal loads read 7.0 .. 7.2 TB/s where
 // ordinary ones read 6.2 (2 GiB, 4 loads of each lane in flight).
 template <bool ONCE, class T>
-DEV uint4 load16(const T* p) {
+DEV u32x4 load16(const T* p) {
   const u32x4_2* q = (const u32x4_2*)p;
-  const u32x4_2 v = ONCE ? __builtin_nontemporal_load(q) : *q;
-  return make_uint4(v.x, v.y, v.z, v.w);
+  return ONCE ? __builtin_nontemporal_load(q) : *q;
 }
 
 // Logits i .. i + kVec of a row, -inf at and behind `end`.
@@ -101,6 +101,55 @@ DEV void stores_done() {
   __syncthreads();
 }
 
+// ------------------------------------------------------------------ exchange between lanes
+// the value of lane l ^ J: moves inside rows of 16 lanes, swaps of rows and of halves
+template <int CTRL>
+DEV uint32_t dpp(uint32_t x) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xf, 0xf, true);
+}
+template <int J>
+DEV uint32_t lane_xor(uint32_t x) {
+  if constexpr (J == 1) return dpp<0xB1>(x);                 // quad [1,0,3,2]
+  else if constexpr (J == 2) return dpp<0x4E>(x);            // quad [2,3,0,1]
+  else if constexpr (J == 3) return dpp<0x1B>(x);            // quad [3,2,1,0]
+  else if constexpr (J == 4) return dpp<0x1B>(dpp<0x141>(x));  // 7 ^ 3
+  else if constexpr (J == 7) return dpp<0x141>(x);           // mirror of 8
+  else if constexpr (J == 8) return dpp<0x128>(x);           // rotation by 8 of 16
+  else if constexpr (J == 15) return dpp<0x140>(x);          // mirror of 16
+  else if constexpr (J == 16) {
+    const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    return threadIdx.x & 16 ? r[0] : r[1];
+  } else if constexpr (J == 31) return lane_xor<16>(lane_xor<15>(x));
+  else if constexpr (J == 32) {
+    const auto r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+    return threadIdx.x & 32 ? r[0] : r[1];
+  } else {
+    static_assert(J == 63, "lane_xor");
+    return lane_xor<32>(lane_xor<31>(x));
+  }
+}
+// sums and maxima over a wave, in every lane
+template <int J>
+DEV float lane_xor_f(float x) {
+  return __builtin_bit_cast(float, lane_xor<J>(__builtin_bit_cast(uint32_t, x)));
+}
+DEV float sum64(float v) {
+  v += lane_xor_f<1>(v);
+  v += lane_xor_f<2>(v);
+  v += lane_xor_f<7>(v);  // (quads are alike by now, and so on)
+  v += lane_xor_f<15>(v);
+  v += lane_xor_f<16>(v);
+  return v + lane_xor_f<32>(v);
+}
+DEV float max64(float v) {
+  v = fmaxf(v, lane_xor_f<1>(v));
+  v = fmaxf(v, lane_xor_f<2>(v));
+  v = fmaxf(v, lane_xor_f<7>(v));
+  v = fmaxf(v, lane_xor_f<15>(v));
+  v = fmaxf(v, lane_xor_f<16>(v));
+  return fmaxf(v, lane_xor_f<32>(v));
+}
+
 // ------------------------------------------------------------------ softmax statistics
 struct Acc {
   float m, s, w, s1;  // reference, sum at c, sum weighted by z - m, sum at c1
@@ -123,45 +172,57 @@ DEV void acc_move(Acc& a, float M, float c, float c1) {
 // lane at columns col + u * step ..
 template <int U, int N>
 struct Group {
-  float x[U][N], top;  // top: the largest of them (NaN left out)
+  float x[U][N];
   int n, col, step;
+
+  __device__ __forceinline__ float top() const {  // the largest of them (NaN left out)
+    float m = -INFINITY;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (u >= n) break;
+#pragma unroll
+      for (int j = 0; j < N; ++j) m = fmaxf(m, x[u][j]);
+    }
+    return m;
+  }
 };
 
-// Adds a group. The reference only follows where a logit lies more than `lift` above it, 2^6 times
-// its weight: fp32 holds the sums nearly as well with a stale one (the entropy's error grows with
-// the distance to the largest logit), and few groups move it. A vector is summed by itself first,
-// which leaves a lane an 8th (4th) of the additions in a row. NaN and +inf logits make s NaN:
-// exp(NaN), and exp(inf - inf).
+// Adds a group, one lane's reference following its own largest logit: it moves where a logit lies
+// above it by `lift`, 2^6 times its weight. fp32 holds the sums nearly as well with a stale one, and
+// few groups move it. NaN and +inf logits make s NaN: exp(NaN), and exp(inf - inf).
 template <bool ENT, bool TWO, int U, int N>
 DEV void acc_add(Acc& a, const Group<U, N>& g, float c, float c1, float lift) {
-  if (g.top > a.m + lift) acc_move<ENT, TWO>(a, g.top, c, c1);
+  const float top = g.top();
+  if (top > a.m + lift) acc_move<ENT, TWO>(a, top, c, c1);
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     if (u >= g.n) break;
-    float s = 0.f, w = 0.f, s1 = 0.f;
 #pragma unroll
     for (int j = 0; j < N; ++j) {
       const float d = g.x[u][j] - a.m;
       const float e = exp2_fast(d * c);
-      s = j ? s + e : e;
+      a.s += e;
       // (a logit of -inf has weight 0, and 0 times -inf is not)
-      const float dw = fmaxf(d, -1e30f);
-      if (ENT) w = j ? fmaf(e, dw, w) : e * dw;
-      const float e1 = TWO ? exp2_fast(d * c1) : 0.f;
-      s1 = j ? s1 + e1 : e1;
+      if (ENT) a.w = fmaf(e, fmaxf(d, -1e30f), a.w);
+      if (TWO) a.s1 += exp2_fast(d * c1);
     }
-    a.s += s;
-    if (ENT) a.w += w;
-    if (TWO) a.s1 += s1;
   }
+}
+
+template <int N>
+DEV float max_of(const float (&x)[N]) {
+  float m = x[0];
+#pragma unroll
+  for (int j = 1; j < N; ++j) m = fmaxf(m, x[j]);
+  return m;
 }
 
 template <bool ENT, bool TWO>
 DEV void acc_wave(Acc& a, float c, float c1) {
-  acc_move<ENT, TWO>(a, wave_max(a.m), c, c1);
-  a.s = wave_sum(a.s);
-  if (ENT) a.w = wave_sum(a.w);
-  if (TWO) a.s1 = wave_sum(a.s1);
+  acc_move<ENT, TWO>(a, max64(a.m), c, c1);
+  a.s = sum64(a.s);
+  if (ENT) a.w = sum64(a.w);
+  if (TWO) a.s1 = sum64(a.s1);
 }
 
 // joined over the workgroup, for every thread
@@ -171,19 +232,8 @@ DEV void acc_block(Acc& a, float c, float c1, Acc* lds) {
   acc_wave<ENT, TWO>(a, c, c1);
   if (lane_id() == 0) lds[threadIdx.x >> 6] = a;
   __syncthreads();
-  float M = kNone;
-#pragma unroll
-  for (int i = 0; i < NW; ++i) M = fmaxf(M, lds[i].m);
-  Acc t{M, 0.f, 0.f, 0.f};
-#pragma unroll
-  for (int i = 0; i < NW; ++i) {
-    Acc b = lds[i];
-    acc_move<ENT, TWO>(b, M, c, c1);
-    t.s += b.s;
-    t.w += b.w;
-    t.s1 += b.s1;
-  }
-  a = t;
+  a = lane_id() < NW ? lds[lane_id()] : acc_empty();
+  acc_wave<ENT, TWO>(a, c, c1);
 }
 
 // the statistics of a row's parts, for every lane of the wave
@@ -199,6 +249,98 @@ DEV Acc join_parts(const LogitSplit& sp, size_t row, float c, float c1) {
   return a;
 }
 
+// ------------------------------------------------------------------ sums at one reference
+// The sums of a whole workgroup at one reference m, the largest logit of its first group: a weight is
+// then exp2(z c + k) with k = -m c rounded, two instructions instead of three and no maximum to keep,
+// and lanes and waves join by addition. k's rounding r = m c + k scales all weights alike and is taken
+// out at the end. fp32's exponents leave room for logits far above m; where they do not (sums that are
+// not finite: also NaN and +inf logits), or m is nothing to go by (no logit above -inf in the first
+// group, or of the size of the type's lowest value), served() is false and the caller sums again with
+// acc_add, a reference for each lane.
+enum Softmaxes { ONE, TWO_EXP, TWO_SQUARE };  // at tau alone; also at 1; the same where tau is 2:
+                                              // exp(z) is then exp(z / 2)^2
+template <bool ENT, Softmaxes SM>
+struct Sums {
+  float m, c, k, k1;
+  float s, w, s1;
+
+  __device__ __forceinline__ void start(float ref, float scale) {
+    m = fabsf(ref) < 1e30f ? ref : 0.f;
+    c = scale;
+    k = -(m * c);
+    k1 = -(m * kLog2e);
+    s = fabsf(ref) < 1e30f ? 0.f : NAN;
+    w = s1 = 0.f;
+  }
+  template <int N>
+  __device__ __forceinline__ void add(const float (&x)[N]) {
+    // a vector by itself first, which leaves a lane an 8th (4th) of the additions in a row
+    float vs = 0.f, vw = 0.f, v1 = 0.f;
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      const float a = fmaf(x[j], c, k), e = exp2_fast(a);
+      vs = j ? vs + e : e;
+      // (a logit of -inf has weight 0, and 0 times -inf is not)
+      if (ENT) vw = j ? fmaf(e, fmaxf(a, -1e30f), vw) : e * fmaxf(a, -1e30f);
+      if (SM == TWO_SQUARE) v1 = j ? fmaf(e, e, v1) : e * e;
+      if (SM == TWO_EXP) {
+        const float e1 = exp2_fast(fmaf(x[j], kLog2e, k1));
+        v1 = j ? v1 + e1 : e1;
+      }
+    }
+    s += vs;
+    if (ENT) w += vw;
+    if (SM != ONE) s1 += v1;
+  }
+  template <int U, int N>
+  __device__ __forceinline__ void add(const Group<U, N>& g) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (u >= g.n) break;
+      add(g.x[u]);
+    }
+  }
+  // over the workgroup, for every thread
+  template <int NT>
+  __device__ __forceinline__ void join(Acc* lds) {
+    s = sum64(s);
+    if (ENT) w = sum64(w);
+    if (SM != ONE) s1 = sum64(s1);
+    if (lane_id() == 0) lds[threadIdx.x >> 6] = Acc{0.f, s, w, s1};
+    __syncthreads();
+    const Acc a = lane_id() < NT / 64 ? lds[lane_id()] : Acc{0.f, 0.f, 0.f, 0.f};
+    s = sum64(a.s);
+    if (ENT) w = sum64(a.w);
+    if (SM != ONE) s1 = sum64(a.s1);
+  }
+  __device__ __forceinline__ bool served() const {
+    const bool one = s > 0.f && s < 1e37f && (!ENT || fabsf(w) < 1e37f);
+    return one && (SM == ONE || (s1 > 0.f && s1 < 1e37f));
+  }
+  // exp(k's rounding) at tau and at 1
+  __device__ __forceinline__ float unround() const { return exp2_fast(-fmaf(m, c, k)); }
+  __device__ __forceinline__ float unround1() const {
+    return SM == TWO_SQUARE ? unround() * unround() : exp2_fast(-fmaf(m, kLog2e, k1));
+  }
+  __device__ __forceinline__ Acc acc() const {
+    const float u = unround();
+    Acc a{m, s * u, 0.f, SM == ONE ? 0.f : s1 * unround1()};
+    if (ENT) a.w = (w - fmaf(m, c, k) * s) * u / c;
+    return a;
+  }
+};
+
+// the largest logit of the workgroup's first group
+template <int NT>
+DEV float block_max(float v, Acc* lds) {
+  v = max64(v);
+  if (lane_id() == 0) lds[threadIdx.x >> 6].m = v;
+  __syncthreads();
+  v = max64(lane_id() < NT / 64 ? lds[lane_id()].m : -INFINITY);
+  __syncthreads();
+  return v;
+}
+
 // Hands columns v0 .. v1 of a row to add(group), -inf in the place of columns behind the end; columns
 // rise from vector to vector and from group to group. The loads of one group are in flight while
 // the one before it is worked on.
@@ -206,19 +348,10 @@ template <class T, int NT, int U, bool ONCE, class F>
 DEV void scan(const T* row, int v0, int v1, F&& add) {
   constexpr int N = kVec<T>, step = NT * N;
   int i = v0 + (int)threadIdx.x * N, b = v0;
-  uint4 next[U];
+  u32x4 next[U];
   Group<U, N> g;
   g.n = U;
   g.step = step;
-  auto top = [&](int n) {
-    g.top = -INFINITY;
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (u >= n) break;
-#pragma unroll
-      for (int j = 0; j < N; ++j) g.top = fmaxf(g.top, g.x[u][j]);
-    }
-  };
   if (b + U * step <= v1) {
 #pragma unroll
     for (int u = 0; u < U; ++u) next[u] = load16<ONCE>(row + i + u * step);
@@ -230,7 +363,6 @@ DEV void scan(const T* row, int v0, int v1, F&& add) {
         for (int u = 0; u < U; ++u) next[u] = load16<ONCE>(row + i + (U + u) * step);
       }
       g.col = i;
-      top(U);
       add(g);
     }
   }
@@ -249,7 +381,6 @@ DEV void scan(const T* row, int v0, int v1, F&& add) {
     else
       load_tail<T>(row, i + u * step, v1, g.x[u]);
   }
-  top(g.n);
   add(g);
 }
 
@@ -260,7 +391,7 @@ DEV void map_row(const T* z, G* dz, int v0, int v1, F&& f) {
   constexpr int N = kVec<T>, step = NT * N;
   int i = v0 + (int)threadIdx.x * N;
   for (; i + (U - 1) * step + N <= v1; i += U * step) {
-    uint4 v[U];
+    u32x4 v[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) v[u] = load16<ONCE>(z + i + u * step);
 #pragma unroll

@@ -415,7 +415,7 @@ struct ScoreGradArgs {
   const int32_t* targets;
   const float *lse, *entropy, *d_logp, *d_entropy;
   float inv_tau;
-  LogitSplit split;        // (n and cols alone)
+  LogitSplit split;        // n and cols, set by the launcher
 };
 hipError_t launch_scores_grad(ScoreGradArgs a, int dtype, int gtype, hipStream_t st);
 struct DistillArgs {
