@@ -7,15 +7,7 @@ namespace mebp {
 namespace {
 
 constexpr int NT = 256;
-#ifndef MEBP_T512
-#define MEBP_T512 (20*512*16)
-#endif
-#ifndef MEBP_T256
-#define MEBP_T256 (20*256*16)
-#endif
-#ifndef MEBP_R
-#define MEBP_R 20
-#endif
+
 
 // ------------------------------------------------------------------ distillation
 // With p = softmax(teacher / tau) over the K entries, q = softmax(z / tau) and q1 = softmax(z) over
@@ -261,9 +253,10 @@ DEV P* advance(P* p, int n) {
 }
 
 // Loss and gradient of a whole row by one workgroup, which holds up to R whole steps of it (16 bytes of
-// each lane) in registers from the statistics to the gradient: those logits are read once. What the row
-// has beyond them is read a second time.
-template <class T, class G, Softmaxes SM, int WG, int R>
+// each lane) in registers and L more in LDS from the statistics to the gradient: those logits are read
+// once. What the row has beyond them is read a second time, the last of it first: that is still in the
+// XCD's L2.
+template <class T, class G, Softmaxes SM, int WG, int R, int L>
 __global__ __launch_bounds__(WG, 4) void k_distill_row(DistillArgs p) {
   constexpr int N = kVec<T>, step = WG * N;
   constexpr bool TWO = SM != ONE;
@@ -272,7 +265,9 @@ __global__ __launch_bounds__(WG, 4) void k_distill_row(DistillArgs p) {
   const size_t row = blockIdx.x;
   const T* z = (const T*)p.z + row * p.ld;
   G* dz = (G*)p.dz + row * p.ldd;
-  const int V = p.vocab, steps = min(R, V / step), held = steps * step;
+  __shared__ u32x4 more[L ? L : 1][WG];
+  const int V = p.vocab, steps = min(R, V / step), steps2 = L ? min(L, V / step - steps) : 0;
+  const int held1 = steps * step, held = held1 + steps2 * step;
   const uint32_t lane = threadIdx.x * N;
   const float w = row_weight(p, row);
   if (w == 0.f) {
@@ -316,6 +311,22 @@ __global__ __launch_bounds__(WG, 4) void k_distill_row(DistillArgs p) {
     unpack<T>(raw[r], x);
     sums.add(x);
   });
+  if constexpr (L > 0) {
+    const T* at = z + held1;
+    for (int r = 0; r < steps2; r += 2, at += 2 * step) {
+      u32x4 v[2];
+      float x[N];
+      v[0] = load16<true>(at + lane);
+      if (r + 1 < steps2) v[1] = load16<true>(at + step + lane);
+      more[r][threadIdx.x] = v[0];
+      unpack<T>(v[0], x);
+      sums.add(x);
+      if (r + 1 == steps2) break;
+      more[r + 1][threadIdx.x] = v[1];
+      unpack<T>(v[1], x);
+      sums.add(x);
+    }
+  }
   bool begun = steps > 0;
   if (held < V)
     scan<T, WG, 2, false>(z, held, V, [&](const auto& h) {
@@ -353,7 +364,17 @@ __global__ __launch_bounds__(WG, 4) void k_distill_row(DistillArgs p) {
       if (SM == TWO_SQUARE) return e * fmaf(b1, e, b0);
       return fmaf(b1, exp2_fast(fmaf(x, kLog2e, sums.k1)), b0 * e);
     };
-    if (held < V) map_row<T, G, WG, 2, true>(z, dz, held, V, f);
+    if (held < V) map_row<T, G, WG, 2, true, true>(z, dz, held, V, f);
+    if constexpr (L > 0) {
+      G* at = dz + held1;
+      for (int r = 0; r < steps2; ++r, at += step) {
+        float x[N];
+        unpack<T>(more[r][threadIdx.x], x);
+#pragma unroll
+        for (int j = 0; j < N; ++j) x[j] = f(x[j]);
+        store_vec<G, N>(at + lane, x);
+      }
+    }
     G* to = dz;
     each<R>([&](auto i) {
       constexpr int r = decltype(i)::value;
@@ -409,17 +430,21 @@ hipError_t launch_distill(DistillArgs a, int dtype, int gtype, hipStream_t st) {
     }
     const char* name = inplace ? "distill_row_inplace" : "distill_row";
     const size_t row = (size_t)a.vocab * sizeof(T);
-    auto run = [&](auto wg) {
+    // as much of a row in registers as leaves none to spill: two exponentials' sums take more of them
+    constexpr int R = SM == TWO_EXP ? 16 : 18;
+    auto run = [&](auto wg, auto lds) {
       constexpr int WG = decltype(wg)::value;
       MEBP_TIMED(st, name, 0.0, both,
-                 hipLaunchKernelGGL((k_distill_row<T, G, SM, WG, MEBP_R>), dim3(a.rows), dim3(WG), 0, st, a));
+                 hipLaunchKernelGGL((k_distill_row<T, G, SM, WG, R, decltype(lds)::value>), dim3(a.rows), dim3(WG), 0, st, a));
     };
-    if (row <= MEBP_T256)
-      run(IC<256>());
-    else if (row <= MEBP_T512)
-      run(IC<512>());
+    // the smallest workgroup whose registers hold the row, so that several share a compute unit; a row
+    // beyond 144 KB has one to itself, and its LDS
+    if (row <= R * 256 * 16)
+      run(IC<256>(), IC<0>());
+    else if (row <= R * 512 * 16)
+      run(IC<512>(), IC<0>());
     else
-      run(IC<1024>());
+      run(IC<1024>(), IC<9>());
     return hipGetLastError();
   };
   auto by_softmaxes = [&](auto&& f) {

@@ -384,13 +384,27 @@ DEV void scan(const T* row, int v0, int v1, F&& add) {
   add(g);
 }
 
-// Writes f(z) over columns v0 .. v1 of a row. Every element is read before it is written, by the
-// thread that writes it: the output may be the input.
-template <class T, class G, int NT, int U, bool ONCE, class F>
+// Writes f(z) over columns v0 .. v1 of a row, BACK: the last ones first. Every element is read before
+// it is written, by the thread that writes it: the output may be the input.
+template <class T, class G, int NT, int U, bool ONCE, bool BACK = false, class F>
 DEV void map_row(const T* z, G* dz, int v0, int v1, F&& f) {
   constexpr int N = kVec<T>, step = NT * N;
-  int i = v0 + (int)threadIdx.x * N;
-  for (; i + (U - 1) * step + N <= v1; i += U * step) {
+  const int i0 = v0 + (int)threadIdx.x * N, groups = (v1 - v0) / (U * step);
+  auto rest = [&] {  // fewer than U steps
+    int i = i0 + groups * U * step;
+    for (; i + N <= v1; i += step) {
+      float x[N];
+      unpack<T>(load16<ONCE>(z + i), x);
+#pragma unroll
+      for (int j = 0; j < N; ++j) x[j] = f(x[j]);
+      store_vec<G, N>(dz + i, x);
+    }
+    for (int j = 0; j < N; ++j)
+      if (i + j < v1) dz[i + j] = to_out<G>(f(cvt(z[i + j])));
+  };
+  if (BACK) rest();
+  for (int n = 0; n < groups; ++n) {
+    const int i = i0 + (BACK ? groups - 1 - n : n) * U * step;
     u32x4 v[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) v[u] = load16<ONCE>(z + i + u * step);
@@ -403,15 +417,7 @@ DEV void map_row(const T* z, G* dz, int v0, int v1, F&& f) {
       store_vec<G, N>(dz + i + u * step, x);
     }
   }
-  for (; i + N <= v1; i += step) {
-    float x[N];
-    unpack<T>(load16<ONCE>(z + i), x);
-#pragma unroll
-    for (int j = 0; j < N; ++j) x[j] = f(x[j]);
-    store_vec<G, N>(dz + i, x);
-  }
-  for (int j = 0; j < N; ++j)
-    if (i + j < v1) dz[i + j] = to_out<G>(f(cvt(z[i + j])));
+  if (!BACK) rest();
 }
 
 // zeros over columns v0 .. v1 of a row
