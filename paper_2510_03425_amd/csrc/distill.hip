@@ -8,7 +8,6 @@ namespace {
 
 constexpr int NT = 256;
 
-
 // ------------------------------------------------------------------ distillation
 // With p = softmax(teacher / tau) over the K entries, q = softmax(z / tau) and q1 = softmax(z) over
 // the vocabulary, a row's loss is w (alpha tau^2 KL(p, q) + (1 - alpha) CE(z, target)) and its
@@ -422,16 +421,18 @@ hipError_t launch_distill(DistillArgs a, int dtype, int gtype, hipStream_t st) {
     using T = std::remove_pointer_t<decltype(tp)>;
     using G = std::remove_pointer_t<decltype(gp)>;
     constexpr Softmaxes SM = (Softmaxes)decltype(sm)::value;
-    if (a.split.n > 1) {
+    const size_t row = (size_t)a.vocab * sizeof(T);
+    // as much of a row in registers as leaves none to spill: two exponentials' sums take more of them
+    constexpr int R = SM == TWO_EXP ? 16 : 18;
+    // few long rows go by parts, in two launches; from 96 of 151936 fp32 logits on a workgroup for each
+    // row is faster (64 rows 25 us by rows and 21 by parts, 96: 27 and 28, 192: 33 and 51)
+    if (a.split.n > 1 && a.rows < 96 && row > R * 512 * 16) {
       stats(tp, sm, std::false_type(), IC<NT>());
       MEBP_TIMED(st, inplace ? "distill_grad_inplace" : "distill_grad", 0.0, both,
                  hipLaunchKernelGGL((k_distill_grad<T, G, SM != ONE>), dim3(grid), dim3(NT), 0, st, a));
       return hipGetLastError();
     }
     const char* name = inplace ? "distill_row_inplace" : "distill_row";
-    const size_t row = (size_t)a.vocab * sizeof(T);
-    // as much of a row in registers as leaves none to spill: two exponentials' sums take more of them
-    constexpr int R = SM == TWO_EXP ? 16 : 18;
     auto run = [&](auto wg, auto lds) {
       constexpr int WG = decltype(wg)::value;
       MEBP_TIMED(st, name, 0.0, both,

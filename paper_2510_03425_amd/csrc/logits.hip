@@ -10,7 +10,7 @@ namespace {
 // above the complement of its column, so that equal logits rank by the lower column and no two
 // keys are alike. 0 is below every logit's key. Each wave keeps its 64 largest keys sorted, one
 // per lane, and appends the logits above a threshold to a buffer, which is sorted and merged in
-// batches of 64.
+// batches of up to 64 (16 lanes do for 16 alternatives).
 DEV uint32_t order_bits(float x) {
   const uint32_t b = __builtin_bit_cast(uint32_t, x + 0.0f);  // -0 ranks as +0
   return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
@@ -37,24 +37,43 @@ DEV u64 halve(u64 key) {
   if constexpr (J > 1) key = halve<J / 2>(key);
   return key;
 }
-DEV u64 sort64(u64 key) {
+DEV u64 sort16(u64 key) {
   key = exchange<1, 1>(key);
   key = halve<1>(exchange<3, 2>(key));
   key = halve<2>(exchange<7, 4>(key));
-  key = halve<4>(exchange<15, 8>(key));
+  return halve<4>(exchange<15, 8>(key));
+}
+// n keys in the first lanes, 0 in the others
+DEV u64 sort_keys(u64 key, int n) {
+  key = sort16(key);
+  if (n <= 16) return key;
   key = halve<8>(exchange<31, 16>(key));
   return halve<16>(exchange<63, 32>(key));
 }
-// the 64 largest of two sorted lists, sorted
-DEV u64 merge64(u64 a, u64 b) {
+// the largest of two sorted lists, sorted: as many as k of them
+DEV u64 merge_keys(u64 a, u64 b, int k) {
+  if (k <= 16) {
+    const u64 r = lane_xor64<15>(b);
+    return halve<8>(a > r ? a : r);
+  }
   const u64 r = lane_xor64<63>(b);
   return halve<32>(a > r ? a : r);
+}
+
+// the largest value, to 2^-7 of it, that at least n lanes' order bits reach
+DEV uint32_t lanes_reach(uint32_t o, int n) {
+  uint32_t t = 0;
+  for (int bit = 31; bit >= 16; --bit) {
+    const uint32_t up = t | 1u << bit;
+    if (__popcll(__ballot(o >= up)) >= n) t = up;
+  }
+  return t;
 }
 
 constexpr int top_buffer(int n) { return 64 + 64 * n; }  // keys of a wave's buffer, vectors of n logits
 
 // The threshold that a logit has to be above to be buffered comes from the lanes' largest logits so
-// far: of each wave the ceil(k / waves)-th largest of its lanes' (to 2^-16 of it, by bisection), and
+// far: of each wave the ceil(k / waves)-th largest of its lanes' (to 2^-7 of it, by bisection), and
 // of the waves the least. k lanes of the row at least have reached it, so it bounds the row's k-th
 // logit from below; it is not far below, as the top logits are mostly in different lanes. `share`
 // holds each wave's bound, which only rises: an older one is valid too. Taken anew whenever the
@@ -98,16 +117,19 @@ struct Top {
     cnt -= n;
     const u64 key = l < n ? buf[cnt + l] : 0ull;
     fence();
-    list = merge64(list, sort64(key));
+    list = merge_keys(list, sort_keys(key, n), k);
+  }
+  // appends the keys of the lanes with `in`; whether there is one
+  __device__ __forceinline__ bool push(u64 key, bool in) {
+    const u64 mask = __ballot(in);
+    if (!mask) return false;
+    if (in)
+      buf[cnt + (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0))] = key;
+    cnt += __popcll(mask);
+    return true;
   }
   __device__ __forceinline__ void publish() {
-    const int part = (k + NW - 1) / NW;
-    const uint32_t o = order_bits(most);
-    uint32_t t = 0;
-    for (int bit = 31; bit >= 8; --bit) {
-      const uint32_t up = t | 1u << bit;
-      if (__popcll(__ballot(o >= up)) >= part) t = up;
-    }
+    const uint32_t t = lanes_reach(order_bits(most), (k + NW - 1) / NW);
     if (lane_id() == 0) __hip_atomic_store(share + (threadIdx.x >> 6), t, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
   }
   __device__ __forceinline__ void shared_threshold() {
@@ -124,8 +146,23 @@ struct Top {
     most = top;
     publish();
   }
-  template <int U, int N>
-  __device__ __forceinline__ void add(const Group<U, N>& g, float top) {
+  template <int N>
+  __device__ __forceinline__ void push(const float (&x)[N], int col) {
+#pragma unroll
+    for (int j = 0; j < N; ++j) push(order_key(x[j], col + j), x[j] > thr);
+  }
+  __device__ __forceinline__ void drain() {
+    if (cnt < 64) return;
+    do flush(64);
+    while (cnt >= 64);
+    const uint32_t kth = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(list >> 32), k - 1);
+    if (kth) thr = fmaxf(thr, order_value(kth));
+  }
+  // A group of the row's columns before `end`. Where the buffer might not take another vector the rest
+  // of the group is read once more, vector by vector (rising logits; a loop of its own keeps one copy
+  // of the sort here instead of U).
+  template <class T, int U, int N>
+  __device__ __forceinline__ void add(const Group<U, N>& g, float top, const T* row, int end) {
     most = fmaxf(most, top);
     const int seen = ++groups;
     if (seen > 1 && (seen & (seen - 1)) == 0) publish();
@@ -135,22 +172,8 @@ struct Top {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       if (u >= g.n) break;
-#pragma unroll
-      for (int j = 0; j < N; ++j) {
-        const float x = g.x[u][j];
-        const bool p = x > thr;
-        const u64 mask = __ballot(p);
-        if (!mask) continue;
-        if (p)
-          buf[cnt + (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0))] =
-              order_key(x, g.col + u * g.step + j);
-        cnt += __popcll(mask);
-      }
-      if (cnt < 64) continue;
-      do flush(64);
-      while (cnt >= 64);
-      const uint32_t kth = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(list >> 32), k - 1);
-      if (kth) thr = fmaxf(thr, order_value(kth));
+      push(g.x[u], g.col + u * g.step);
+      drain();
     }
   }
 
@@ -163,7 +186,7 @@ struct Top {
     for (int half = NW / 2; half > 0; half /= 2) {
       if (wave >= half && wave < 2 * half) lists[(wave - half) * 64 + l] = list;
       __syncthreads();
-      if (wave < half) list = merge64(list, lists[wave * 64 + l]);
+      if (wave < half) list = merge_keys(list, lists[wave * 64 + l], k);
       __syncthreads();
     }
   }
@@ -215,7 +238,7 @@ __global__ __launch_bounds__(NT) void k_scores(ScoreArgs p) {
   t.start(p.top_k, buf + (threadIdx.x >> 6) * B, share);
   Sums<true, ONE> sums;
   bool begun = false;
-  scan<T, NT, 4, true>(z, v0, v1, [&](const auto& g) {
+  scan<T, NT, TOP ? 2 : 4, true>(z, v0, v1, [&](const auto& g) {
     float top = 0.f;
     if (TOP || !begun) top = g.top();
     if (!begun) {  // (of every thread: each has a first group)
@@ -224,7 +247,7 @@ __global__ __launch_bounds__(NT) void k_scores(ScoreArgs p) {
       begun = true;
     }
     sums.add(g);
-    if constexpr (TOP) t.add(g, top);
+    if constexpr (TOP) t.add(g, top, z, v1);
   });
   sums.template join<NT>(red);
   Acc a = sums.acc();
@@ -244,22 +267,32 @@ __global__ __launch_bounds__(NT) void k_scores(ScoreArgs p) {
   }
 }
 
-// one workgroup per row: its waves merge every fourth part's list, then theirs
+// One workgroup per row. The parts' largest logits (the heads of their lists) bound the row's k-th from
+// below where there are at least k parts; each list gives the keys of its beginning that reach it, one
+// of each list at a time, to one wave's buffer.
 template <class T>
 __global__ __launch_bounds__(256) void k_scores_join(ScoreArgs p) {
-  __shared__ u64 lists[2 * 64];
+  __shared__ u64 keys[kLogitParts * 64], buf[128];
   const size_t row = blockIdx.x;
-  const int l = lane_id(), wave = threadIdx.x >> 6;
-  Top<4> t;
-  t.start(p.top_k, nullptr, nullptr);
-  if (p.top_k) {
-    for (int i = wave; i < p.split.n; i += 4)
-      t.list = merge64(t.list, l < p.top_k ? p.split.keys[(row * p.split.n + i) * p.top_k + l] : 0ull);
-    t.join(lists);
-  }
-  if (wave) return;
+  const int l = lane_id(), n = p.split.n, k = p.top_k;
+  for (int i = threadIdx.x; i < n * k; i += 256) keys[i] = p.split.keys[row * n * k + i];
+  if (k) __syncthreads();
+  if (threadIdx.x >= 64) return;
+  const float zt = target_logit<T>(p, (const T*)p.z + row * p.ld, row);
   const Acc a = join_parts<true, false>(p.split, row, p.c, 0.f);
-  write_scores(p, row, a, target_logit<T>(p, (const T*)p.z + row * p.ld, row), t.list);
+  Top<1> t;
+  t.start(k, buf, nullptr);
+  if (k) {
+    const uint32_t head = l < n ? (uint32_t)(keys[l * k] >> 32) : 0u;
+    const uint32_t bound = n >= k ? lanes_reach(head, k) : 0u;
+    for (int j = 0; j < k; ++j) {
+      const u64 key = l < n ? keys[l * k + j] : 0ull;
+      if (!t.push(key, key && (uint32_t)(key >> 32) >= bound)) break;
+      if (t.cnt >= 64) t.flush(64);
+    }
+    t.flush(t.cnt);
+  }
+  write_scores(p, row, a, zt, t.list);
 }
 
 // ------------------------------------------------------------------ gradient
@@ -332,11 +365,13 @@ hipError_t launch_scores(ScoreArgs a, int dtype, hipStream_t st) {
   });
 }
 
-// The gradient goes by parts of 8192 columns whatever the rows: 4 loads of each lane of 256 in flight
-// in 16 bits, and many small workgroups leave no part of the chip waiting (1024 x 151936 bf16 110 us,
-// 5.6 TB/s; a workgroup per row 125 .. 130 us).
+// The gradient goes by parts of 8192 columns: 4 loads of each lane of 256 in flight in 16 bits, and
+// many small workgroups leave no part of the chip waiting (1024 x 151936 bf16 110 us, 5.6 TB/s; a
+// workgroup per row 125 .. 130 us); by smaller ones where that makes fewer than four workgroups for
+// each compute unit.
 hipError_t launch_scores_grad(ScoreGradArgs a, int dtype, int gtype, hipStream_t st) {
   a.split.cols = 8192;
+  while (a.split.cols > 2048 && (size_t)a.rows * ((a.vocab + a.split.cols - 1) / a.split.cols) < 1024) a.split.cols /= 2;
   a.split.n = (a.vocab + a.split.cols - 1) / a.split.cols;
   const unsigned grid = (unsigned)((size_t)a.rows * a.split.n);
   const double bytes = (double)a.rows * a.vocab * (type_bytes(dtype) + type_bytes(gtype));

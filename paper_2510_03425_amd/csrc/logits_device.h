@@ -349,30 +349,31 @@ DEV void scan(const T* row, int v0, int v1, F&& add) {
   constexpr int N = kVec<T>, step = NT * N;
   int i = v0 + (int)threadIdx.x * N, b = v0;
   u32x4 next[U];
-  Group<U, N> g;
-  g.n = U;
-  g.step = step;
-  if (b + U * step <= v1) {
+  // (of the last group a lane loads the vectors that are whole)
+  auto load = [&](int from, int at) {
+    if (from + U * step <= v1) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) next[u] = load16<ONCE>(row + i + u * step);
-    for (; b + U * step <= v1; b += U * step, i += U * step) {
+      for (int u = 0; u < U; ++u) next[u] = load16<ONCE>(row + at + u * step);
+    } else {
 #pragma unroll
-      for (int u = 0; u < U; ++u) unpack<T>(next[u], g.x[u]);
-      if (b + 2 * U * step <= v1) {
-#pragma unroll
-        for (int u = 0; u < U; ++u) next[u] = load16<ONCE>(row + i + (U + u) * step);
-      }
-      g.col = i;
-      add(g);
+      for (int u = 0; u < U; ++u)
+        if (at + u * step + N <= v1) next[u] = load16<ONCE>(row + at + u * step);
     }
+  };
+  Group<U, N> g;
+  g.step = step;
+  load(b, i);
+  for (; b + U * step <= v1; b += U * step, i += U * step) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) unpack<T>(next[u], g.x[u]);
+    if (b + U * step < v1) load(b + U * step, i + U * step);
+    g.n = U;
+    g.col = i;
+    add(g);
   }
   if (b >= v1) return;
-  // fewer than U vectors of each lane are left
   g.n = (v1 - b + step - 1) / step;
   g.col = i;
-#pragma unroll
-  for (int u = 0; u < U; ++u)
-    if (i + u * step + N <= v1) next[u] = load16<ONCE>(row + i + u * step);
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     if (u >= g.n) break;

@@ -31,7 +31,9 @@ def make_config(cfg: Config) -> L.MebpConfig:
 
 
 def stream_handle() -> int:
-    return torch.cuda.current_stream().cuda_stream
+    """torch's current stream on the current device (its handle alone: a torch.cuda.Stream of it
+    takes 2.6 us to make)."""
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
 def _dev(a: np.ndarray, device) -> torch.Tensor:
@@ -54,29 +56,33 @@ def _on_device(f):
     current stream of that device."""
     @functools.wraps(f)
     def g(z, *a, **kw):
-        if z.device.type != "cuda":
+        if not z.is_cuda:
             raise ValueError("logits must be on the GPU")
-        if z.device.index == torch.cuda.current_device():
+        if z.get_device() == torch.cuda.current_device():
             return f(z, *a, **kw)
         with torch.cuda.device(z.device):
             return f(z, *a, **kw)
     return g
 
 
-def logits_struct(z: torch.Tensor) -> L.MebpLogits:
-    """[rows][vocab] logits (or their gradient) whose columns follow one another."""
-    if z.dim() != 2 or z.dtype not in LOGIT_TYPE or (z.stride(1) != 1 and z.shape[1] > 1):
+def logits_struct(z: torch.Tensor, like: Optional[torch.Tensor] = None) -> L.MebpLogits:
+    """[rows][vocab] logits (or their gradient, on the device of ``like``) whose columns follow
+    one another."""
+    dtype = LOGIT_TYPE.get(z.dtype)
+    if dtype is None or z.dim() != 2 or (z.stride(1) != 1 and z.shape[1] > 1):
         raise ValueError("logits must be a fp32, fp16 or bf16 matrix with contiguous rows")
+    if like is not None and z.get_device() != like.get_device():
+        raise ValueError(f"dz must be on {like.device}")
     rows, vocab = z.shape
-    return L.MebpLogits(z.data_ptr(), z.stride(0) if rows > 1 else vocab, rows, vocab, LOGIT_TYPE[z.dtype])
+    return L.MebpLogits(z.data_ptr(), z.stride(0) if rows > 1 else vocab, rows, vocab, dtype)
 
 
 def _operand(t: Optional[torch.Tensor], dtype, shape, like: torch.Tensor, what: str) -> int:
     """Address of an operand, None as NULL."""
     if t is None:
         return 0
-    if t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous() or t.device != like.device:
-        raise ValueError(f"{what} must be contiguous {dtype} {shape} on {like.device}")
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous() or t.get_device() != like.get_device():
+        raise ValueError(f"{what} must be contiguous {dtype} {tuple(shape)} on {like.device}")
     return t.data_ptr()
 
 
@@ -85,9 +91,9 @@ def _logits_ws(ws: Optional[torch.Tensor], z: torch.Tensor, top_k: int):
     if ws is None:
         n = L.mebp_logits_workspace_bytes(z.shape[0], z.shape[1], top_k)
         ws = torch.empty(max(n, 256), dtype=torch.uint8, device=z.device)
-    elif ws.device != z.device or not ws.is_contiguous():
+    elif ws.get_device() != z.get_device() or not ws.is_contiguous():
         raise ValueError(f"workspace must be contiguous on {z.device}")
-    return ws, ws.numel() * ws.element_size()
+    return ws, ws.nbytes
 
 
 @_on_device
@@ -103,13 +109,14 @@ def token_logprobs(z: torch.Tensor, targets: Optional[torch.Tensor] = None, top_
         if top_k > 0:
             out["top_ids"] = torch.empty((n, top_k), dtype=torch.int32, device=z.device)
             out["top_logp"] = torch.empty((n, top_k), dtype=torch.float32, device=z.device)
-    s = L.MebpTokenScores()
-    for k, t in out.items():
-        top = k.startswith("top_")
-        setattr(s, k, _operand(t, torch.int32 if k == "top_ids" else torch.float32, (n, top_k) if top else (n,), z, k))
+    f32, one, get = torch.float32, (n,), out.get
+    s = L.MebpTokenScores(
+        _operand(get("logp"), f32, one, z, "logp"), _operand(get("lse"), f32, one, z, "lse"),
+        _operand(get("entropy"), f32, one, z, "entropy"), _operand(get("top_ids"), torch.int32, (n, top_k), z, "top_ids"),
+        _operand(get("top_logp"), f32, (n, top_k), z, "top_logp"))
     zs = logits_struct(z)
     ws, nb = _logits_ws(ws, z, top_k)
-    L.mebp_token_logprobs(zs, _operand(targets, torch.int32, (n,), z, "targets"), temperature, top_k, s, ws.data_ptr(),
+    L.mebp_token_logprobs(zs, _operand(targets, torch.int32, one, z, "targets"), temperature, top_k, s, ws.data_ptr(),
                           nb, stream_handle())
     return out
 
@@ -125,12 +132,10 @@ def token_logprobs_backward(z: torch.Tensor, targets: Optional[torch.Tensor], ls
     if dz is None:
         dz = torch.empty(z.shape, dtype=z.dtype, device=z.device)
     f32 = torch.float32
-    if dz.device != z.device:
-        raise ValueError(f"dz must be on {z.device}")
     L.mebp_token_logprobs_backward(logits_struct(z), _operand(targets, torch.int32, n, z, "targets"), temperature,
                                    _operand(lse, f32, n, z, "lse"), _operand(entropy, f32, n, z, "entropy"),
                                    _operand(d_logp, f32, n, z, "d_logp"), _operand(d_entropy, f32, n, z, "d_entropy"),
-                                   logits_struct(dz), stream_handle())
+                                   logits_struct(dz, z), stream_handle())
     return dz
 
 
@@ -144,15 +149,13 @@ def distill_topk(z: torch.Tensor, ids: torch.Tensor, logits: torch.Tensor, row_l
     n, k = z.shape[0], ids.shape[-1]
     if row_loss is None:
         row_loss = torch.empty(n, dtype=torch.float32, device=z.device)
-    if dz is not None and dz.device != z.device:
-        raise ValueError(f"dz must be on {z.device}")
     d = L.MebpDistill(_operand(ids, torch.int32, (n, k), z, "ids"), _operand(logits, torch.float32, (n, k), z, "logits"),
                       _operand(targets, torch.int32, (n,), z, "targets"),
                       _operand(row_weight, torch.float32, (n,), z, "row_weight"), k, temperature, alpha)
     zs = logits_struct(z)
     ws, nb = _logits_ws(ws, z, 0)
     L.mebp_distill_topk(zs, d, _operand(row_loss, torch.float32, (n,), z, "row_loss"),
-                        None if dz is None else logits_struct(dz), ws.data_ptr(), nb, stream_handle())
+                        None if dz is None else logits_struct(dz, z), ws.data_ptr(), nb, stream_handle())
     return row_loss
 
 
