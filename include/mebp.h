@@ -334,6 +334,52 @@ typedef struct {
 int mebp_distill_topk(const mebp_logits* z, const mebp_distill* d, float* row_loss, const mebp_logits* dz, void* ws,
                       size_t ws_bytes, mebp_stream_t stream);
 
+/* ---------------- the LM head's logits ------------------------------------------------
+ * z = rmsnorm(x) E^T of the final norm and the tied int4 embedding for `rows` hidden states
+ * x [rows][d] fp32 (what the last layer's checkpoint holds, or any of its rows), and the
+ * operators above on them. Operands and products as in mebp_lm_head_ce_backward: fp16 forward,
+ * bf16 backward, fp32 sums. Rows go in blocks, so that the logits and the gradient of a block (fp32
+ * and bf16) take at most MEBP_LM_CHUNK_MB (environment, default 512) MiB, or those of 64 rows.
+ * x, dx, norm_final 16-byte aligned; dx must not be x. rows = 0 enqueues nothing.          */
+
+/* Bytes of workspace for the four calls below (top_k: that of mebp_lm_head_logprobs, else 0).
+ * Pure host computation; 0 for an invalid config or shape.                               */
+size_t mebp_head_workspace_bytes(const mebp_config* cfg, int32_t rows, int32_t top_k);
+
+/* The logits themselves: z of `rows` rows and cfg->vocab columns, MEBP_F32 or MEBP_F16 (rounded to
+ * it), ld a multiple of 8 below 2^20, data 16-byte aligned (written).                     */
+int mebp_lm_head_logits(const mebp_config* cfg, const mebp_q4* emb, const float* norm_final, const float* x,
+                        int32_t rows, const mebp_logits* z, void* ws, size_t ws_bytes, mebp_stream_t stream);
+
+/* Their gradient back to the hidden states: dx [rows][d] fp32 from dz MEBP_BF16 of the same
+ * shape rules.                                                                           */
+int mebp_lm_head_logits_backward(const mebp_config* cfg, const mebp_q4* emb, const float* norm_final, const float* x,
+                                 int32_t rows, const mebp_logits* dz, float* dx, void* ws, size_t ws_bytes,
+                                 mebp_stream_t stream);
+
+/* mebp_token_logprobs of the head's logits: scores a text, or records a teacher's alternatives. */
+int mebp_lm_head_logprobs(const mebp_config* cfg, const mebp_q4* emb, const float* norm_final, const float* x,
+                          int32_t rows, const int32_t* targets, float temperature, int32_t top_k,
+                          const mebp_token_scores* out, void* ws, size_t ws_bytes, mebp_stream_t stream);
+
+/* mebp_distill_topk of the head's logits: the sum of the rows' losses and its gradient w.r.t. x.
+ *   loss  one fp32 on the device (written);  row_loss [rows] fp32 (written), or NULL
+ *   dx    [rows][d] fp32 (written)                                                        */
+int mebp_lm_head_distill_backward(const mebp_config* cfg, const mebp_q4* emb, const float* norm_final, const float* x,
+                                  int32_t rows, const mebp_distill* d, float* loss, float* row_loss, float* dx,
+                                  void* ws, size_t ws_bytes, mebp_stream_t stream);
+
+/* mebp_train_step with mebp_lm_head_distill_backward as its final block: row n = b*T + t of `d` is
+ * position t of sequence b (its entries and its target are of the token that follows there, and its
+ * weight makes the sum a mean); T may be 1. Other arguments as in mebp_train_step; the workspace is
+ * the larger one of mebp_distill_step_workspace_bytes.                                    */
+size_t mebp_distill_step_workspace_bytes(const mebp_config* cfg, int32_t B, int32_t T);
+int mebp_train_step_distill(const mebp_config* cfg, const mebp_q4* emb, const mebp_layer_base* layers,
+                            const float* norm_final, const mebp_layer_lora* lora, const int32_t* ids, int32_t B,
+                            int32_t T, const mebp_distill* d, float* ckpt, float* loss, float* row_loss,
+                            const mebp_layer_lora_grad* grads, float* dx0, void* ws, size_t ws_bytes,
+                            mebp_stream_t stream);
+
 /* Message for the last non-zero status returned on the calling thread ("" if none). */
 const char* mebp_last_error(void);
 

@@ -25,7 +25,9 @@ EXPORTED = (
     "mebp_kernel_timing_report", "mebp_kernel_repeat", "mebp_lora_grad_accumulate", "mebp_lora_adamw_step",
     "mebp_train_step_offload", "mebp_test_gemm", "mebp_layer_recompute_backward_static",
     "mebp_set_workspace_guards", "mebp_workspace_guard_check", "mebp_logits_workspace_bytes",
-    "mebp_token_logprobs", "mebp_token_logprobs_backward", "mebp_distill_topk",
+    "mebp_token_logprobs", "mebp_token_logprobs_backward", "mebp_distill_topk", "mebp_head_workspace_bytes",
+    "mebp_lm_head_logits", "mebp_lm_head_logits_backward", "mebp_lm_head_logprobs", "mebp_lm_head_distill_backward",
+    "mebp_distill_step_workspace_bytes", "mebp_train_step_distill",
 )
 
 MEBP_F32, MEBP_F16, MEBP_BF16 = 0, 1, 2  # element types of a matrix of logits
@@ -143,6 +145,18 @@ def lib() -> C.CDLL:
                                                        C.POINTER(MebpLogits), P]),
             "mebp_distill_topk": (C.c_int, [C.POINTER(MebpLogits), C.POINTER(MebpDistill), P, C.POINTER(MebpLogits), P,
                                             SZ, P]),
+            "mebp_head_workspace_bytes": (SZ, [cfgp, I32, I32]),
+            "mebp_lm_head_logits": (C.c_int, [cfgp, C.POINTER(MebpQ4), P, P, I32, C.POINTER(MebpLogits), P, SZ, P]),
+            "mebp_lm_head_logits_backward": (C.c_int, [cfgp, C.POINTER(MebpQ4), P, P, I32, C.POINTER(MebpLogits), P, P,
+                                                       SZ, P]),
+            "mebp_lm_head_logprobs": (C.c_int, [cfgp, C.POINTER(MebpQ4), P, P, I32, P, C.c_float, I32,
+                                                C.POINTER(MebpTokenScores), P, SZ, P]),
+            "mebp_lm_head_distill_backward": (C.c_int, [cfgp, C.POINTER(MebpQ4), P, P, I32, C.POINTER(MebpDistill), P, P,
+                                                        P, P, SZ, P]),
+            "mebp_distill_step_workspace_bytes": (SZ, [cfgp, I32, I32]),
+            "mebp_train_step_distill": (C.c_int, [cfgp, C.POINTER(MebpQ4), C.POINTER(MebpLayerBase), P,
+                                                  C.POINTER(MebpLayerLora), P, I32, I32, C.POINTER(MebpDistill), P, P, P,
+                                                  C.POINTER(MebpLayerLoraGrad), P, P, SZ, P]),
             "mebp_kernel_timing": (C.c_int, [I32, I32]),
             "mebp_kernel_timing_report": (C.c_int, [C.c_char_p, SZ]),
             "mebp_kernel_repeat": (C.c_int, [C.c_char_p, I32]),
@@ -282,6 +296,46 @@ def mebp_token_logprobs_backward(z, targets, temperature, lse, entropy, d_logp, 
 
 def mebp_distill_topk(z, distill, row_loss, dz, ws, ws_bytes, stream=0, check=True):
     r = lib().mebp_distill_topk(_ref(z), _ref(distill), row_loss, _ref(dz), ws, ws_bytes, stream)
+    return _check(r) if check else r
+
+
+def mebp_head_workspace_bytes(cfg: MebpConfig, rows: int, top_k: int = 0) -> int:
+    return lib().mebp_head_workspace_bytes(C.byref(cfg), rows, top_k)
+
+
+def mebp_lm_head_logits(cfg, emb, norm_final, x, rows, z, ws, ws_bytes, stream=0, check=True):
+    r = lib().mebp_lm_head_logits(C.byref(cfg), _ref(emb), norm_final, x, rows, _ref(z), ws, ws_bytes, stream)
+    return _check(r) if check else r
+
+
+def mebp_lm_head_logits_backward(cfg, emb, norm_final, x, rows, dz, dx, ws, ws_bytes, stream=0, check=True):
+    r = lib().mebp_lm_head_logits_backward(C.byref(cfg), _ref(emb), norm_final, x, rows, _ref(dz), dx, ws, ws_bytes,
+                                           stream)
+    return _check(r) if check else r
+
+
+def mebp_lm_head_logprobs(cfg, emb, norm_final, x, rows, targets, temperature, top_k, out, ws, ws_bytes, stream=0,
+                          check=True):
+    r = lib().mebp_lm_head_logprobs(C.byref(cfg), _ref(emb), norm_final, x, rows, targets, temperature, top_k, _ref(out),
+                                    ws, ws_bytes, stream)
+    return _check(r) if check else r
+
+
+def mebp_lm_head_distill_backward(cfg, emb, norm_final, x, rows, distill, loss, row_loss, dx, ws, ws_bytes, stream=0,
+                                  check=True):
+    r = lib().mebp_lm_head_distill_backward(C.byref(cfg), _ref(emb), norm_final, x, rows, _ref(distill), loss, row_loss,
+                                            dx, ws, ws_bytes, stream)
+    return _check(r) if check else r
+
+
+def mebp_distill_step_workspace_bytes(cfg: MebpConfig, B: int, T: int) -> int:
+    return lib().mebp_distill_step_workspace_bytes(C.byref(cfg), B, T)
+
+
+def mebp_train_step_distill(cfg, emb, layers, norm_final, lora, ids, B, T, distill, ckpt, loss, row_loss, grads, dx0,
+                            ws, ws_bytes, stream=0, check=True):
+    r = lib().mebp_train_step_distill(C.byref(cfg), _ref(emb), layers, norm_final, lora, ids, B, T, _ref(distill), ckpt,
+                                      loss, row_loss, grads, dx0, ws, ws_bytes, stream)
     return _check(r) if check else r
 
 

@@ -91,9 +91,10 @@ std::atomic<int> g_guards{[] {
 constexpr size_t kGuardBytes = 256;
 constexpr int kMaxGuards = 2 * S_COUNT;
 
-// Slots of the workspaces of the operators on logits; their guards' tags follow the others'.
-enum OpSlot { OP_STATS, OP_KEYS, OP_PICKED, OP_COUNT };
-const char* kOpSlotNames[OP_COUNT] = {"logit_stats", "logit_keys", "logit_picked"};
+// Slots of the workspaces of the operators on logits and of the head that runs them; their guards' tags follow the others'.
+enum OpSlot { OP_STATS, OP_KEYS, OP_PICKED, OP_HF, OP_Z, OP_DZ, OP_DHF, OP_PLANES, OP_ROW_LOSS, OP_COUNT };
+const char* kOpSlotNames[OP_COUNT] = {"logit_stats", "logit_keys", "logit_picked", "head_hf", "head_logits",
+                                      "head_dlogits", "head_dhf", "head_planes", "head_row_loss"};
 constexpr int kOpTag = 2 * S_COUNT;
 
 // A layer's weights as fragments: none, one product's at a time, or all at once.
@@ -166,13 +167,16 @@ size_t large_tile_elems(int M, int Kout, std::initializer_list<int> Ns, bool sof
 // Columns of one LM-head vocabulary chunk: the chunk's fp16 logits [N][chunk] take at most
 // MEBP_LM_CHUNK_MB (default 512) MiB; a multiple of 256 columns, the whole vocabulary when
 // it fits.
-int lm_chunk_cols(size_t N, int V) {
+size_t lm_chunk_budget() {
   static const size_t budget = [] {
     const char* e = getenv("MEBP_LM_CHUNK_MB");
     const long v = e && *e ? atol(e) : 512;
     return (size_t)(v > 0 ? v : 512) << 20;
   }();
-  size_t c = budget / (N * 2) / 256 * 256;
+  return budget;
+}
+int lm_chunk_cols(size_t N, int V) {
+  size_t c = lm_chunk_budget() / (N * 2) / 256 * 256;
   if (c < 256) c = 256;
   return c >= (size_t)V ? V : (int)c;
 }
@@ -1294,10 +1298,13 @@ OffloadStreams* offload_streams() {
   return o;
 }
 
+// final_block(x, x_last, g, gb, hf_ready): x_last -> loss and dE/dx_last in fp32 (g) and bf16 (gb); hf_ready:
+// the final norm of x_last is in the workspace's slot already.
+template <class FinalBlock>
 int train_step_impl(const mebp_config* cfg, const mebp_q4* emb, const mebp_layer_base* layers,
                     const float* norm_final, const mebp_layer_lora* lora, const int32_t* ids, int32_t B, int32_t T,
-                    float* ring, Offload* off, float* loss, const mebp_layer_lora_grad* grads, float* dx0, void* ws,
-                    mebp_stream_t stream) {
+                    float* ring, Offload* off, FinalBlock&& final_block, const mebp_layer_lora_grad* grads,
+                    float* dx0, void* ws, mebp_stream_t stream) {
   int e;
   Ctx x = make_ctx(cfg, B, T, ws, stream);
   const size_t stride = (size_t)x.D.N * x.D.d, bytes = stride * sizeof(float);
@@ -1383,7 +1390,7 @@ int train_step_impl(const mebp_config* cfg, const mebp_q4* emb, const mebp_layer
   };
   if (!side) {
     // final linear + loss block, then the layers in reverse on the caller's stream
-    if ((e = lm_head(x, emb, norm_final, ck(L), ids, loss, g, dyb_top, hf_fused))) return e;
+    if ((e = final_block(x, ck(L), g, dyb_top, hf_fused))) return e;
     if (off && L - off->R >= 0 && (e = fetch(L - off->R, x.st))) return e;
     for (int l = L - 1; l >= 0; --l) {
       Ctx b = x;
@@ -1416,7 +1423,7 @@ int train_step_impl(const mebp_config* cfg, const mebp_q4* emb, const mebp_layer
     // the first recompute)
     if ((e = recompute(L - 1))) return e;
     HIP_TRY(hipEventRecord(side->ev_rec, side->st));
-    if ((e = lm_head(x, emb, norm_final, ck(L), ids, loss, g, dyb_top, hf_fused))) return e;
+    if ((e = final_block(x, ck(L), g, dyb_top, hf_fused))) return e;
     if (off && L - off->R >= 0 && (e = fetch(L - off->R, x.st))) return e;
     for (int l = L - 1; l >= 0; --l) {
       HIP_TRY(hipStreamWaitEvent(x.st, side->ev_rec, 0));  // recompute(l) done
@@ -1454,6 +1461,13 @@ int train_step_impl(const mebp_config* cfg, const mebp_q4* emb, const mebp_layer
     HIP_TRY(hipStreamWaitEvent(x.st, off->ev_go, 0));
   }
   return MEBP_OK;
+}
+
+// the final linear layer and the next-token cross-entropy
+auto ce_block(const mebp_q4* emb, const float* norm_final, const int32_t* ids, float* loss) {
+  return [=](const Ctx& x, const float* x_last, float* g, bf16* gb, bool hf_ready) {
+    return lm_head(x, emb, norm_final, x_last, ids, loss, g, gb, hf_ready);
+  };
 }
 
 }  // namespace
@@ -1628,11 +1642,12 @@ int mebp_embed(const mebp_config* cfg, const mebp_q4* emb, const int32_t* ids, i
 
 int check_train_args(const mebp_config* cfg, const mebp_q4* emb, const mebp_layer_base* layers,
                      const float* norm_final, const mebp_layer_lora* lora, const int32_t* ids, int32_t B, int32_t T,
-                     float* loss, const mebp_layer_lora_grad* grads, float* dx0, void* ws, size_t ws_bytes) {
+                     float* loss, const mebp_layer_lora_grad* grads, float* dx0, void* ws, size_t ws_bytes,
+                     bool next_token = true) {
   int e;
   if ((e = check_config(cfg)) || (e = check_shape(B, T))) return e;
   if (cfg->vocab <= 0) return fail(MEBP_EINVAL, "vocab must be > 0 for a training step");
-  if (T < 2) return fail(MEBP_EINVAL, "T must be >= 2 (no next-token target otherwise)");
+  if (next_token && T < 2) return fail(MEBP_EINVAL, "T must be >= 2 (no next-token target otherwise)");
   if (!layers || !lora) return fail(MEBP_EINVAL, "layers / lora array is NULL");
   if (!grads && cfg->lora_mask) return fail(MEBP_EINVAL, "grads array is NULL");
   for (int l = 0; l < cfg->n_layers; ++l) {
@@ -1657,7 +1672,8 @@ int mebp_train_step(const mebp_config* cfg, const mebp_q4* emb, const mebp_layer
       (e = check_act(ckpt, "ckpt")))
     return e;
   return guarded(cfg, B, T, ws, stream, [&] {
-    return train_step_impl(cfg, emb, layers, norm_final, lora, ids, B, T, ckpt, nullptr, loss, grads, dx0, ws, stream);
+    return train_step_impl(cfg, emb, layers, norm_final, lora, ids, B, T, ckpt, nullptr,
+                           ce_block(emb, norm_final, ids, loss), grads, dx0, ws, stream);
   });
 }
 
@@ -1696,7 +1712,8 @@ int mebp_train_step_offload(const mebp_config* cfg, const mebp_q4* emb, const me
   static std::mutex mu;  // the copy stream and its events are shared by the calls on a device
   std::lock_guard<std::mutex> g(mu);
   return guarded(cfg, B, T, ws, stream, [&] {
-    return train_step_impl(cfg, emb, layers, norm_final, lora, ids, B, T, ring, &off, loss, grads, dx0, ws, stream);
+    return train_step_impl(cfg, emb, layers, norm_final, lora, ids, B, T, ring, &off,
+                           ce_block(emb, norm_final, ids, loss), grads, dx0, ws, stream);
   });
 }
 
@@ -2046,6 +2063,282 @@ int mebp_distill_topk(const mebp_logits* z, const mebp_distill* d, float* row_lo
   return guarded(o, ws, stream, [&] {
     HIP_TRY(launch_distill(distill_args(*z, *d, row_loss, dz, s), z->dtype, dz ? dz->dtype : 0, (hipStream_t)stream));
     return (int)MEBP_OK;
+  });
+}
+
+}  // extern "C"
+
+namespace {
+// ------------------------------------------------------------------ the head's logits
+// Rows of a block: fp32 logits and bf16 gradients within the budget of the fused head's chunks.
+int head_block_rows(int rows, int V) {
+  const size_t r = lm_chunk_budget() / ((size_t)V * 6);
+  const int n = (int)std::min<size_t>(r >= 256 ? r / 256 * 256 : std::max<size_t>(r / 64 * 64, 64), 1 << 16);
+  return std::max(1, std::min(rows, n));
+}
+
+struct HeadLayout {
+  OpLayout o;
+  int rows;              // of a block
+  size_t plane_floats;   // of the dH product's split planes
+};
+HeadLayout head_layout(const mebp_config* c, int rows, int top_k) {
+  HeadLayout h;
+  const int V = c->vocab, d = c->hidden;
+  const int r = h.rows = head_block_rows(rows, V);
+  // parts of all rows of a block: logit_split() makes no more than this of any number of them
+  const size_t parts = std::min<size_t>((size_t)r * kLogitParts, 1024 + r);
+  h.o.place(OP_STATS, parts * sizeof(float4));
+  h.o.place(OP_KEYS, parts * top_k * 8);
+  h.o.place(OP_PICKED, (size_t)r * (kMaxTop + 1) * 4);
+  h.o.place(OP_HF, (size_t)r * d * 2);
+  h.o.place(OP_Z, (size_t)r * V * 4);
+  h.o.place(OP_DZ, (size_t)r * V * 2);
+  h.o.place(OP_DHF, (size_t)r * d * 4);
+  h.plane_floats = (size_t)lm_q4_splits(r, d, V) * r * d;
+  h.o.place(OP_PLANES, h.plane_floats * 4);
+  h.o.place(OP_ROW_LOSS, (size_t)rows * 4);
+  h.o.done();
+  return h;
+}
+
+int check_head(const mebp_config* c, const mebp_q4* emb, const float* norm_final, const float* x, int rows) {
+  int e;
+  if ((e = check_config(c))) return e;
+  if (c->vocab <= 0) return fail(MEBP_EINVAL, "vocab must be > 0 for the LM head");
+  if ((e = check_logits_shape(rows, c->vocab, 0)) || (e = check_q4(emb, "embedding")) ||
+      (e = check_act(norm_final, "norm_final")))
+    return e;
+  return rows ? check_act(x, "x") : MEBP_OK;
+}
+
+// logits or gradients that the products write or read themselves
+int check_head_logits(const mebp_config* c, int rows, const mebp_logits* z, const char* what) {
+  int e;
+  if ((e = check_logits(z, what))) return e;
+  if (z->rows != rows || z->vocab != c->vocab) return fail(MEBP_EINVAL, "%s: not of %d rows and the config's vocab", what, rows);
+  if (z->ld % 8 || z->ld >= (1 << 20)) return fail(MEBP_EUNSUPPORTED, "%s: ld %lld not a multiple of 8 below 2^20", what, (long long)z->ld);
+  return rows ? check_act(z->data, what) : MEBP_OK;
+}
+
+int check_head_grad(const float* x, const float* dx, int rows) {
+  if (!rows) return MEBP_OK;
+  const int e = check_act(dx, "dx");
+  return e ? e : dx == x ? fail(MEBP_EINVAL, "dx must not be x") : MEBP_OK;
+}
+
+struct Head {
+  const mebp_config* c;
+  const mebp_q4* emb;
+  const float* norm;
+  HeadLayout h;
+  void* ws;
+  hipStream_t st;
+
+  template <class F>
+  int blocks(int rows, F&& f) const {
+    for (int r0 = 0; r0 < rows; r0 += h.rows) {
+      const int e = f(r0, std::min(h.rows, rows - r0));
+      if (e) return e;
+    }
+    return MEBP_OK;
+  }
+  mebp_logits block(int slot, int n, int dtype) const {
+    return mebp_logits{h.o.at<void>(ws, slot), c->vocab, n, c->vocab, dtype};
+  }
+  // z of n rows, from x or from its final norm hf where that is given
+  int logits(const float* x, const f16* hf, const mebp_logits& z) const {
+    const int d = c->hidden, n = z.rows;
+    if (!hf) {
+      f16* y = h.o.at<f16>(ws, OP_HF);
+      HIP_TRY(launch_rmsnorm_fwd(x, norm, n, d, c->rms_eps, y, nullptr, st));
+      hf = y;
+    }
+    NtArgs a{};
+    a.X = hf;
+    a.lda = d;
+    a.M = n;
+    a.K = d;
+    a.nseg = 1;
+    a.seg[0].q4 = emb->q4;
+    a.seg[0].scale = emb->scale;
+    a.seg[0].N = c->vocab;
+    a.seg[0].out = z.data;
+    a.seg[0].ldo = (int)z.ld;
+    HIP_TRY(launch_gemm_nt(a, z.dtype == MEBP_F32 ? NT_STORE_F32 : NT_STORE_F16, st));
+    return MEBP_OK;
+  }
+  // dx of n rows, and its bf16 copy where dxb is given
+  int backward(const float* x, const mebp_logits& dz, float* dx, bf16* dxb) const {
+    const int d = c->hidden, n = dz.rows;
+    float *planes = h.o.at<float>(ws, OP_PLANES), *dhf = h.o.at<float>(ws, OP_DHF);
+    TnArgs t{};
+    t.M = n;
+    t.Kout = d;
+    t.nseg = 1;
+    t.seg[0].G = (const bf16*)dz.data;
+    t.seg[0].ldg = (int)dz.ld;
+    t.seg[0].q4 = emb->q4;
+    t.seg[0].scale = emb->scale;
+    t.seg[0].N = c->vocab;
+    t.out = planes;
+    t.ldo = d;
+    t.part_floats = h.plane_floats;
+    t.splits = (int)std::min<size_t>(lm_q4_splits(n, d, c->vocab), h.plane_floats / ((size_t)n * d));
+    HIP_TRY(launch_gemm_tn(t, TN_PARTIAL_F32, TN_A_BF16, st));
+    HIP_TRY(launch_ce_dh_accum(planes, t.splits, n, d, nullptr, 1, dhf, st));
+    HIP_TRY(launch_rmsnorm_bwd(x, norm, dhf, nullptr, n, d, c->rms_eps, dx, dxb, st));
+    return MEBP_OK;
+  }
+  int distill(const float* x, const f16* hf, int rows, const mebp_distill& p, float* loss, float* row_loss, float* dx,
+              bf16* dxb) const {
+    const size_t d = c->hidden;
+    float* rl = row_loss ? row_loss : h.o.at<float>(ws, OP_ROW_LOSS);
+    const int e = blocks(rows, [&](int r0, int n) {
+      mebp_distill q = p;
+      q.ids += (size_t)r0 * p.k;
+      q.logits += (size_t)r0 * p.k;
+      if (q.targets) q.targets += r0;
+      if (q.row_weight) q.row_weight += r0;
+      const mebp_logits z = block(OP_Z, n, MEBP_F32), dz = block(OP_DZ, n, MEBP_BF16);
+      LogitSplit s = logit_split(n, c->vocab);
+      set_slots(h.o, ws, &s);
+      int e2;
+      if ((e2 = logits(x + r0 * d, hf ? hf + r0 * d : nullptr, z))) return e2;
+      HIP_TRY(launch_distill(distill_args(z, q, rl + r0, &dz, s), z.dtype, dz.dtype, st));
+      return backward(x + r0 * d, dz, dx + r0 * d, dxb ? dxb + r0 * d : nullptr);
+    });
+    if (e) return e;
+    HIP_TRY(launch_ce_loss(rl, nullptr, rows, 1.0f, loss, st));
+    return MEBP_OK;
+  }
+};
+}  // namespace
+
+extern "C" {
+
+size_t mebp_head_workspace_bytes(const mebp_config* cfg, int32_t rows, int32_t top_k) {
+  std::string saved = g_last_error;
+  if (check_config(cfg) || check_logits_shape(rows, cfg->vocab, top_k)) {
+    g_last_error = saved;
+    return 0;
+  }
+  return head_layout(cfg, rows, top_k).o.L.total;
+}
+
+int mebp_lm_head_logits(const mebp_config* cfg, const mebp_q4* emb, const float* norm_final, const float* x,
+                        int32_t rows, const mebp_logits* z, void* ws, size_t ws_bytes, mebp_stream_t stream) {
+  int e;
+  if ((e = check_head(cfg, emb, norm_final, x, rows)) || (e = check_head_logits(cfg, rows, z, "logits"))) return e;
+  if (z->dtype == MEBP_BF16) return fail(MEBP_EUNSUPPORTED, "logits: dtype bf16 (the head writes fp32 or fp16)");
+  const Head h{cfg, emb, norm_final, head_layout(cfg, rows, 0), ws, (hipStream_t)stream};
+  if ((e = check_op_ws(h.h.o, ws, ws_bytes))) return e;
+  if (!rows) return MEBP_OK;
+  return guarded(h.h.o, ws, stream, [&] {
+    return h.blocks(rows, [&](int r0, int n) {
+      mebp_logits b = *z;
+      b.rows = n;
+      b.data = (char*)z->data + (size_t)r0 * z->ld * logit_size(z->dtype);
+      return h.logits(x + (size_t)r0 * cfg->hidden, nullptr, b);
+    });
+  });
+}
+
+int mebp_lm_head_logits_backward(const mebp_config* cfg, const mebp_q4* emb, const float* norm_final, const float* x,
+                                 int32_t rows, const mebp_logits* dz, float* dx, void* ws, size_t ws_bytes,
+                                 mebp_stream_t stream) {
+  int e;
+  if ((e = check_head(cfg, emb, norm_final, x, rows)) || (e = check_head_logits(cfg, rows, dz, "dz")) ||
+      (e = check_head_grad(x, dx, rows)))
+    return e;
+  if (dz->dtype != MEBP_BF16) return fail(MEBP_EUNSUPPORTED, "dz: dtype not bf16");
+  const Head h{cfg, emb, norm_final, head_layout(cfg, rows, 0), ws, (hipStream_t)stream};
+  if ((e = check_op_ws(h.h.o, ws, ws_bytes))) return e;
+  if (!rows) return MEBP_OK;
+  return guarded(h.h.o, ws, stream, [&] {
+    return h.blocks(rows, [&](int r0, int n) {
+      mebp_logits b = *dz;
+      b.rows = n;
+      b.data = (char*)dz->data + (size_t)r0 * dz->ld * 2;
+      const size_t at = (size_t)r0 * cfg->hidden;
+      return h.backward(x + at, b, dx + at, nullptr);
+    });
+  });
+}
+
+int mebp_lm_head_logprobs(const mebp_config* cfg, const mebp_q4* emb, const float* norm_final, const float* x,
+                          int32_t rows, const int32_t* targets, float temperature, int32_t top_k,
+                          const mebp_token_scores* out, void* ws, size_t ws_bytes, mebp_stream_t stream) {
+  int e;
+  if ((e = check_head(cfg, emb, norm_final, x, rows)) || (e = check_logits_shape(rows, cfg->vocab, top_k)) ||
+      (e = check_scores(targets, temperature, rows, top_k, out)))
+    return e;
+  const Head h{cfg, emb, norm_final, head_layout(cfg, rows, top_k), ws, (hipStream_t)stream};
+  if ((e = check_op_ws(h.h.o, ws, ws_bytes))) return e;
+  if (!rows) return MEBP_OK;
+  return guarded(h.h.o, ws, stream, [&] {
+    return h.blocks(rows, [&](int r0, int n) {
+      const mebp_logits z = h.block(OP_Z, n, MEBP_F32);
+      mebp_token_scores o = *out;
+      if (o.logp) o.logp += r0;
+      if (o.lse) o.lse += r0;
+      if (o.entropy) o.entropy += r0;
+      if (o.top_ids) o.top_ids += (size_t)r0 * top_k;
+      if (o.top_logp) o.top_logp += (size_t)r0 * top_k;
+      LogitSplit s = logit_split(n, cfg->vocab);
+      set_slots(h.h.o, ws, &s);
+      int e2;
+      if ((e2 = h.logits(x + (size_t)r0 * cfg->hidden, nullptr, z))) return e2;
+      HIP_TRY(launch_scores(score_args(z, targets ? targets + r0 : nullptr, temperature, top_k, o, s), z.dtype, h.st));
+      return (int)MEBP_OK;
+    });
+  });
+}
+
+int mebp_lm_head_distill_backward(const mebp_config* cfg, const mebp_q4* emb, const float* norm_final, const float* x,
+                                  int32_t rows, const mebp_distill* d, float* loss, float* row_loss, float* dx,
+                                  void* ws, size_t ws_bytes, mebp_stream_t stream) {
+  int e;
+  if ((e = check_head(cfg, emb, norm_final, x, rows)) || (e = check_distill(d, rows, loss)) ||
+      (e = check_head_grad(x, dx, rows)))
+    return e;
+  if (row_loss && !aligned(row_loss, 4)) return fail(MEBP_EINVAL, "row_loss not 4-byte aligned");
+  const Head h{cfg, emb, norm_final, head_layout(cfg, rows, 0), ws, (hipStream_t)stream};
+  if ((e = check_op_ws(h.h.o, ws, ws_bytes))) return e;
+  if (!rows) return MEBP_OK;
+  return guarded(h.h.o, ws, stream, [&] { return h.distill(x, nullptr, rows, *d, loss, row_loss, dx, nullptr); });
+}
+
+size_t mebp_distill_step_workspace_bytes(const mebp_config* cfg, int32_t B, int32_t T) {
+  const size_t step = mebp_workspace_bytes(cfg, B, T);
+  const size_t head = step ? mebp_head_workspace_bytes(cfg, B * T, 0) : 0;
+  return head ? step + head : 0;
+}
+
+int mebp_train_step_distill(const mebp_config* cfg, const mebp_q4* emb, const mebp_layer_base* layers,
+                            const float* norm_final, const mebp_layer_lora* lora, const int32_t* ids, int32_t B,
+                            int32_t T, const mebp_distill* d, float* ckpt, float* loss, float* row_loss,
+                            const mebp_layer_lora_grad* grads, float* dx0, void* ws, size_t ws_bytes,
+                            mebp_stream_t stream) {
+  int e;
+  if ((e = check_train_args(cfg, emb, layers, norm_final, lora, ids, B, T, loss, grads, dx0, ws, ws_bytes, false)) ||
+      (e = check_act(ckpt, "ckpt")) || (e = check_logits_shape(B * T, cfg->vocab, 0)) ||
+      (e = check_distill(d, B * T, loss)))
+    return e;
+  if (row_loss && !aligned(row_loss, 4)) return fail(MEBP_EINVAL, "row_loss not 4-byte aligned");
+  // the step's own layout, then the head's
+  const size_t step = mebp_workspace_bytes(cfg, B, T), need = mebp_distill_step_workspace_bytes(cfg, B, T);
+  if (ws_bytes < need) return fail(MEBP_EWORKSPACE, "workspace %zu bytes < required %zu", ws_bytes, need);
+  void* head_ws = (char*)ws + step;
+  const HeadLayout hl = head_layout(cfg, B * T, 0);
+  auto block = [&](const Ctx& x, const float* x_last, float* g, bf16* gb, bool hf_ready) {
+    const Head h{cfg, emb, norm_final, hl, head_ws, x.st};
+    return h.distill(x_last, hf_ready ? xs<f16>(x, S_HF) : nullptr, x.D.N, *d, loss, row_loss, g, gb);
+  };
+  return guarded(cfg, B, T, ws, stream, [&] {
+    return guarded(hl.o, head_ws, stream, [&] {
+      return train_step_impl(cfg, emb, layers, norm_final, lora, ids, B, T, ckpt, nullptr, block, grads, dx0, ws, stream);
+    });
   });
 }
 

@@ -96,6 +96,29 @@ def _logits_ws(ws: Optional[torch.Tensor], z: torch.Tensor, top_k: int):
     return ws, ws.nbytes
 
 
+def _scores(z: torch.Tensor, n: int, targets, top_k: int, out: Optional[dict]):
+    """The outputs of a scoring call over n rows (made where `out` is None), and the struct of them."""
+    f32, one = torch.float32, (n,)
+    if out is None:
+        names = ["lse", "entropy"] + (["logp"] if targets is not None else [])
+        out = {k: torch.empty(n, dtype=f32, device=z.device) for k in names}
+        if top_k > 0:
+            out["top_ids"] = torch.empty((n, top_k), dtype=torch.int32, device=z.device)
+            out["top_logp"] = torch.empty((n, top_k), dtype=f32, device=z.device)
+    get = out.get
+    return out, L.MebpTokenScores(
+        _operand(get("logp"), f32, one, z, "logp"), _operand(get("lse"), f32, one, z, "lse"),
+        _operand(get("entropy"), f32, one, z, "entropy"), _operand(get("top_ids"), torch.int32, (n, top_k), z, "top_ids"),
+        _operand(get("top_logp"), f32, (n, top_k), z, "top_logp"))
+
+
+def _distill(z: torch.Tensor, n: int, ids, logits, temperature, alpha, targets, row_weight) -> L.MebpDistill:
+    k = ids.shape[-1]
+    return L.MebpDistill(_operand(ids, torch.int32, (n, k), z, "ids"), _operand(logits, torch.float32, (n, k), z, "logits"),
+                         _operand(targets, torch.int32, (n,), z, "targets"),
+                         _operand(row_weight, torch.float32, (n,), z, "row_weight"), k, temperature, alpha)
+
+
 @_on_device
 def token_logprobs(z: torch.Tensor, targets: Optional[torch.Tensor] = None, top_k: int = 0, temperature: float = 1.0,
                    out: Optional[dict] = None, ws: Optional[torch.Tensor] = None) -> dict:
@@ -103,20 +126,10 @@ def token_logprobs(z: torch.Tensor, targets: Optional[torch.Tensor] = None, top_
     ``targets``), ``lse``, ``entropy`` [rows] and, with ``top_k``, int32 ``top_ids`` and ``top_logp``
     [rows][top_k]. ``out``: the wanted ones of these as tensors to write into."""
     n = z.shape[0]
-    if out is None:
-        names = ["lse", "entropy"] + (["logp"] if targets is not None else [])
-        out = {k: torch.empty(n, dtype=torch.float32, device=z.device) for k in names}
-        if top_k > 0:
-            out["top_ids"] = torch.empty((n, top_k), dtype=torch.int32, device=z.device)
-            out["top_logp"] = torch.empty((n, top_k), dtype=torch.float32, device=z.device)
-    f32, one, get = torch.float32, (n,), out.get
-    s = L.MebpTokenScores(
-        _operand(get("logp"), f32, one, z, "logp"), _operand(get("lse"), f32, one, z, "lse"),
-        _operand(get("entropy"), f32, one, z, "entropy"), _operand(get("top_ids"), torch.int32, (n, top_k), z, "top_ids"),
-        _operand(get("top_logp"), f32, (n, top_k), z, "top_logp"))
+    out, s = _scores(z, n, targets, top_k, out)
     zs = logits_struct(z)
     ws, nb = _logits_ws(ws, z, top_k)
-    L.mebp_token_logprobs(zs, _operand(targets, torch.int32, one, z, "targets"), temperature, top_k, s, ws.data_ptr(),
+    L.mebp_token_logprobs(zs, _operand(targets, torch.int32, (n,), z, "targets"), temperature, top_k, s, ws.data_ptr(),
                           nb, stream_handle())
     return out
 
@@ -146,12 +159,10 @@ def distill_topk(z: torch.Tensor, ids: torch.Tensor, logits: torch.Tensor, row_l
                  ws: Optional[torch.Tensor] = None) -> torch.Tensor:
     """``mebp_distill_topk``: the loss of each row against a teacher's int32 ``ids`` and fp32
     ``logits`` [rows][k], and its gradient into ``dz`` where that is given."""
-    n, k = z.shape[0], ids.shape[-1]
+    n = z.shape[0]
     if row_loss is None:
         row_loss = torch.empty(n, dtype=torch.float32, device=z.device)
-    d = L.MebpDistill(_operand(ids, torch.int32, (n, k), z, "ids"), _operand(logits, torch.float32, (n, k), z, "logits"),
-                      _operand(targets, torch.int32, (n,), z, "targets"),
-                      _operand(row_weight, torch.float32, (n,), z, "row_weight"), k, temperature, alpha)
+    d = _distill(z, n, ids, logits, temperature, alpha, targets, row_weight)
     zs = logits_struct(z)
     ws, nb = _logits_ws(ws, z, 0)
     L.mebp_distill_topk(zs, d, _operand(row_loss, torch.float32, (n,), z, "row_loss"),
@@ -236,6 +247,7 @@ class DeviceModel:
         self.ws = torch.empty(self.ws_bytes, dtype=torch.uint8, device=device)
         self.loss = torch.zeros(1, dtype=torch.float32, device=device)
         self.ckpt = None
+        self.distill_ws = None
 
     # ------------------------------------------------------------------ entry points
     def layer_forward(self, l: int, x_in: torch.Tensor, x_out: torch.Tensor):
@@ -277,6 +289,75 @@ class DeviceModel:
         L.mebp_train_step_offload(self.ccfg, self.emb, self.base, ptr(self.norm_final), self.lora, ptr(self.ids),
                                   self.B, self.T, ptr(ckpt_host), ptr(ring), ring.shape[0], ptr(self.loss), self.grads,
                                   ptr(dx0), ptr(self.ws), self.ws_bytes, stream_handle())
+
+    # ---------------------------------------------------------------- operators on the head's logits
+    def _head_ws(self, rows: int, top_k: int = 0):
+        """A workspace of the head's calls, which lives until the stream is done with it."""
+        n = L.mebp_head_workspace_bytes(self.ccfg, rows, top_k)
+        if n == 0:
+            raise L.MebpError(L.MEBP_EINVAL, "invalid shape for the head's workspace")
+        return torch.empty(n, dtype=torch.uint8, device=self.device), n
+
+    def lm_head_logits(self, x: torch.Tensor, dtype: torch.dtype = torch.float32) -> torch.Tensor:
+        """Logits [rows][vocab] of hidden states x [rows][d] fp32, in fp32 or fp16."""
+        rows = x.shape[0]
+        z = torch.empty((rows, self.cfg.vocab), dtype=dtype, device=x.device)
+        ws, nb = self._head_ws(rows)
+        L.mebp_lm_head_logits(self.ccfg, self.emb, ptr(self.norm_final), self._x(x), rows, logits_struct(z), ptr(ws), nb,
+                              stream_handle())
+        return z
+
+    def lm_head_logits_backward(self, x: torch.Tensor, dz: torch.Tensor) -> torch.Tensor:
+        """The gradient w.r.t. x of bf16 gradients w.r.t. its logits."""
+        rows = x.shape[0]
+        dx = torch.empty_like(x)
+        ws, nb = self._head_ws(rows)
+        L.mebp_lm_head_logits_backward(self.ccfg, self.emb, ptr(self.norm_final), self._x(x), rows, logits_struct(dz, x),
+                                       ptr(dx), ptr(ws), nb, stream_handle())
+        return dx
+
+    def lm_head_logprobs(self, x: torch.Tensor, targets: Optional[torch.Tensor] = None, top_k: int = 0,
+                         temperature: float = 1.0, out: Optional[dict] = None) -> dict:
+        """`token_logprobs` of the head's logits of x, which are never held at once."""
+        rows = x.shape[0]
+        out, s = _scores(x, rows, targets, top_k, out)
+        ws, nb = self._head_ws(rows, top_k)
+        L.mebp_lm_head_logprobs(self.ccfg, self.emb, ptr(self.norm_final), self._x(x), rows,
+                                _operand(targets, torch.int32, (rows,), x, "targets"), temperature, top_k, s, ptr(ws), nb,
+                                stream_handle())
+        return out
+
+    def lm_head_distill(self, x: torch.Tensor, dx: torch.Tensor, ids: torch.Tensor, logits: torch.Tensor,
+                        temperature: float = 1.0, alpha: float = 1.0, targets: Optional[torch.Tensor] = None,
+                        row_weight: Optional[torch.Tensor] = None, row_loss: Optional[torch.Tensor] = None):
+        """Loss (into self.loss) and gradient of distilling the head's logits of x (`distill_topk`)."""
+        rows = x.shape[0]
+        d = _distill(x, rows, ids, logits, temperature, alpha, targets, row_weight)
+        ws, nb = self._head_ws(rows)
+        L.mebp_lm_head_distill_backward(self.ccfg, self.emb, ptr(self.norm_final), self._x(x), rows, d, ptr(self.loss),
+                                        _operand(row_loss, torch.float32, (rows,), x, "row_loss"),
+                                        _operand(dx, torch.float32, (rows, self.cfg.hidden), x, "dx"), ptr(ws), nb,
+                                        stream_handle())
+
+    def train_step_distill(self, ids: torch.Tensor, logits: torch.Tensor, temperature: float = 1.0, alpha: float = 1.0,
+                           targets: Optional[torch.Tensor] = None, row_weight: Optional[torch.Tensor] = None,
+                           row_loss: Optional[torch.Tensor] = None, dx0: Optional[torch.Tensor] = None):
+        """`train_step` against a teacher's int32 ids and fp32 logits [N][k]; its workspace is made by
+        the first such step."""
+        if self.L == 0:
+            raise ValueError("this input set has no layers")
+        ck = self.alloc_ckpt()
+        d = _distill(ck, self.N, ids, logits, temperature, alpha, targets, row_weight)
+        need = L.mebp_distill_step_workspace_bytes(self.ccfg, self.B, self.T)
+        if self.distill_ws is None or self.distill_ws.numel() < need:
+            self.distill_ws = torch.empty(need, dtype=torch.uint8, device=self.device)
+        L.mebp_train_step_distill(self.ccfg, self.emb, self.base, ptr(self.norm_final), self.lora, ptr(self.ids), self.B,
+                                  self.T, d, ptr(ck), ptr(self.loss),
+                                  _operand(row_loss, torch.float32, (self.N,), ck, "row_loss"), self.grads, ptr(dx0),
+                                  ptr(self.distill_ws), self.distill_ws.numel(), stream_handle())
+
+    def _x(self, x: torch.Tensor) -> int:
+        return _operand(x, torch.float32, (x.shape[0], self.cfg.hidden), self.norm_final, "x")
 
     def grad_probe(self) -> torch.Tensor:
         """First and last layers' LoRA gradients, concatenated (a cheap result fingerprint)."""

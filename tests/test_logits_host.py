@@ -7,8 +7,10 @@ import pytest
 import torch
 
 import logits_ref as R
+from mebp_inputs import CONFIGS, MINI
 from paper_2510_03425_amd import _lib as L
 from paper_2510_03425_amd import device as D
+from paper_2510_03425_amd.device import make_config
 
 Z, T, OUT, DZ, WS = 0x1000000, 0x2000000, 0x3000000, 0x8000000, 0x10000000
 BIG = 1 << 40
@@ -155,3 +157,95 @@ def test_reference_gradients_against_differences():
             d, _ = R.scores_grad(z, t, tau, a, b)
             want = (s(z + h * v)[name] - s(z - h * v)[name]) / (2 * h)
             assert torch.allclose(want, (d * v).sum(1), rtol=1e-7, atol=1e-8), name
+
+
+# ------------------------------------------------------------------ the head's logits
+EMB = L.MebpQ4(q4=0x1000, scale=0x2000)
+
+
+def _head(f, *args, cfg=None, emb=EMB, norm=0x300000, x=0x400000, rows=8, ws=WS, nb=BIG):
+    return f(cfg or make_config(MINI), emb, norm, x, rows, *args, ws, nb, 0, check=False)
+
+
+def _hz(**kw):
+    a = dict(data=Z, ld=MINI.vocab, rows=8, vocab=MINI.vocab, dtype=L.MEBP_F32)
+    a.update(kw)
+    return L.MebpLogits(**a)
+
+
+HEAD_CALLS = {
+    "logits": lambda **kw: _head(L.mebp_lm_head_logits, _hz(rows=kw.get("rows", 8)), **kw),
+    "backward": lambda **kw: _head(L.mebp_lm_head_logits_backward, _hz(rows=kw.get("rows", 8), dtype=L.MEBP_BF16), DZ, **kw),
+    "logprobs": lambda **kw: _head(L.mebp_lm_head_logprobs, T, 1.0, 5, L.MebpTokenScores(lse=OUT), **kw),
+    "distill": lambda **kw: _head(L.mebp_lm_head_distill_backward, L.MebpDistill(T, T, T, T, 8, 1.0, 0.5), OUT, OUT, DZ, **kw),
+}
+
+
+@pytest.mark.parametrize("name", list(HEAD_CALLS))
+def test_head_refused(built_lib, name):
+    call = HEAD_CALLS[name]
+    assert call(x=0) == L.MEBP_EINVAL and call(x=0x400004) == L.MEBP_EINVAL
+    assert call(norm=0) == L.MEBP_EINVAL and call(emb=None) == L.MEBP_EINVAL
+    assert call(rows=-1) == L.MEBP_EINVAL and call(ws=0) == L.MEBP_EINVAL and call(ws=WS + 64) == L.MEBP_EINVAL
+    c = make_config(MINI)
+    need = L.mebp_head_workspace_bytes(c, 8, 5 if name == "logprobs" else 0)
+    assert call(nb=need - 1) == L.MEBP_EWORKSPACE
+    c.vocab = 0
+    assert call(cfg=c) == L.MEBP_EINVAL and "vocab" in L.mebp_last_error()
+    assert call(rows=0, x=0) == L.MEBP_OK
+
+
+def test_head_logits_refused(built_lib):
+    f = lambda z: _head(L.mebp_lm_head_logits, z)
+    assert f(None) == L.MEBP_EINVAL and f(_hz(rows=7)) == L.MEBP_EINVAL and f(_hz(vocab=32)) == L.MEBP_EINVAL
+    assert f(_hz(dtype=L.MEBP_BF16)) == L.MEBP_EUNSUPPORTED and f(_hz(ld=MINI.vocab + 4)) == L.MEBP_EUNSUPPORTED
+    assert f(_hz(ld=1 << 20)) == L.MEBP_EUNSUPPORTED and f(_hz(data=Z + 8)) == L.MEBP_EINVAL
+    b = lambda z, dx=DZ: _head(L.mebp_lm_head_logits_backward, z, dx)
+    ok = _hz(dtype=L.MEBP_BF16)
+    assert b(_hz()) == L.MEBP_EUNSUPPORTED and b(ok, 0) == L.MEBP_EINVAL and b(ok, DZ + 4) == L.MEBP_EINVAL
+    assert b(ok, 0x400000) == L.MEBP_EINVAL and "dx" in L.mebp_last_error()
+
+
+def test_head_operators_refused(built_lib):
+    s = lambda t, tau, k, out: _head(L.mebp_lm_head_logprobs, t, tau, k, out)
+    assert s(T, 0.0, 5, L.MebpTokenScores(lse=OUT)) == L.MEBP_EINVAL
+    assert s(T, 1.0, 65, L.MebpTokenScores(lse=OUT)) == L.MEBP_EUNSUPPORTED
+    assert s(0, 1.0, 5, L.MebpTokenScores(logp=OUT)) == L.MEBP_EINVAL
+    assert s(T, 1.0, 0, L.MebpTokenScores(top_ids=OUT)) == L.MEBP_EINVAL
+    d = lambda loss=OUT, rl=0, **kw: _head(L.mebp_lm_head_distill_backward, L.MebpDistill(
+        **dict(dict(ids=T, logits=T, targets=T, row_weight=0, k=8, temperature=1.0, alpha=0.5), **kw)), loss, rl, DZ)
+    assert d(k=0) == L.MEBP_EUNSUPPORTED and d(alpha=2.0) == L.MEBP_EINVAL and d(ids=0) == L.MEBP_EINVAL
+    assert d(targets=0) == L.MEBP_EINVAL and d(loss=0) == L.MEBP_EINVAL and d(rl=OUT + 1) == L.MEBP_EINVAL
+
+
+def test_head_workspace_sizes(built_lib):
+    c = make_config(MINI)
+    assert L.mebp_head_workspace_bytes(c, -1) == 0 and L.mebp_head_workspace_bytes(c, 8, 65) == 0
+    assert 0 < L.mebp_head_workspace_bytes(c, 8) <= L.mebp_head_workspace_bytes(c, 8, 64) < L.mebp_head_workspace_bytes(c, 900, 64)
+    # many rows go in blocks: their logits and gradients stay within the budget of 512 MiB
+    big = make_config(CONFIGS["gemma3-4b"])
+    a, b = L.mebp_head_workspace_bytes(big, 4096), L.mebp_head_workspace_bytes(big, 16384)
+    assert b - a == (16384 - 4096) * 4 and a < 900 << 20
+    step = L.mebp_distill_step_workspace_bytes(c, 2, 160)
+    assert step == L.mebp_workspace_bytes(c, 2, 160) + L.mebp_head_workspace_bytes(c, 320)
+    assert L.mebp_distill_step_workspace_bytes(c, 0, 160) == 0
+
+
+def test_distillation_step_refused(built_lib):
+    c = make_config(MINI)
+    d = L.MebpDistill(T, T, T, T, 8, 1.0, 0.5)
+    need = L.mebp_distill_step_workspace_bytes(c, 2, 160)
+    n = c.n_layers
+    base, lora, grads = (L.MebpLayerBase * n)(), (L.MebpLayerLora * n)(), (L.MebpLayerLoraGrad * n)()
+    for l in range(n):
+        for i in range(7):
+            base[l].w[i].q4, base[l].w[i].scale = 0x1000, 0x2000
+            lora[l].A[i] = lora[l].B[i] = grads[l].dA[i] = grads[l].dB[i] = 0x3000
+        base[l].norm_attn = base[l].norm_mlp = 0x4000
+    f = lambda distill=d, nb=need, ckpt=0x5000, loss=OUT, rl=0: L.mebp_train_step_distill(
+        c, EMB, base, 0x300000, lora, T, 2, 160, distill, ckpt, loss, rl, grads, 0, WS, nb, 0, check=False)
+    assert f(nb=need - 1) == L.MEBP_EWORKSPACE
+    assert f(nb=L.mebp_workspace_bytes(c, 2, 160)) == L.MEBP_EWORKSPACE
+    assert f(distill=None) == L.MEBP_EINVAL and f(ckpt=0) == L.MEBP_EINVAL and f(loss=0) == L.MEBP_EINVAL
+    assert f(rl=OUT + 2) == L.MEBP_EINVAL
+    assert f(distill=L.MebpDistill(T, T, T, T, 99, 1.0, 0.5)) == L.MEBP_EUNSUPPORTED
