@@ -264,7 +264,7 @@ typedef struct {
   void* data;      /* [rows][ld], aligned to its element's size                            */
   int64_t ld;      /* elements from one row to the next, >= vocab; those behind a row's     */
                    /* vocab are neither read nor written                                   */
-  int32_t rows;    /* 0 .. 2^23                                                             */
+  int32_t rows;    /* 0 .. 2^22                                                             */
   int32_t vocab;   /* 1 .. 2^30                                                             */
   int32_t dtype;   /* MEBP_F32, MEBP_F16 or MEBP_BF16                                      */
 } mebp_logits;
@@ -314,7 +314,7 @@ int mebp_token_logprobs_backward(const mebp_logits* z, const int32_t* targets, f
 typedef struct {
   const int32_t* ids;      /* [rows][k] the teacher's token ids; < 0: no entry; an id may     */
                            /* occur twice (its probabilities add); >= vocab: the row is NaN  */
-  const float* logits;     /* [rows][k]; -inf: no entry                                     */
+  const float* logits;     /* [rows][k]; -inf: no entry; NaN or +inf: the row is NaN         */
   const int32_t* targets;  /* [rows] hard labels, read if alpha < 1; < 0: no such term here;  */
                            /* >= vocab: the row is NaN                                      */
   const float* row_weight; /* [rows] w, e.g. 1 / rows for a mean; NULL: 1. A row of weight 0 */
@@ -347,7 +347,8 @@ int mebp_distill_topk(const mebp_logits* z, const mebp_distill* d, float* row_lo
 size_t mebp_head_workspace_bytes(const mebp_config* cfg, int32_t rows, int32_t top_k);
 
 /* The logits themselves: z of `rows` rows and cfg->vocab columns, MEBP_F32 or MEBP_F16 (rounded to
- * it), ld a multiple of 8 below 2^20, data 16-byte aligned (written).                     */
+ * it), ld a multiple of 8 below 2^20 (a block's rows times ld below 2^29), data 16-byte aligned
+ * (written).                                                                             */
 int mebp_lm_head_logits(const mebp_config* cfg, const mebp_q4* emb, const float* norm_final, const float* x,
                         int32_t rows, const mebp_logits* z, void* ws, size_t ws_bytes, mebp_stream_t stream);
 
@@ -467,7 +468,8 @@ int mebp_kernel_timing_report(char* buf, size_t len);
  * that may be repeated computes its outputs from inputs it does not overwrite; the kernels
  * that update a buffer in place are refused with MEBP_EINVAL ("gemm_tn_act_bwd",
  * "splitk_finalize_actbwd", "rope_fwd", "qkv_post", "headnorm_bwd", "ce_chunk_stats",
- * "ce_probs", "ce_dh_accum", "ce_final", "lora_adamw", "lora_grad_accumulate"). With timing enabled, each burst of repeated launches is bracketed by one
+ * "ce_probs", "ce_dh_accum", "ce_final", "token_scores_grad_inplace", "distill_grad_inplace",
+ * "distill_row_inplace", "lora_adamw", "lora_grad_accumulate"). With timing enabled, each burst of repeated launches is bracketed by one
  * event pair and reported as `times` launches, so the report's average is the kernel's
  * back-to-back in-stream duration. Host-thread-unsafe; for benchmarks only. */
 int mebp_kernel_repeat(const char* kernel, int32_t times);

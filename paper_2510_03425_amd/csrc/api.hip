@@ -508,6 +508,7 @@ struct OpLayout {
   void done() {
     L.status_off = L.total;
     if (L.guards) L.total += 256;
+    L.total = std::max<size_t>(L.total, 256);  // (0 bytes are an invalid shape's)
   }
   template <class Tp>
   Tp* at(void* ws, int i) const {
@@ -1846,8 +1847,8 @@ constexpr int kMaxTop = 64;
 
 int check_logits_shape(int rows, int vocab, int top_k) {
   if (rows < 0 || vocab < 1) return fail(MEBP_EINVAL, "logits: rows %d < 0 or vocab %d < 1", rows, vocab);
-  if (rows > (1 << 23) || vocab > (1 << 30))
-    return fail(MEBP_EUNSUPPORTED, "logits: %d x %d above 2^23 rows or 2^30 columns", rows, vocab);
+  if (rows > (1 << 22) || vocab > (1 << 30))
+    return fail(MEBP_EUNSUPPORTED, "logits: %d x %d above 2^22 rows or 2^30 columns", rows, vocab);
   if (top_k < 0 || top_k > kMaxTop) return fail(MEBP_EUNSUPPORTED, "top_k %d not in [0, %d]", top_k, kMaxTop);
   return MEBP_OK;
 }
@@ -1894,9 +1895,10 @@ int check_temperature(float tau) {
 OpLayout logits_layout(int rows, int vocab, int top_k, LogitSplit* s) {
   OpLayout o;
   *s = logit_split(rows, vocab);
-  o.place(OP_STATS, (size_t)rows * s->n * sizeof(float4));
-  o.place(OP_KEYS, (size_t)rows * s->n * top_k * 8);
-  o.place(OP_PICKED, (size_t)rows * (kMaxTop + 1) * 4);
+  const size_t joined = s->n > 1 ? rows : 0;  // (a row in one part leaves nothing to join)
+  o.place(OP_STATS, joined * s->n * sizeof(float4));
+  o.place(OP_KEYS, joined * s->n * top_k * 8);
+  o.place(OP_PICKED, joined * (kMaxTop + 1) * 4);
   o.done();
   return o;
 }
@@ -2001,7 +2003,7 @@ size_t mebp_logits_workspace_bytes(int32_t rows, int32_t vocab, int32_t top_k) {
     return 0;
   }
   LogitSplit s;
-  return std::max<size_t>(logits_layout(rows, vocab, top_k, &s).L.total, 256);
+  return logits_layout(rows, vocab, top_k, &s).L.total;
 }
 
 int mebp_token_logprobs(const mebp_logits* z, const int32_t* targets, float temperature, int32_t top_k,
@@ -2118,6 +2120,9 @@ int check_head_logits(const mebp_config* c, int rows, const mebp_logits* z, cons
   if ((e = check_logits(z, what))) return e;
   if (z->rows != rows || z->vocab != c->vocab) return fail(MEBP_EINVAL, "%s: not of %d rows and the config's vocab", what, rows);
   if (z->ld % 8 || z->ld >= (1 << 20)) return fail(MEBP_EUNSUPPORTED, "%s: ld %lld not a multiple of 8 below 2^20", what, (long long)z->ld);
+  // (the products address a block with 32 bits)
+  if (z->ld * head_block_rows(rows, c->vocab) >= (1 << 29))
+    return fail(MEBP_EUNSUPPORTED, "%s: ld %lld too large for blocks of %d rows", what, (long long)z->ld, head_block_rows(rows, c->vocab));
   return rows ? check_act(z->data, what) : MEBP_OK;
 }
 

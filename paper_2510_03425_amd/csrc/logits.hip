@@ -77,7 +77,7 @@ constexpr int top_buffer(int n) { return 64 + 64 * n; }  // keys of a wave's buf
 // of the waves the least. k lanes of the row at least have reached it, so it bounds the row's k-th
 // logit from below; it is not far below, as the top logits are mostly in different lanes. `share`
 // holds each wave's bound, which only rises: an older one is valid too. Taken anew whenever the
-// groups seen have doubled, it lets about as many logits through between two of these times, some
+// groups seen have doubled (from four on), it lets about as many logits through between two of these times, some
 // 16 of a wave for 64 alternatives on 8 waves.
 //
 // A wave whose list has filled up has its own k-th as a second threshold: columns rise from one
@@ -165,7 +165,7 @@ struct Top {
   __device__ __forceinline__ void add(const Group<U, N>& g, float top, const T* row, int end) {
     most = fmaxf(most, top);
     const int seen = ++groups;
-    if (seen > 1 && (seen & (seen - 1)) == 0) publish();
+    if (seen > 2 && (seen & (seen - 1)) == 0) publish();
     if (!__any(top > thr)) return;
     shared_threshold();
     if (!__any(top > thr)) return;
@@ -270,9 +270,9 @@ __global__ __launch_bounds__(NT) void k_scores(ScoreArgs p) {
   }
 }
 
-// One workgroup per row. The parts' largest logits (the heads of their lists) bound the row's k-th from
-// below where there are at least k parts; each list gives the keys of its beginning that reach it, one
-// of each list at a time, to one wave's buffer.
+// One workgroup per row. Where there are at least k parts, their largest logits (the heads of their
+// lists) bound the row's k-th from below: each list gives the keys of its beginning that reach it, one
+// of each list at a time, to one wave's buffer. Else the waves merge whole lists, and then theirs.
 template <class T>
 __global__ __launch_bounds__(256) void k_scores_join(ScoreArgs p) {
   __shared__ u64 keys[kLogitParts * 64], buf[128];
@@ -280,14 +280,17 @@ __global__ __launch_bounds__(256) void k_scores_join(ScoreArgs p) {
   const int l = lane_id(), n = p.split.n, k = p.top_k;
   for (int i = threadIdx.x; i < n * k; i += 256) keys[i] = p.split.keys[row * n * k + i];
   if (k) __syncthreads();
+  Top<4> t;
+  t.start(k, buf, nullptr);
+  if (n < k) {
+    for (int i = threadIdx.x >> 6; i < n; i += 4) t.list = merge_keys(t.list, l < k ? keys[i * k + l] : 0ull, k);
+    t.join(buf);
+  }
   if (threadIdx.x >= 64) return;
   const float zt = target_logit<T>(p, (const T*)p.z + row * p.ld, row);
   const Acc a = join_parts<true, false>(p.split, row, p.c, 0.f);
-  Top<1> t;
-  t.start(k, buf, nullptr);
-  if (k) {
-    const uint32_t head = l < n ? (uint32_t)(keys[l * k] >> 32) : 0u;
-    const uint32_t bound = n >= k ? lanes_reach(head, k) : 0u;
+  if (k && n >= k) {
+    const uint32_t bound = lanes_reach(l < n ? (uint32_t)(keys[l * k] >> 32) : 0u, k);
     for (int j = 0; j < k; ++j) {
       const u64 key = l < n ? keys[l * k + j] : 0ull;
       if (!t.push(key, key && (uint32_t)(key >> 32) >= bound)) break;
@@ -375,6 +378,8 @@ hipError_t launch_scores(ScoreArgs a, int dtype, hipStream_t st) {
 hipError_t launch_scores_grad(ScoreGradArgs a, int dtype, int gtype, hipStream_t st) {
   a.split.cols = 8192;
   while (a.split.cols > 2048 && (size_t)a.rows * ((a.vocab + a.split.cols - 1) / a.split.cols) < 1024) a.split.cols /= 2;
+  // (a grid of 256-lane workgroups holds fewer than 2^24 of them)
+  while ((size_t)a.rows * ((a.vocab + a.split.cols - 1) / a.split.cols) > (1u << 23)) a.split.cols *= 2;
   a.split.n = (a.vocab + a.split.cols - 1) / a.split.cols;
   const unsigned grid = (unsigned)((size_t)a.rows * a.split.n);
   const double bytes = (double)a.rows * a.vocab * (type_bytes(dtype) + type_bytes(gtype));

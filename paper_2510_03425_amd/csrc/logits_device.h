@@ -253,10 +253,11 @@ DEV Acc join_parts(const LogitSplit& sp, size_t row, float c, float c1) {
 // The sums of a whole workgroup at one reference m, the largest logit of its first group: a weight is
 // then exp2(z c + k) with k = -m c rounded, two instructions instead of three and no maximum to keep,
 // and lanes and waves join by addition. k's rounding r = m c + k scales all weights alike and is taken
-// out at the end. fp32's exponents leave room for logits far above m; where they do not (sums that are
-// not finite: also NaN and +inf logits), or m is nothing to go by (no logit above -inf in the first
-// group, or of the size of the type's lowest value), served() is false and the caller sums again with
-// acc_add, a reference for each lane.
+// out at the end. fp32's exponents leave room for logits above m; where one lies 2^40 times its weight
+// above, and z c + k rounds the exponent by more than 2^-19 (or sums are not finite: NaN and +inf
+// logits), or m is nothing to go by (no logit above -inf in the first group, or of the size of the
+// type's lowest value), served() is false and the caller sums again with acc_add, a reference for each
+// lane.
 enum Softmaxes { ONE, TWO_EXP, TWO_SQUARE };  // at tau alone; also at 1; the same where tau is 2:
                                               // exp(z) is then exp(z / 2)^2
 template <bool ENT, Softmaxes SM>
@@ -314,8 +315,7 @@ struct Sums {
     if (SM != ONE) s1 = sum64(a.s1);
   }
   __device__ __forceinline__ bool served() const {
-    const bool one = s > 0.f && s < 1e37f && (!ENT || fabsf(w) < 1e37f);
-    return one && (SM == ONE || (s1 > 0.f && s1 < 1e37f));
+    return s > 0.f && s < 1e12f && (!ENT || fabsf(w) < 1e37f) && (SM == ONE || (s1 > 0.f && s1 < 1e37f));
   }
   // exp(k's rounding) at tau and at 1
   __device__ __forceinline__ float unround() const { return exp2_fast(-fmaf(m, c, k)); }
@@ -330,7 +330,7 @@ struct Sums {
   }
 };
 
-// the largest logit of the workgroup's first group
+// the largest value of the workgroup
 template <int NT>
 DEV float block_max(float v, Acc* lds) {
   v = max64(v);

@@ -43,7 +43,7 @@ def _distill(z=None, dz=None, loss=OUT, ws=WS, nb=BIG, **kw):
 @pytest.mark.parametrize("bad,code", [
     (dict(data=0), L.MEBP_EINVAL), (dict(data=Z + 2), L.MEBP_EINVAL), (dict(ld=999), L.MEBP_EINVAL),
     (dict(rows=-1), L.MEBP_EINVAL), (dict(vocab=0), L.MEBP_EINVAL), (dict(dtype=3), L.MEBP_EINVAL),
-    (dict(dtype=-1), L.MEBP_EINVAL), (dict(rows=(1 << 23) + 1), L.MEBP_EUNSUPPORTED),
+    (dict(dtype=-1), L.MEBP_EINVAL), (dict(rows=(1 << 22) + 1), L.MEBP_EUNSUPPORTED),
     (dict(vocab=(1 << 30) + 1, ld=1 << 31), L.MEBP_EUNSUPPORTED), (dict(ld=(1 << 32) + 1), L.MEBP_EUNSUPPORTED),
 ])
 def test_logits_refused(built_lib, call, bad, code):
@@ -106,8 +106,8 @@ def test_no_rows_enqueue_nothing(built_lib):
 
 def test_workspace_sizes(built_lib):
     f = L.mebp_logits_workspace_bytes
-    assert f(-1, 10) == 0 and f(1, 0) == 0 and f(1, 10, 65) == 0 and f((1 << 23) + 1, 10) == 0
-    for rows in (1, 3, 100, 1000, 4096):
+    assert f(-1, 10) == 0 and f(1, 0) == 0 and f(1, 10, 65) == 0 and f((1 << 22) + 1, 10) == 0
+    for rows in (1, 3, 100, 255, 1000, 1 << 22):
         for vocab in (1, 1000, 151936, 262144):
             assert 256 <= f(rows, vocab, 0) <= f(rows, vocab, 64) <= 4 << 20, (rows, vocab)
     prev = L.mebp_set_workspace_guards(True)
@@ -200,6 +200,8 @@ def test_head_logits_refused(built_lib):
     assert f(None) == L.MEBP_EINVAL and f(_hz(rows=7)) == L.MEBP_EINVAL and f(_hz(vocab=32)) == L.MEBP_EINVAL
     assert f(_hz(dtype=L.MEBP_BF16)) == L.MEBP_EUNSUPPORTED and f(_hz(ld=MINI.vocab + 4)) == L.MEBP_EUNSUPPORTED
     assert f(_hz(ld=1 << 20)) == L.MEBP_EUNSUPPORTED and f(_hz(data=Z + 8)) == L.MEBP_EINVAL
+    far = _head(L.mebp_lm_head_logits, _hz(rows=4096, ld=(1 << 20) - 8), rows=4096)
+    assert far == L.MEBP_EUNSUPPORTED and "blocks" in L.mebp_last_error()
     b = lambda z, dx=DZ: _head(L.mebp_lm_head_logits_backward, z, dx)
     ok = _hz(dtype=L.MEBP_BF16)
     assert b(_hz()) == L.MEBP_EUNSUPPORTED and b(ok, 0) == L.MEBP_EINVAL and b(ok, DZ + 4) == L.MEBP_EINVAL
