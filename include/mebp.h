@@ -329,8 +329,9 @@ typedef struct {
  *   dz = w (alpha tau (q - p) + (1 - alpha) (q1 - 1[target])).
  *   row_loss [rows] fp32 (written)
  *   dz       as in mebp_token_logprobs_backward
- * A row without entries has no distillation term. A row of nothing but -inf has loss +inf
- * (0 without entries and label) and gradient 0.                                            */
+ * A row without entries has no distillation term, one without a label either loss and gradient 0.
+ * Else a row of nothing but -inf has loss +inf and gradient 0, and a NaN or +inf logit makes a row
+ * NaN.                                                                                    */
 int mebp_distill_topk(const mebp_logits* z, const mebp_distill* d, float* row_loss, const mebp_logits* dz, void* ws,
                       size_t ws_bytes, mebp_stream_t stream);
 

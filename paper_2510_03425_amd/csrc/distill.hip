@@ -132,7 +132,7 @@ __global__ __launch_bounds__(64) void k_distill_join(DistillArgs p) {
 // What a row's gradient is made of (LDS, by the first wave).
 struct RowTerms {
   float m, c0, c1;  // reference, coefficients of exp((z - m) / tau) and of exp(z - m)
-  bool empty;       // no logit above -inf, or weight 0: no gradient
+  bool empty;       // no logit above -inf, or no term: no gradient
   // the columns that have a sparse term, -1: none, and the whole gradient there; the target is the last
   int col[65];
   float g[65];
@@ -172,7 +172,7 @@ DEV void set_terms(const DistillArgs& p, const Acc& a, const Teacher& t, const S
   const float mass = t.any ? sum64(t.id < 0 ? 0.f : t.p) : 0.f;
   const float soft = w * p.alpha * p.tau * mass, one = w * (1.f - p.alpha);
   const float hard = target >= p.vocab ? NAN : target >= 0 ? one : 0.f;
-  const bool empty = a.s == 0.f;
+  const bool empty = a.s == 0.f || (!t.any && target < 0);
   const float c0 = (TWO ? soft : soft + hard) / a.s, c1 = TWO ? hard / a.s1 : 0.f;
   r.col[l] = t.id < p.vocab && sp.first && !empty ? t.id : -1;
   r.g[l] = dense_grad<TWO>(zk, a.m, c0, c1, p.c) - w * p.alpha * p.tau * sp.P - (t.id == target ? one : 0.f);

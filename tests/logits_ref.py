@@ -109,6 +109,10 @@ def distill(z, ids, teacher, targets, weight, tau, alpha):
                 loss[r] = NAN
             loss[r] *= w[r]
             continue
+        if bool(torch.isnan(x).any()) or bool((x == INF).any()):
+            if len(i) or t >= 0:
+                loss[r], dz[r] = NAN, NAN
+            continue
         q, q1 = torch.softmax(x / tau, 0), torch.softmax(x, 0)
         L = torch.zeros((), dtype=torch.float64)
         if len(i):

@@ -229,7 +229,7 @@ def test_distill(built_lib, gpu, rows, vocab, k, dtype, gtype):
 def test_distill_of_special_entries(built_lib, gpu, vocab, tau, alpha):
     """Absent, repeated and out-of-range entries and targets, a target among the entries, rows of
     weight 0 with NaN logits, masked student rows."""
-    n, k = 14, 6
+    n, k = 15, 6
     z, _ = _logits(n, vocab, F32, 4)
     ids, tl, t = _teacher(n, k, vocab, 8)
     w = torch.rand(n, generator=torch.Generator().manual_seed(2)) + 0.5
@@ -249,6 +249,7 @@ def test_distill_of_special_entries(built_lib, gpu, vocab, tau, alpha):
     ids[12] = ids[12, 0].clone()     # one token, k times
     t[12] = ids[12, 0]
     tl[13] = torch.tensor([300.0, 0.0, -300.0, 1.0, 299.0, -1e30])
+    z[14], ids[14], t[14] = NAN, -1, -1  # nothing to learn from
     zd = _upload(z)
     dz = torch.empty_like(zd)
     loss = D.distill_topk(zd, ids.to(gpu), tl.to(gpu), None, dz, tau, alpha, t.to(gpu), w.to(gpu))
@@ -256,6 +257,68 @@ def test_distill_of_special_entries(built_lib, gpu, vocab, tau, alpha):
     for i in range(n):
         s = slice(i, i + 1)
         _check_distill(z[s], ids[s], tl[s], t[s], w[s], tau, alpha, loss[s], dz[s], f"row {i}")
+
+
+@pytest.mark.parametrize("rows,vocab,dtype,gtype", [
+    # rows of which a workgroup holds all in registers, some in LDS too, and some not at all
+    (97, 50257, F32, BF16), (96, 120001, F32, F32), (96, 131071, BF16, BF16), (98, 245763, F16, F16),
+])
+@pytest.mark.parametrize("tau,alpha", [(1.0, 1.0), (2.0, 0.7), (1.5, 0.7)])
+def test_distill_of_long_rows(built_lib, gpu, rows, vocab, dtype, gtype, tau, alpha):
+    say("distill rows", rows, vocab, dtype, gtype, tau, alpha)
+    z, zd = _logits(rows, vocab, dtype, rows + vocab, pad=1)
+    ids, tl, t = _teacher(rows, 8, vocab, rows)
+    w = torch.rand(rows, generator=torch.Generator().manual_seed(2)) + 0.5
+    w[3] = 0.0
+    dz = _upload(torch.zeros(rows, vocab, dtype=gtype), pad=3)
+    loss = D.distill_topk(zd, ids.to(gpu), tl.to(gpu), None, dz, tau, alpha, t.to(gpu), w.to(gpu))
+    torch.cuda.synchronize()
+    some = torch.tensor([0, 1, 3, 17, rows - 1])
+    _check_distill(z[some], ids[some], tl[some], t[some], w[some], tau, alpha, loss[some.to(gpu)], dz[some.to(gpu)])
+    _padding_untouched(dz)
+    # every row against 64 bits on the GPU, as a whole
+    u, q = zd.double(), torch.empty((rows, vocab), dtype=torch.float64, device=gpu)
+    p = torch.softmax(tl.to(gpu).double() / tau, 1)
+    q.copy_(alpha * tau * torch.softmax(u / tau, 1))
+    q.scatter_add_(1, ids.to(gpu).long(), -alpha * tau * p)
+    if alpha < 1:
+        q += (1 - alpha) * torch.softmax(u, 1)
+        q.scatter_add_(1, t.to(gpu).long()[:, None], torch.full((rows, 1), alpha - 1, dtype=torch.float64, device=gpu))
+    q *= w.to(gpu).double()[:, None]
+    err = (dz.double() - q).norm(dim=1) / q.norm(dim=1).clamp_min(1e-300)
+    assert bool((err <= 1e-5 + R.HALF_STEP[gtype] * 1.01).all()), err.max()
+
+
+@pytest.mark.parametrize("vocab,copies", [(1003, 1), (40003, 1), (40003, 7)])  # by rows, by parts, long rows
+@pytest.mark.parametrize("tau,alpha", [(1.0, 1.0), (2.0, 0.6), (1.5, 0.5)])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_distill_of_special_students(built_lib, gpu, vocab, copies, tau, alpha, dtype):
+    names, z = _special_rows(vocab, dtype)
+    late = z[0].clone()
+    late[: vocab // 2] = -INF  # the first columns are masked off
+    names, z = names + ["first half masked"], torch.cat([z, late[None]])
+    n = len(names)
+    ids, tl, t = _teacher(n, 5, vocab, 3)
+    at = names.index("one left")
+    ids[at] = vocab // 2  # (other tokens are masked: an infinite loss)
+    t[at] = vocab // 2
+    rep = lambda x: x.repeat(copies, *[1] * (x.dim() - 1)).to(gpu)
+    zd = _upload(z.repeat(copies, 1))
+    dz = torch.empty_like(zd, dtype=F32)
+    loss = D.distill_topk(zd, rep(ids), rep(tl), None, dz, tau, alpha, rep(t), None)
+    only = D.distill_topk(zd, rep(ids), rep(tl), None, None, tau, alpha, rep(t), None)
+    torch.cuda.synchronize()
+    for i, name in enumerate(names):
+        say("special student", name, dtype, vocab, tau, alpha)
+        s, d = slice(i, i + 1), slice((copies - 1) * n + i, (copies - 1) * n + i + 1)
+        if name in ("lowest", "half lowest"):
+            # the loss of a token at the type's lowest value is of its size, or beyond the type
+            assert not torch.isnan(dz[d]).any()
+            _check_distill(z[s], ids[s], tl[s], t[s], None, tau, alpha, R.distill(z[s], ids[s], tl[s], t[s], None, tau, alpha)[0],
+                           dz[d], name)
+            continue
+        _check_distill(z[s], ids[s], tl[s], t[s], None, tau, alpha, loss[d], dz[d], name)
+        _check_distill(z[s], ids[s], tl[s], t[s], None, tau, alpha, only[d], None, name)
 
 
 # ------------------------------------------------------------------ how they are called
