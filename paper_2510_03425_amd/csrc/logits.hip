@@ -77,8 +77,8 @@ constexpr int top_buffer(int n) { return 64 + 64 * n; }  // keys of a wave's buf
 // of the waves the least. k lanes of the row at least have reached it, so it bounds the row's k-th
 // logit from below; it is not far below, as the top logits are mostly in different lanes. `share`
 // holds each wave's bound, which only rises: an older one is valid too. Taken anew whenever the
-// groups seen have doubled (from four on), it lets about as many logits through between two of these times, some
-// 16 of a wave for 64 alternatives on 8 waves.
+// groups seen have doubled (from four on), it lets about as many logits through between two of these
+// times, some 16 of a wave for 64 alternatives on 8 waves.
 //
 // A wave whose list has filled up has its own k-th as a second threshold: columns rise from one
 // vector of a wave to the next, so a logit that equals it ranks behind it. One that equals another
@@ -158,11 +158,9 @@ struct Top {
     const uint32_t kth = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(list >> 32), k - 1);
     if (kth) thr = fmaxf(thr, order_value(kth));
   }
-  // A group of the row's columns before `end`. Where the buffer might not take another vector the rest
-  // of the group is read once more, vector by vector (rising logits; a loop of its own keeps one copy
-  // of the sort here instead of U).
-  template <class T, int U, int N>
-  __device__ __forceinline__ void add(const Group<U, N>& g, float top, const T* row, int end) {
+  // a group, vector by vector: the buffer takes one more where it holds less than 64 keys
+  template <int U, int N>
+  __device__ __forceinline__ void add(const Group<U, N>& g, float top) {
     most = fmaxf(most, top);
     const int seen = ++groups;
     if (seen > 2 && (seen & (seen - 1)) == 0) publish();
@@ -250,7 +248,7 @@ __global__ __launch_bounds__(NT) void k_scores(ScoreArgs p) {
       begun = true;
     }
     sums.add(g);
-    if constexpr (TOP) t.add(g, top, z, v1);
+    if constexpr (TOP) t.add(g, top);
   });
   sums.template join<NT>(red);
   Acc a = sums.acc();
@@ -337,11 +335,14 @@ __global__ __launch_bounds__(NT) void k_scores_grad(ScoreGradArgs p) {
 
 }  // namespace
 
-// Parts of a row: enough workgroups for the chip where there are few rows, of no fewer than 4096
-// columns each.
+// Parts of a row: enough workgroups for the chip where there are few long rows, of no fewer than 4096
+// columns each. The launch that joins them costs more than a workgroup's pass over a short row (call of
+// 8 rows of 50257 fp32 logits 15.0 us by parts and 10.7 whole, with 20 alternatives 15.3 both; of 100000
+// 15.3 and 12.9, 15.2 and 21.7), and from one row for each compute unit on there is nothing to gain
+// (151936 fp32 with 20 alternatives: 192 rows 30 us by parts and 38 whole, 256 rows 37 both).
 LogitSplit logit_split(int rows, int vocab) {
   LogitSplit s{};
-  const int want = rows >= 256 ? 1 : std::min(kLogitParts, (1024 + rows - 1) / std::max(rows, 1));
+  const int want = rows >= 256 || vocab <= 65536 ? 1 : std::min(kLogitParts, (1024 + rows - 1) / std::max(rows, 1));
   const int most = (vocab + 4095) / 4096;
   const int n = std::max(1, std::min(want, most));
   s.cols = ((vocab + n - 1) / n + 2047) / 2048 * 2048;

@@ -138,9 +138,11 @@ def test_hard_labels_alone_are_the_next_token_loss(built_lib, gpu):
     assert rel_l2(dx1.cpu(), dx0.cpu()) <= 2 * TOL
 
 
-def test_more_rows_than_a_block_holds(built_lib, gpu):
-    """Blocks of 1536 rows at this vocabulary, the last one of 164, on guarded workspaces."""
-    hidden, vocab, rows = 128, 50304, 1700
+@pytest.mark.parametrize("vocab,rows,block", [(50304, 1700, 1536), (70016, 1100, 1024)])
+def test_more_rows_than_a_block_holds(built_lib, gpu, vocab, rows, block):
+    """A block of `block` rows and the last one of some (of the larger vocabulary: by parts of
+    rows), on guarded workspaces."""
+    hidden = 128
     cfg = MINI.with_(name="blocks", n_layers=1, hidden=hidden, n_heads=1, n_kv_heads=1, head_dim=128, ffn=192, vocab=vocab,
                      batch=1, seq=64)
     inp = _inputs(cfg)
@@ -172,7 +174,7 @@ def test_more_rows_than_a_block_holds(built_lib, gpu):
     assert abs(dm.loss.item() - loss) <= 1e-3 * abs(loss)
     assert rel_l2(dx.cpu(), want.cpu()) <= TOL
     # z^T z x: each block with its own rows
-    for q in (slice(0, 40), slice(1530, 1545), slice(1660, 1700)):
+    for q in (slice(0, 40), slice(block - 6, block + 9), slice(rows - 40, rows)):
         xr = x[q].double().requires_grad_()
         g = torch.autograd.grad(ref.logits(xr), xr, z[q].bfloat16().double())[0]
         assert rel_l2(back[q].cpu(), g.cpu()) <= TOL

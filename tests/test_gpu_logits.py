@@ -53,7 +53,7 @@ def _check_scores(z, got, targets, top_k, tau):
 
 SHAPES = [  # rows, vocab, top_k: one column to more than one part of a row
     (1, 1, 1), (1, 2, 5), (3, 7, 64), (2, 63, 3), (5, 255, 64), (4, 1000, 20), (3, 2049, 1), (2, 4096, 8), (2, 4099, 33),
-    (1, 50257, 20), (7, 12289, 64), (1025, 1030, 4), (2, 151936, 64),
+    (1, 50257, 20), (7, 12289, 64), (1025, 1030, 4), (2, 151936, 64), (3, 65536, 7), (1, 70001, 64), (200, 65537, 2),
 ]
 
 
@@ -98,7 +98,7 @@ def _special_rows(vocab, dtype):
 
 
 @pytest.mark.parametrize("dtype", [F32, F16, BF16])
-@pytest.mark.parametrize("vocab,top_k", [(1003, 20), (20001, 64)])
+@pytest.mark.parametrize("vocab,top_k", [(1003, 20), (20001, 64), (70001, 64), (150001, 9)])
 def test_scores_of_special_rows(built_lib, gpu, dtype, vocab, top_k):
     names, z = _special_rows(vocab, dtype)
     t = torch.arange(len(names), dtype=torch.int32) * 37 % vocab
@@ -206,7 +206,7 @@ def _check_distill(z, ids, tl, t, w, tau, alpha, loss, dz, what=""):
 MODES = [(1.0, 1.0), (2.0, 0.7), (1.0, 0.4), (0.5, 1.0), (3.0, 0.0)]  # tau, alpha
 
 
-@pytest.mark.parametrize("rows,vocab,k", [(1, 1, 1), (2, 5, 8), (3, 1000, 64), (4, 4099, 16), (1, 50257, 32), (1030, 700, 3)])
+@pytest.mark.parametrize("rows,vocab,k", [(1, 1, 1), (2, 5, 8), (3, 1000, 64), (4, 4099, 16), (1, 50257, 32), (1030, 700, 3), (2, 70001, 64)])
 @pytest.mark.parametrize("dtype,gtype", [(F32, F32), (F32, BF16), (F16, F16), (BF16, BF16), (BF16, F32)])
 def test_distill(built_lib, gpu, rows, vocab, k, dtype, gtype):
     z, zd = _logits(rows, vocab, dtype, rows + vocab, pad=3)
@@ -224,7 +224,7 @@ def test_distill(built_lib, gpu, rows, vocab, k, dtype, gtype):
         _padding_untouched(zd)
 
 
-@pytest.mark.parametrize("vocab", [900, 20001])
+@pytest.mark.parametrize("vocab", [900, 20001, 70001])
 @pytest.mark.parametrize("tau,alpha", [(1.0, 1.0), (2.0, 0.6), (1.0, 0.5)])
 def test_distill_of_special_entries(built_lib, gpu, vocab, tau, alpha):
     """Absent, repeated and out-of-range entries and targets, a target among the entries, rows of
@@ -289,7 +289,7 @@ def test_distill_of_long_rows(built_lib, gpu, rows, vocab, dtype, gtype, tau, al
     assert bool((err <= 1e-5 + R.HALF_STEP[gtype] * 1.01).all()), err.max()
 
 
-@pytest.mark.parametrize("vocab,copies", [(1003, 1), (40003, 1), (40003, 7)])  # by rows, by parts, long rows
+@pytest.mark.parametrize("vocab,copies", [(1003, 1), (40003, 1), (70001, 1), (40003, 7)])  # (70001: by parts)
 @pytest.mark.parametrize("tau,alpha", [(1.0, 1.0), (2.0, 0.6), (1.5, 0.5)])
 @pytest.mark.parametrize("dtype", [F32, BF16])
 def test_distill_of_special_students(built_lib, gpu, vocab, copies, tau, alpha, dtype):
@@ -329,7 +329,7 @@ def _all_calls(z, t, ids, tl, w, ws, dz, dz2):
     return [s[k] for k in sorted(s)] + [dz2, loss, dz]
 
 
-@pytest.mark.parametrize("rows,vocab", [(3, 30011), (1040, 3001)])
+@pytest.mark.parametrize("rows,vocab", [(3, 30011), (3, 70011), (1040, 3001)])
 def test_streams_graphs_and_repeats_give_the_same_bits(built_lib, gpu, rows, vocab):
     def inputs(seed):
         z, zd = _logits(rows, vocab, BF16, seed)
@@ -371,7 +371,7 @@ def test_streams_graphs_and_repeats_give_the_same_bits(built_lib, gpu, rows, voc
 
 
 @pytest.mark.parametrize("dtype", [F32, F16, BF16])
-@pytest.mark.parametrize("rows,vocab", [(2, 20001), (1040, 1001)])
+@pytest.mark.parametrize("rows,vocab", [(2, 20001), (2, 70001), (1040, 1001)])
 def test_gradients_in_place(built_lib, gpu, dtype, rows, vocab):
     z, zd = _logits(rows, vocab, dtype, 6, pad=3)
     ids, tl, t = (x.to(gpu) for x in _teacher(rows, 9, vocab, 6))
@@ -451,7 +451,7 @@ def test_no_rows(built_lib, gpu):
 def test_guarded_workspaces(built_lib, gpu):
     prev = L.mebp_set_workspace_guards(True)
     try:
-        for rows, vocab in ((2, 30011), (1030, 501)):
+        for rows, vocab in ((2, 30011), (2, 70011), (1030, 501)):
             z, zd = _logits(rows, vocab, F32, 3)
             ids, tl, t = (x.to(gpu) for x in _teacher(rows, 64, vocab, 1))
             D.token_logprobs(zd, t, 64)
