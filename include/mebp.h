@@ -300,8 +300,10 @@ int mebp_token_logprobs(const mebp_logits* z, const int32_t* targets, float temp
  *                  read only with d_entropy)
  *   d_logp, d_entropy  [rows] fp32; either may be NULL (0). targets may be NULL without d_logp
  *   dz   of the logits' rows and vocab, any type and ld. May be the logits themselves (same
- *        data, type and ld), and must not overlap them otherwise
- * A target < 0 gives its row no d_logp term, one >= vocab makes the row NaN. A row whose lse
+ *        data, type and ld); otherwise the two must lie apart, also where rows of one would fit
+ *        between rows of the other
+ * A target < 0 gives its row no d_logp term, one >= vocab makes the row NaN; at a target whose logit
+ * is -inf the gradient is d_logp / tau. A row whose lse
  * is -inf gets zeros. No workspace.                                                        */
 int mebp_token_logprobs_backward(const mebp_logits* z, const int32_t* targets, float temperature, const float* lse,
                                  const float* entropy, const float* d_logp, const float* d_entropy,
@@ -312,9 +314,11 @@ int mebp_token_logprobs_backward(const mebp_logits* z, const int32_t* targets, f
  *   loss = w (alpha tau^2 sum_k p_k (ln p_k - ln q[id_k]) - (1 - alpha) ln q1[target]).
  * The teacher's top log probabilities serve as its logits as well.                         */
 typedef struct {
-  const int32_t* ids;      /* [rows][k] the teacher's token ids; < 0: no entry; an id may     */
-                           /* occur twice (its probabilities add); >= vocab: the row is NaN  */
-  const float* logits;     /* [rows][k]; -inf: no entry; NaN or +inf: the row is NaN         */
+  const int32_t* ids;      /* [rows][k] the teacher's token ids, read if alpha > 0; < 0: no    */
+                           /* entry; an id may occur twice (its probabilities add); >= vocab: */
+                           /* the row is NaN                                                 */
+  const float* logits;     /* [rows][k], read if alpha > 0; -inf: no entry; NaN or +inf: the */
+                           /* row is NaN                                                     */
   const int32_t* targets;  /* [rows] hard labels, read if alpha < 1; < 0: no such term here;  */
                            /* >= vocab: the row is NaN                                      */
   const float* row_weight; /* [rows] w, e.g. 1 / rows for a mean; NULL: 1. A row of weight 0 */
@@ -330,6 +334,8 @@ typedef struct {
  *   row_loss [rows] fp32 (written)
  *   dz       as in mebp_token_logprobs_backward
  * A row without entries has no distillation term, one without a label either loss and gradient 0.
+ * Where the student's logit of an entry or of the label is -inf the loss is +inf, and that column's
+ * gradient is its term of p (of the label) alone.
  * Else a row of nothing but -inf has loss +inf and gradient 0, and a NaN or +inf logit makes a row
  * NaN.                                                                                    */
 int mebp_distill_topk(const mebp_logits* z, const mebp_distill* d, float* row_loss, const mebp_logits* dz, void* ws,
@@ -341,7 +347,7 @@ int mebp_distill_topk(const mebp_logits* z, const mebp_distill* d, float* row_lo
  * operators above on them. Operands and products as in mebp_lm_head_ce_backward: fp16 forward,
  * bf16 backward, fp32 sums. Rows go in blocks, so that the logits and the gradient of a block (fp32
  * and bf16) take at most MEBP_LM_CHUNK_MB (environment, default 512) MiB, or those of 64 rows.
- * x, dx, norm_final 16-byte aligned; dx must not be x. rows = 0 enqueues nothing.          */
+ * x, dx, norm_final 16-byte aligned; dx must not overlap x. rows = 0 enqueues nothing.     */
 
 /* Bytes of workspace for the four calls below (top_k: that of mebp_lm_head_logprobs, else 0).
  * Pure host computation; 0 for an invalid config or shape.                               */

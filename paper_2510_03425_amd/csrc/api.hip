@@ -91,7 +91,8 @@ std::atomic<int> g_guards{[] {
 constexpr size_t kGuardBytes = 256;
 constexpr int kMaxGuards = 2 * S_COUNT;
 
-// Slots of the workspaces of the operators on logits and of the head that runs them; their guards' tags follow the others'.
+// Slots of the workspaces of the operators on logits and of the head that runs them; their guards'
+// tags follow the others'.
 enum OpSlot { OP_STATS, OP_KEYS, OP_PICKED, OP_HF, OP_Z, OP_DZ, OP_DHF, OP_PLANES, OP_ROW_LOSS, OP_COUNT };
 const char* kOpSlotNames[OP_COUNT] = {"logit_stats", "logit_keys", "logit_picked", "head_hf", "head_logits",
                                       "head_dlogits", "head_dhf", "head_planes", "head_row_loss"};
@@ -2126,10 +2127,12 @@ int check_head_logits(const mebp_config* c, int rows, const mebp_logits* z, cons
   return rows ? check_act(z->data, what) : MEBP_OK;
 }
 
-int check_head_grad(const float* x, const float* dx, int rows) {
+int check_head_grad(const mebp_config* c, const float* x, const float* dx, int rows) {
   if (!rows) return MEBP_OK;
   const int e = check_act(dx, "dx");
-  return e ? e : dx == x ? fail(MEBP_EINVAL, "dx must not be x") : MEBP_OK;
+  if (e) return e;
+  const uintptr_t a = (uintptr_t)x, b = (uintptr_t)dx, bytes = (uintptr_t)rows * c->hidden * 4;
+  return a < b + bytes && b < a + bytes ? fail(MEBP_EINVAL, "dx overlaps x") : MEBP_OK;
 }
 
 struct Head {
@@ -2254,7 +2257,7 @@ int mebp_lm_head_logits_backward(const mebp_config* cfg, const mebp_q4* emb, con
                                  mebp_stream_t stream) {
   int e;
   if ((e = check_head(cfg, emb, norm_final, x, rows)) || (e = check_head_logits(cfg, rows, dz, "dz")) ||
-      (e = check_head_grad(x, dx, rows)))
+      (e = check_head_grad(cfg, x, dx, rows)))
     return e;
   if (dz->dtype != MEBP_BF16) return fail(MEBP_EUNSUPPORTED, "dz: dtype not bf16");
   const Head h{cfg, emb, norm_final, head_layout(cfg, rows, 0), ws, (hipStream_t)stream};
@@ -2305,7 +2308,7 @@ int mebp_lm_head_distill_backward(const mebp_config* cfg, const mebp_q4* emb, co
                                   void* ws, size_t ws_bytes, mebp_stream_t stream) {
   int e;
   if ((e = check_head(cfg, emb, norm_final, x, rows)) || (e = check_distill(d, rows, loss)) ||
-      (e = check_head_grad(x, dx, rows)))
+      (e = check_head_grad(cfg, x, dx, rows)))
     return e;
   if (row_loss && !aligned(row_loss, 4)) return fail(MEBP_EINVAL, "row_loss not 4-byte aligned");
   const Head h{cfg, emb, norm_final, head_layout(cfg, rows, 0), ws, (hipStream_t)stream};

@@ -65,6 +65,15 @@ def _on_device(f):
     return g
 
 
+def _on_model_device(f):
+    """Runs a method with the model's device current."""
+    @functools.wraps(f)
+    def g(self, *a, **kw):
+        with torch.cuda.device(self.norm_final.device):
+            return f(self, *a, **kw)
+    return g
+
+
 def logits_struct(z: torch.Tensor, like: Optional[torch.Tensor] = None) -> L.MebpLogits:
     """[rows][vocab] logits (or their gradient, on the device of ``like``) whose columns follow
     one another."""
@@ -298,6 +307,7 @@ class DeviceModel:
             raise L.MebpError(L.MEBP_EINVAL, "invalid shape for the head's workspace")
         return torch.empty(n, dtype=torch.uint8, device=self.device), n
 
+    @_on_model_device
     def lm_head_logits(self, x: torch.Tensor, dtype: torch.dtype = torch.float32) -> torch.Tensor:
         """Logits [rows][vocab] of hidden states x [rows][d] fp32, in fp32 or fp16."""
         rows = x.shape[0]
@@ -307,6 +317,7 @@ class DeviceModel:
                               stream_handle())
         return z
 
+    @_on_model_device
     def lm_head_logits_backward(self, x: torch.Tensor, dz: torch.Tensor) -> torch.Tensor:
         """The gradient w.r.t. x of bf16 gradients w.r.t. its logits."""
         rows = x.shape[0]
@@ -316,6 +327,7 @@ class DeviceModel:
                                        ptr(dx), ptr(ws), nb, stream_handle())
         return dx
 
+    @_on_model_device
     def lm_head_logprobs(self, x: torch.Tensor, targets: Optional[torch.Tensor] = None, top_k: int = 0,
                          temperature: float = 1.0, out: Optional[dict] = None) -> dict:
         """`token_logprobs` of the head's logits of x, which are never held at once."""
@@ -327,6 +339,7 @@ class DeviceModel:
                                 stream_handle())
         return out
 
+    @_on_model_device
     def lm_head_distill(self, x: torch.Tensor, dx: torch.Tensor, ids: torch.Tensor, logits: torch.Tensor,
                         temperature: float = 1.0, alpha: float = 1.0, targets: Optional[torch.Tensor] = None,
                         row_weight: Optional[torch.Tensor] = None, row_loss: Optional[torch.Tensor] = None):
@@ -339,6 +352,7 @@ class DeviceModel:
                                         _operand(dx, torch.float32, (rows, self.cfg.hidden), x, "dx"), ptr(ws), nb,
                                         stream_handle())
 
+    @_on_model_device
     def train_step_distill(self, ids: torch.Tensor, logits: torch.Tensor, temperature: float = 1.0, alpha: float = 1.0,
                            targets: Optional[torch.Tensor] = None, row_weight: Optional[torch.Tensor] = None,
                            row_loss: Optional[torch.Tensor] = None, dx0: Optional[torch.Tensor] = None):

@@ -206,6 +206,9 @@ def test_head_logits_refused(built_lib):
     ok = _hz(dtype=L.MEBP_BF16)
     assert b(_hz()) == L.MEBP_EUNSUPPORTED and b(ok, 0) == L.MEBP_EINVAL and b(ok, DZ + 4) == L.MEBP_EINVAL
     assert b(ok, 0x400000) == L.MEBP_EINVAL and "dx" in L.mebp_last_error()
+    size = 8 * MINI.hidden * 4  # of x, and of dx
+    for at in (0x400000 + size - 16, 0x400000 - size + 16):
+        assert b(ok, at) == L.MEBP_EINVAL and "dx" in L.mebp_last_error()
 
 
 def test_head_operators_refused(built_lib):
