@@ -221,8 +221,8 @@ DEV float target_logit(const ScoreArgs& p, const T* z, size_t row) {
 }
 
 // One workgroup per part of a row; the only part of a row writes its scores, others their
-// statistics and lists for k_scores_join.
-template <class T, bool TOP, int NT>
+// statistics and lists for k_scores_join. U: loads of a lane in flight.
+template <class T, bool TOP, int NT, int U>
 __global__ __launch_bounds__(NT) void k_scores(ScoreArgs p) {
   constexpr int NW = NT / 64, B = TOP ? top_buffer(kVec<T>) : 1;
   __shared__ Acc red[NW];
@@ -236,9 +236,7 @@ __global__ __launch_bounds__(NT) void k_scores(ScoreArgs p) {
   t.start(p.top_k, buf + (threadIdx.x >> 6) * B, share);
   Sums<true, ONE> sums;
   bool begun = false;
-  // loads of a lane in flight: 4 read 151936 fp32 logits of 256 rows in 25 us (2: 31 us); with
-  // alternatives' work beside them 2 are faster (2048 x 262144 bf16, 64 of them: 196 us, 4: 206 us)
-  scan<T, NT, TOP ? 2 : 4, true>(z, v0, v1, [&](const auto& g) {
+  scan<T, NT, U, true>(z, v0, v1, [&](const auto& g) {
     float top = 0.f;
     if (TOP) top = g.top();
     if (!begun) {  // (of every thread: each has a first group)
@@ -338,11 +336,11 @@ __global__ __launch_bounds__(NT) void k_scores_grad(ScoreGradArgs p) {
 // Parts of a row: enough workgroups for the chip where there are few long rows, of no fewer than 4096
 // columns each. The launch that joins them costs more than a workgroup's pass over a short row (call of
 // 8 rows of 50257 fp32 logits 15.0 us by parts and 10.7 whole, with 20 alternatives 15.3 both; of 100000
-// 15.3 and 12.9, 15.2 and 21.7), and from one row for each compute unit on there is nothing to gain
-// (151936 fp32 with 20 alternatives: 192 rows 30 us by parts and 38 whole, 256 rows 37 both).
+// 15.3 and 12.9, 15.2 and 21.7), and so do the parts of many rows together (151936 fp32 logits: 128 rows
+// 19 us by parts and 23 whole, 192 rows 25 and 22; with 20 alternatives 24 and 30, 31 and 29).
 LogitSplit logit_split(int rows, int vocab) {
   LogitSplit s{};
-  const int want = rows >= 256 || vocab <= 65536 ? 1 : std::min(kLogitParts, (1024 + rows - 1) / std::max(rows, 1));
+  const int want = rows >= 160 || vocab <= 65536 ? 1 : std::min(kLogitParts, (1024 + rows - 1) / std::max(rows, 1));
   const int most = (vocab + 4095) / 4096;
   const int n = std::max(1, std::min(want, most));
   s.cols = ((vocab + n - 1) / n + 2047) / 2048 * 2048;
@@ -355,16 +353,22 @@ hipError_t launch_scores(ScoreArgs a, int dtype, hipStream_t st) {
   return by_type(dtype, [&](auto* tp) {
     using T = std::remove_pointer_t<decltype(tp)>;
     const double bytes = (double)a.rows * a.vocab * sizeof(T);
-    auto run = [&](auto top, auto nt) {
-      constexpr int NT = decltype(nt)::value;
+    auto run = [&](auto top, auto nt, auto loads) {
+      constexpr int NT = decltype(nt)::value, U = decltype(loads)::value;
       MEBP_TIMED(st, a.top_k ? "token_scores_top" : "token_scores", 0.0, bytes,
-                 hipLaunchKernelGGL((k_scores<T, decltype(top)::value, NT>), dim3(grid), dim3(NT), 0, st, a));
+                 hipLaunchKernelGGL((k_scores<T, decltype(top)::value, NT, U>), dim3(grid), dim3(NT), 0, st, a));
     };
     const bool wide = a.split.n == 1 && a.vocab > 16384;
-    if (a.top_k)
-      wide ? run(std::true_type(), IC<512>()) : run(std::true_type(), IC<256>());
+    // 4 loads in flight read 151936 fp32 logits of 256 rows in 25 us, 2 in 31. Beside the alternatives'
+    // work 2 are faster where several workgroups share a compute unit (64 of 2048 x 262144 bf16 196 us,
+    // with 4 206; 5 of 800 x 50257 fp16 31 and 35), 4 where a row has one to itself (20 of 256 x 151936
+    // fp32 37 us with 2, 31 with 4; 262144 56 and 47)
+    if (!a.top_k)
+      wide ? run(std::false_type(), IC<512>(), IC<4>()) : run(std::false_type(), IC<256>(), IC<4>());
+    else if (wide && a.rows <= 256)
+      run(std::true_type(), IC<512>(), IC<4>());
     else
-      wide ? run(std::false_type(), IC<512>()) : run(std::false_type(), IC<256>());
+      wide ? run(std::true_type(), IC<512>(), IC<2>()) : run(std::true_type(), IC<256>(), IC<2>());
     if (a.split.n > 1)
       MEBP_TIMED(st, "token_scores_join", 0.0, (double)grid * (16 + 8 * a.top_k),
                  hipLaunchKernelGGL((k_scores_join<T>), dim3(a.rows), dim3(256), 0, st, a));

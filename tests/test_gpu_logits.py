@@ -53,7 +53,7 @@ def _check_scores(z, got, targets, top_k, tau):
 
 SHAPES = [  # rows, vocab, top_k: one column to more than one part of a row
     (1, 1, 1), (1, 2, 5), (3, 7, 64), (2, 63, 3), (5, 255, 64), (4, 1000, 20), (3, 2049, 1), (2, 4096, 8), (2, 4099, 33),
-    (1, 50257, 20), (7, 12289, 64), (1025, 1030, 4), (2, 151936, 64), (3, 65536, 7), (1, 70001, 64), (200, 65537, 2),
+    (1, 50257, 20), (7, 12289, 64), (1025, 1030, 4), (2, 151936, 64), (3, 65536, 7), (1, 70001, 64), (159, 65537, 2), (160, 65537, 2), (256, 17000, 33),
 ]
 
 
