@@ -319,10 +319,11 @@ __global__ __launch_bounds__(NT) void k_scores_grad(ScoreGradArgs p) {
   const float AB = A + B * (p.d_entropy ? p.entropy[row] : 0.f);
   const bool here = t >= v0 && t < v1;
   const float zt = here && threadIdx.x == 0 ? cvt(z[t]) : 0.f;
+  // (q = 0 at logits of -inf, and 0 times -inf is not; the logarithm meets its weight before B, whose
+  // product with it alone may be beyond fp32)
   auto f = [&](float x) {
-    const float lq = x * p.inv_tau - lse;
-    // (q = 0 at logits of -inf)
-    return -exp2_fast(lq * kLog2e) * fmaf(B, fmaxf(lq, -1e30f), AB);
+    const float lq = x * p.inv_tau - lse, q = exp2_fast(lq * kLog2e);
+    return -fmaf(B, q * fmaxf(lq, -1e30f), q * AB);
   };
   if (here) __syncthreads();  // zt is read before any thread writes (the output may be the input)
   map_row<T, G, NT, 4, true>(z, dz, v0, v1, f);
