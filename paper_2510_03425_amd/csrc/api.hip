@@ -2049,6 +2049,7 @@ int mebp_token_logprobs_backward(const mebp_logits* z, const int32_t* targets, f
   a.d_logp = d_logp;
   a.d_entropy = d_entropy;
   a.inv_tau = 1.0f / temperature;
+  a.c = exp2_scale(temperature);
   HIP_TRY(launch_scores_grad(a, z->dtype, dz->dtype, (hipStream_t)stream));
   return MEBP_OK;
 }

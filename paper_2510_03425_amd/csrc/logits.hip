@@ -300,16 +300,32 @@ __global__ __launch_bounds__(256) void k_scores_join(ScoreArgs p) {
 // ------------------------------------------------------------------ gradient
 // d logp_t / dz = (1[t] - q) / tau and dH / dz = -q (ln q + H) / tau, weighted by the gradients of
 // the two; the target's column is written again with its 1.
+//
+// ln q = z / tau - lse, and an fp32 lse is off by 2^-24 of itself: by 2^-18 at kWideLse, by all of ln s
+// for a row of finite mask values such as -1e9. A row whose lse is larger is summed again, and written, by
+// its first part alone (the output may be the input, which its other parts must not write meanwhile):
+// ln q = (z - m) / tau - ln s then (1024 x 151936 bf16 227 us where all rows are such and 111 else; 8 x
+// 151936 fp32 36 and 3.3; with 4 loads in flight 191 and 32, but the registers cost the others 3 %).
+constexpr float kWideLse = 128.f;
+
 template <class T, class G, int NT>
 __global__ __launch_bounds__(NT) void k_scores_grad(ScoreGradArgs p) {
+  __shared__ Acc red[NT / 64];
   const size_t row = blockIdx.x / p.split.n;
   const int part = (int)(blockIdx.x % p.split.n);
   const T* z = (const T*)p.z + row * p.ld;
   G* dz = (G*)p.dz + row * p.ldd;
-  const int v0 = part * p.split.cols, v1 = min(p.vocab, v0 + p.split.cols);
-  const int t = p.targets && p.d_logp ? p.targets[row] : -1;
   const float lse = p.lse[row];
-  if (lse == -INFINITY) {
+  const bool wide = lse != -INFINITY && fabsf(lse) > kWideLse;
+  if (wide && part > 0) return;
+  const int v0 = part * p.split.cols, v1 = wide ? p.vocab : min(p.vocab, v0 + p.split.cols);
+  const int t = p.targets && p.d_logp ? p.targets[row] : -1;
+  Acc a = acc_empty();
+  if (wide) {
+    scan<T, NT, 2, false>(z, 0, p.vocab, [&](const auto& g) { acc_add<false, false>(a, g, p.c, 0.f, 0.f); });
+    acc_block<NT, false, false>(a, p.c, 0.f, red);
+  }
+  if (wide ? a.s == 0.f : lse == -INFINITY) {
     zero_row<G, NT>(dz, v0, v1);
     return;
   }
@@ -321,15 +337,23 @@ __global__ __launch_bounds__(NT) void k_scores_grad(ScoreGradArgs p) {
   const float zt = here && threadIdx.x == 0 ? cvt(z[t]) : 0.f;
   // (q = 0 at logits of -inf, and 0 times -inf is not; the logarithm meets its weight before B, whose
   // product with it alone may be beyond fp32)
-  auto f = [&](float x) {
-    const float lq = x * p.inv_tau - lse, q = exp2_fast(lq * kLog2e);
+  auto grad = [&](float lq) {
+    const float q = exp2_fast(lq * kLog2e);
     return -fmaf(B, q * fmaxf(lq, -1e30f), q * AB);
   };
-  if (here) __syncthreads();  // zt is read before any thread writes (the output may be the input)
-  map_row<T, G, NT, 4, true>(z, dz, v0, v1, f);
-  if (!here) return;
-  stores_done();
-  if (threadIdx.x == 0) dz[t] = to_out<G>(f(zt) + A);
+  auto write = [&](auto&& lq) {
+    if (here) __syncthreads();  // zt is read before any thread writes (the output may be the input)
+    map_row<T, G, NT, 4, true>(z, dz, v0, v1, [&](float x) { return grad(lq(x)); });
+    if (!here) return;
+    stores_done();
+    if (threadIdx.x == 0) dz[t] = to_out<G>(grad(lq(zt)) + A);
+  };
+  if (wide) {
+    const float log_s = logf(a.s);
+    write([&](float x) { return (x - a.m) * p.inv_tau - log_s; });
+  } else {
+    write([&](float x) { return x * p.inv_tau - lse; });
+  }
 }
 
 }  // namespace

@@ -414,7 +414,7 @@ struct ScoreGradArgs {
   int rows, vocab;
   const int32_t* targets;
   const float *lse, *entropy, *d_logp, *d_entropy;
-  float inv_tau;
+  float inv_tau, c;        // 1 / tau, log2(e) / tau
   LogitSplit split;        // n and cols, set by the launcher
 };
 hipError_t launch_scores_grad(ScoreGradArgs a, int dtype, int gtype, hipStream_t st);
