@@ -1917,9 +1917,9 @@ void set_slots(const OpLayout& o, void* ws, LogitSplit* s) {
   s->picked = o.at<float>(ws, OP_PICKED);
 }
 
-// log2(e) / tau, and the rise of a logit in which the largest weight of the call's softmaxes grows 2^6 times
+// log2(e) / tau, and the rise of a logit in which the largest weight of the call's softmaxes doubles
 float exp2_scale(float tau) { return (float)(1.4426950408889634 / (double)tau); }
-float reference_lift(float c, bool unit) { return 6.0f / (unit ? std::max(c, 1.4426950408889634f) : c); }
+float reference_lift(float c, bool unit) { return 1.0f / (unit ? std::max(c, 1.4426950408889634f) : c); }
 
 int check_scores(const int32_t* targets, float tau, int rows, int top_k, const mebp_token_scores* out) {
   int e;

@@ -84,17 +84,12 @@ __global__ __launch_bounds__(NT) void k_distill_stats(DistillArgs p) {
   const T* z = (const T*)p.z + row * p.ld;
   const int v0 = part * p.split.cols, v1 = min(p.vocab, v0 + p.split.cols);
   Sums<false, SM> sums;
-  bool begun = false;
-  scan<T, NT, 4, ONCE>(z, v0, v1, [&](const auto& g) {
-    if (!begun) sums.start(block_max<NT>(g.top(), red), p.c);  // (of every thread: each has a first group)
-    begun = true;
-    sums.add(g);
-  });
-  sums.template join<NT>(red);
-  Acc a = sums.acc();
-  if (!sums.served()) {
+  sums.start(p.c, p.lift);
+  scan<T, NT, 4, ONCE>(z, v0, v1, [&](const auto& g) { sums.template add<4>(g); });
+  Acc a = sums.template join<NT>(red);
+  if (!served<TWO>(a)) {
     a = acc_empty();
-    scan<T, NT, 1, false>(z, v0, v1, [&](const auto& g) { acc_add<false, TWO>(a, g, p.c, kLog2e, p.lift); });
+    scan<T, NT, 1, false>(z, v0, v1, [&](const auto& g) { acc_add<false, TWO>(a, g, p.c, kLog2e); });
     __syncthreads();
     acc_block<NT, false, TWO>(a, p.c, kLog2e, red);
   }
@@ -297,11 +292,7 @@ __global__ __launch_bounds__(WG, 4) void k_distill_row(DistillArgs p) {
     sp = sparse_terms(p, t, target);
   }
   Sums<false, SM> sums;
-  if (steps > 0) {
-    float x[N];
-    unpack<T>(raw[0], x);
-    sums.start(block_max<WG>(max_of(x), red), p.c);
-  }
+  sums.start(p.c, p.lift);
   each<R>([&](auto i) {
     constexpr int r = decltype(i)::value;
     if (r >= steps) return;
@@ -326,19 +317,12 @@ __global__ __launch_bounds__(WG, 4) void k_distill_row(DistillArgs p) {
       sums.add(x);
     }
   }
-  bool begun = steps > 0;
-  if (held < V)
-    scan<T, WG, 2, false>(z, held, V, [&](const auto& h) {
-      if (!begun) sums.start(block_max<WG>(h.top(), red), p.c);
-      begun = true;
-      sums.add(h);
-    });
-  sums.template join<WG>(red);
-  Acc a = sums.acc();
-  const bool served = sums.served();
-  if (!served) {
+  if (held < V) scan<T, WG, 2, false>(z, held, V, [&](const auto& h) { sums.template add<2>(h); });
+  Acc a = sums.template join<WG>(red);
+  const bool first_pass = served<TWO>(a);
+  if (!first_pass) {
     a = acc_empty();
-    scan<T, WG, 1, false>(z, 0, V, [&](const auto& g) { acc_add<false, TWO>(a, g, p.c, kLog2e, p.lift); });
+    scan<T, WG, 1, false>(z, 0, V, [&](const auto& g) { acc_add<false, TWO>(a, g, p.c, kLog2e); });
     __syncthreads();
     acc_block<WG, false, TWO>(a, p.c, kLog2e, red);
   }
@@ -353,15 +337,17 @@ __global__ __launch_bounds__(WG, 4) void k_distill_row(DistillArgs p) {
     return;
   }
   const float m = terms.m, c0 = terms.c0, c1 = terms.c1;
-  if (!served) {
+  if (!first_pass) {
     map_row<T, G, WG, 1, false>(z, dz, 0, V, [&](float x) { return dense_grad<TWO>(x, m, c0, c1, p.c); });
   } else {
-    const float b0 = c0 * sums.unround(), b1 = TWO ? c1 * sums.unround1() : 0.f;
+    // weights at the row's own whole exponent, as Sums has them
+    const float k = whole_exponent(m, p.c), k1 = whole_exponent(m, kLog2e), u = exp2_fast(-fmaf(m, p.c, -k));
+    const float b0 = c0 * u, b1 = !TWO ? 0.f : c1 * (SM == TWO_SQUARE ? u * u : exp2_fast(-fmaf(m, kLog2e, -k1)));
     auto f = [&](float x) {
-      const float e = exp2_fast(fmaf(x, p.c, sums.k));
+      const float e = exp2_fast(fmaf(x, p.c, -k));
       if (SM == ONE) return b0 * e;
       if (SM == TWO_SQUARE) return e * fmaf(b1, e, b0);
-      return fmaf(b1, exp2_fast(fmaf(x, kLog2e, sums.k1)), b0 * e);
+      return fmaf(b1, exp2_fast(fmaf(x, kLog2e, -k1)), b0 * e);
     };
     if (held < V) map_row<T, G, WG, 2, true, true>(z, dz, held, V, f);
     if constexpr (L > 0) {

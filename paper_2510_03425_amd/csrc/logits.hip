@@ -87,7 +87,6 @@ template <int NW>
 struct Top {
   u64 list;    // this lane's key of the sorted list
   float thr;   // only logits above it can be among the first k
-  float most;  // this lane's largest logit
   int cnt, k;  // buffered keys, k (both the same in all lanes)
   int groups;  // seen
   u64* buf;
@@ -95,7 +94,7 @@ struct Top {
 
   __device__ __forceinline__ void start(int top_k, u64* b, uint32_t* sh) {
     list = 0;
-    thr = most = -INFINITY;
+    thr = -INFINITY;
     cnt = groups = 0;
     k = top_k;
     buf = b;
@@ -128,7 +127,8 @@ struct Top {
     cnt += __popcll(mask);
     return true;
   }
-  __device__ __forceinline__ void publish() {
+  // most: this lane's largest logit so far
+  __device__ __forceinline__ void publish(float most) {
     const uint32_t t = lanes_reach(order_bits(most), (k + NW - 1) / NW);
     if (lane_id() == 0) __hip_atomic_store(share + (threadIdx.x >> 6), t, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
   }
@@ -140,12 +140,7 @@ struct Top {
     thr = fmaxf(thr, below(least));
   }
 
-  // top: the group's largest logit. The first group's bounds are published by first(), before a
-  // barrier that every wave has to pass before the second.
-  __device__ __forceinline__ void first(float top) {
-    most = top;
-    publish();
-  }
+  // The first group's bounds are published before a barrier that every wave has to pass before it adds.
   template <int N>
   __device__ __forceinline__ void push(const float (&x)[N], int col) {
 #pragma unroll
@@ -158,12 +153,12 @@ struct Top {
     const uint32_t kth = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(list >> 32), k - 1);
     if (kth) thr = fmaxf(thr, order_value(kth));
   }
-  // a group, vector by vector: the buffer takes one more where it holds less than 64 keys
+  // a group (top: its largest logit), vector by vector: the buffer takes one more where it holds less than
+  // 64 keys
   template <int U, int N>
-  __device__ __forceinline__ void add(const Group<U, N>& g, float top) {
-    most = fmaxf(most, top);
+  __device__ __forceinline__ void add(const Group<U, N>& g, float top, float most) {
     const int seen = ++groups;
-    if (seen > 2 && (seen & (seen - 1)) == 0) publish();
+    if (seen > 2 && (seen & (seen - 1)) == 0) publish(most);
     if (!__any(top > thr)) return;
     shared_threshold();
     if (!__any(top > thr)) return;
@@ -235,24 +230,23 @@ __global__ __launch_bounds__(NT) void k_scores(ScoreArgs p) {
   Top<NW> t;
   t.start(p.top_k, buf + (threadIdx.x >> 6) * B, share);
   Sums<true, ONE> sums;
+  sums.start(p.c, p.lift);
   bool begun = false;
   scan<T, NT, U, true>(z, v0, v1, [&](const auto& g) {
-    float top = 0.f;
-    if (TOP) top = g.top();
-    if (!begun) {  // (of every thread: each has a first group)
-      if constexpr (TOP) t.first(top);
-      // (the first vector's, so that the sums are the same bits with and without alternatives)
-      sums.start(block_max<NT>(max_of(g.x[0]), red), p.c);
-      begun = true;
+    const float top = sums.template add<2>(g);
+    if constexpr (TOP) {
+      if (!begun) {  // (of every thread: each has a first group)
+        t.publish(sums.most);
+        __syncthreads();
+        begun = true;
+      }
+      t.add(g, top, sums.most);
     }
-    sums.add(g);
-    if constexpr (TOP) t.add(g, top);
   });
-  sums.template join<NT>(red);
-  Acc a = sums.acc();
-  if (!sums.served()) {
+  Acc a = sums.template join<NT>(red);
+  if (!served<false>(a)) {
     a = acc_empty();
-    scan<T, NT, 1, false>(z, v0, v1, [&](const auto& g) { acc_add<true, false>(a, g, p.c, 0.f, p.lift); });
+    scan<T, NT, 1, false>(z, v0, v1, [&](const auto& g) { acc_add<true, false>(a, g, p.c, 0.f); });
     __syncthreads();
     acc_block<NT, true, false>(a, p.c, 0.f, red);
   }
@@ -322,7 +316,7 @@ __global__ __launch_bounds__(NT) void k_scores_grad(ScoreGradArgs p) {
   const int t = p.targets && p.d_logp ? p.targets[row] : -1;
   Acc a = acc_empty();
   if (wide) {
-    scan<T, NT, 2, false>(z, 0, p.vocab, [&](const auto& g) { acc_add<false, false>(a, g, p.c, 0.f, 0.f); });
+    scan<T, NT, 2, false>(z, 0, p.vocab, [&](const auto& g) { acc_add<false, false>(a, g, p.c, 0.f); });
     acc_block<NT, false, false>(a, p.c, 0.f, red);
   }
   if (wide ? a.s == 0.f : lse == -INFINITY) {

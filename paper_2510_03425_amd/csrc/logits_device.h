@@ -187,13 +187,12 @@ struct Group {
   }
 };
 
-// Adds a group, one lane's reference following its own largest logit: it moves where a logit lies
-// above it by `lift`, 2^6 times its weight. fp32 holds the sums nearly as well with a stale one, and
-// few groups move it. NaN and +inf logits make s NaN: exp(NaN), and exp(inf - inf).
+// Adds a group, one lane's reference following its own largest logit. NaN and +inf logits make s NaN:
+// exp(NaN), and exp(inf - inf).
 template <bool ENT, bool TWO, int U, int N>
-DEV void acc_add(Acc& a, const Group<U, N>& g, float c, float c1, float lift) {
+DEV void acc_add(Acc& a, const Group<U, N>& g, float c, float c1) {
   const float top = g.top();
-  if (top > a.m + lift) acc_move<ENT, TWO>(a, top, c, c1);
+  if (top > a.m) acc_move<ENT, TWO>(a, top, c, c1);
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     if (u >= g.n) break;
@@ -249,43 +248,74 @@ DEV Acc join_parts(const LogitSplit& sp, size_t row, float c, float c1) {
   return a;
 }
 
-// ------------------------------------------------------------------ sums at one reference
-// The sums of a whole workgroup at one reference m, the largest logit of its first group: a weight is
-// then exp2(z c + k) with k = -m c rounded, two instructions instead of three and no maximum to keep,
-// and lanes and waves join by addition. k's rounding r = m c + k scales all weights alike and is taken
-// out at the end. fp32's exponents leave room for logits above m; where one lies 2^40 times its weight
-// above, and z c + k rounds the exponent by more than 2^-19 (or sums are not finite: NaN and +inf
-// logits), or m is nothing to go by (no logit above -inf in the first group, or of the size of the
-// type's lowest value), served() is false and the caller sums again with acc_add, a reference for each
-// lane.
+// ------------------------------------------------------------------ sums at a wave's reference
+// The sums of a wave at one reference, 2^k: a weight is then exp2(z c - k), two instructions, and k, a
+// whole number, costs no bits, as the difference is rounded once and a move to another k is a scaling by a
+// power of two. k follows the wave's largest logit: it moves where one lies above the last by `lift`, twice
+// its weight, so that no weight is above 2^1.5 and the largest are the most precise. That happens a few times
+// in a row (for logits in no order, as often as the logarithm of the number of steps).
+//
+// What leaves the wave is relative to its largest logit itself, whose weight is divided out as it was added:
+// s >= 1, w <= 0, so that no log probability is above 0 and no entropy below. k = inf, which makes all
+// weights 0, where no logit was above -inf yet and where k would have no whole numbers left (logits of 2^23
+// temperatures and more, of the size of the type's lowest value among them, and +inf). A wave that ends there
+// has s NaN, as one with a NaN logit, and the caller sums again with acc_add: served().
 enum Softmaxes { ONE, TWO_EXP, TWO_SQUARE };  // at tau alone; also at 1; the same where tau is 2:
                                               // exp(z) is then exp(z / 2)^2
+// the reference of a largest logit m
+DEV float whole_exponent(float m, float c) {
+  const float k = rintf(m * c);
+  return fabsf(k) < 0x1p23f ? k : INFINITY;
+}
+// what the weights at one reference are at another
+DEV float rescaling(float from, float to) { return from == INFINITY ? 0.f : exp2_fast(from - to); }
+
 template <bool ENT, Softmaxes SM>
 struct Sums {
-  float m, c, k, k1;
-  float s, w, s1;
+  float c, lift;
+  float k, k1;      // the references at tau and at 1 (TWO_EXP)
+  float over;       // a logit above it moves them
+  float most;       // this lane's largest logit
+  float s, w, s1;   // w: weighted by z c - k
 
-  __device__ __forceinline__ void start(float ref, float scale) {
-    m = fabsf(ref) < 1e30f ? ref : 0.f;
+  __device__ __forceinline__ void start(float scale, float rise) {
     c = scale;
-    k = -(m * c);
-    k1 = -(m * kLog2e);
-    s = fabsf(ref) < 1e30f ? 0.f : NAN;
-    w = s1 = 0.f;
+    lift = rise;
+    s = w = s1 = 0.f;
+    k = k1 = INFINITY;
+    over = most = -INFINITY;
+  }
+  // top: this lane's largest logit among those that are added next
+  __device__ __forceinline__ void meet(float top) {
+    most = fmaxf(most, top);
+    if (!__any(top > over)) return;
+    const float m = __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, max64(most))));
+    const float to = whole_exponent(m, c), f = rescaling(k, to);
+    // (f = 0 leaves nothing, and k - to times s may be far beyond)
+    if (ENT) w = f > 0.f ? f * fmaf(k - to, s, w) : 0.f;
+    s *= f;
+    if (SM == TWO_SQUARE) s1 *= f * f;
+    if (SM == TWO_EXP) {
+      const float to1 = whole_exponent(m, kLog2e);
+      s1 *= rescaling(k1, to1);
+      k1 = to1;
+    }
+    k = to;
+    over = m + lift;
   }
   template <int N>
-  __device__ __forceinline__ void add(const float (&x)[N]) {
+  __device__ __forceinline__ void add_met(const float (&x)[N]) {
     // a vector by itself first, which leaves a lane an 8th (4th) of the additions in a row
     float vs = 0.f, vw = 0.f, v1 = 0.f;
 #pragma unroll
     for (int j = 0; j < N; ++j) {
-      const float a = fmaf(x[j], c, k), e = exp2_fast(a);
+      const float a = fmaf(x[j], c, -k), e = exp2_fast(a);
       vs = j ? vs + e : e;
       // (a logit of -inf has weight 0, and 0 times -inf is not)
       if (ENT) vw = j ? fmaf(e, fmaxf(a, -1e30f), vw) : e * fmaxf(a, -1e30f);
       if (SM == TWO_SQUARE) v1 = j ? fmaf(e, e, v1) : e * e;
       if (SM == TWO_EXP) {
-        const float e1 = exp2_fast(fmaf(x[j], kLog2e, k1));
+        const float e1 = exp2_fast(fmaf(x[j], kLog2e, -k1));
         v1 = j ? v1 + e1 : e1;
       }
     }
@@ -293,52 +323,55 @@ struct Sums {
     if (ENT) w += vw;
     if (SM != ONE) s1 += v1;
   }
-  template <int U, int N>
-  __device__ __forceinline__ void add(const Group<U, N>& g) {
+  template <int N>
+  __device__ __forceinline__ void add(const float (&x)[N]) {
+    meet(max_of(x));
+    add_met(x);
+  }
+  // STEP vectors at a time, which groups of other sizes then give the same bits. Returns this lane's largest
+  // logit of them all (NaN where all are).
+  template <int STEP, int U, int N>
+  __device__ __forceinline__ float add(const Group<U, N>& g) {
+    float all = 0.f;
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (u >= g.n) break;
-      add(g.x[u]);
+    for (int u0 = 0; u0 < U; u0 += STEP) {
+      if (u0 >= g.n) break;
+      float top = max_of(g.x[u0]);
+#pragma unroll
+      for (int u = u0 + 1; u < u0 + STEP; ++u)
+        if (u < g.n) top = fmaxf(top, max_of(g.x[u]));
+      meet(top);
+#pragma unroll
+      for (int u = u0; u < u0 + STEP; ++u)
+        if (u < g.n) add_met(g.x[u]);
+      all = u0 ? fmaxf(all, top) : top;
     }
+    return all;
   }
   // over the workgroup, for every thread
   template <int NT>
-  __device__ __forceinline__ void join(Acc* lds) {
-    s = sum64(s);
-    if (ENT) w = sum64(w);
-    if (SM != ONE) s1 = sum64(s1);
-    if (lane_id() == 0) lds[threadIdx.x >> 6] = Acc{0.f, s, w, s1};
+  __device__ __forceinline__ Acc join(Acc* lds) const {
+    Acc a = acc_empty();
+    if (over > -INFINITY) {  // (alike in all lanes; else all logits were -inf or NaN)
+      a.m = max64(most);
+      const float at = fmaf(a.m, c, -k), e = exp2_fast(at), sum = sum64(s);
+      a.s = sum / e;
+      if (ENT) a.w = fminf(fmaf(-at, sum, sum64(w)) / (e * c), 0.f);
+      if (SM == TWO_SQUARE) a.s1 = sum64(s1) / (e * e);
+      if (SM == TWO_EXP) a.s1 = sum64(s1) / exp2_fast(fmaf(a.m, kLog2e, -k1));
+    } else {
+      a.s = sum64(s);
+    }
+    if (lane_id() == 0) lds[threadIdx.x >> 6] = a;
     __syncthreads();
-    const Acc a = lane_id() < NT / 64 ? lds[lane_id()] : Acc{0.f, 0.f, 0.f, 0.f};
-    s = sum64(a.s);
-    if (ENT) w = sum64(a.w);
-    if (SM != ONE) s1 = sum64(a.s1);
-  }
-  __device__ __forceinline__ bool served() const {
-    return s > 0.f && s < 1e12f && (!ENT || fabsf(w) < 1e37f) && (SM == ONE || (s1 > 0.f && s1 < 1e37f));
-  }
-  // exp(k's rounding) at tau and at 1
-  __device__ __forceinline__ float unround() const { return exp2_fast(-fmaf(m, c, k)); }
-  __device__ __forceinline__ float unround1() const {
-    return SM == TWO_SQUARE ? unround() * unround() : exp2_fast(-fmaf(m, kLog2e, k1));
-  }
-  __device__ __forceinline__ Acc acc() const {
-    const float u = unround();
-    Acc a{m, s * u, 0.f, SM == ONE ? 0.f : s1 * unround1()};
-    if (ENT) a.w = (w - fmaf(m, c, k) * s) * u / c;
+    a = lane_id() < NT / 64 ? lds[lane_id()] : acc_empty();
+    acc_wave<ENT, SM != ONE>(a, c, kLog2e);
     return a;
   }
 };
-
-// the largest value of the workgroup
-template <int NT>
-DEV float block_max(float v, Acc* lds) {
-  v = max64(v);
-  if (lane_id() == 0) lds[threadIdx.x >> 6].m = v;
-  __syncthreads();
-  v = max64(lane_id() < NT / 64 ? lds[lane_id()].m : -INFINITY);
-  __syncthreads();
-  return v;
+template <bool TWO>
+DEV bool served(const Acc& a) {
+  return a.s == a.s && (!TWO || a.s1 == a.s1);
 }
 
 // Hands columns v0 .. v1 of a row to add(group), -inf in the place of columns behind the end; columns
