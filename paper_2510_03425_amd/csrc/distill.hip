@@ -26,7 +26,7 @@ DEV Teacher teacher_row(const DistillArgs& a, size_t row) {
   float v = -INFINITY;
   if (l < a.k && a.alpha > 0.f) {
     t.id = a.ids[row * a.k + l];
-    v = a.logits[row * a.k + l] * a.inv_tau;
+    v = a.logits[row * a.k + l];
     if (t.id < 0 || v == -INFINITY) {
       t.id = -1;
       v = -INFINITY;
@@ -34,11 +34,12 @@ DEV Teacher teacher_row(const DistillArgs& a, size_t row) {
   }
   t.any = __any(t.id >= 0);
   if (!t.any) return t;
-  float M = max64(v);
-  const float e = v == -INFINITY ? 0.f : exp2_fast((v - M) * kLog2e);
+  // (the difference first: a quotient by tau may leave fp32, and has fewer bits below its point)
+  const float d = (v - max64(v)) * a.inv_tau;
+  const float e = v == -INFINITY ? 0.f : exp2_fast(d * kLog2e);
   const float S = sum64(e);
   t.p = e / S;
-  t.lp = (v - M) - logf(S);
+  t.lp = d - logf(S);
   if (t.id >= a.vocab) t.p = NAN;
   return t;
 }
