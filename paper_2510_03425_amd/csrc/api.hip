@@ -1984,11 +1984,13 @@ DistillArgs distill_args(const mebp_logits& z, const mebp_distill& d, float* row
   a.logits = d.logits;
   a.targets = d.targets;
   a.weight = d.row_weight;
-  a.tau = d.temperature;
-  a.inv_tau = 1.0f / d.temperature;
+  // (hard labels alone: the softmax at 1 is the only one)
+  const float tau = d.alpha > 0.f ? d.temperature : 1.f;
+  a.tau = tau;
+  a.inv_tau = 1.0f / tau;
   a.alpha = d.alpha;
-  a.c = exp2_scale(d.temperature);
-  a.lift = reference_lift(a.c, d.alpha < 1.f && d.temperature != 1.f);
+  a.c = exp2_scale(tau);
+  a.lift = reference_lift(a.c, d.alpha < 1.f && tau != 1.f);
   a.loss = row_loss;
   a.split = s;
   return a;

@@ -99,3 +99,24 @@ def test_students_at_the_lowest_value(built_lib, gpu, dtype, copies, vocab, tau,
         s = slice(i, i + 1)
         for got in (loss, only):
             _close(z[s], ids[s], tl[s], t[s], tau, alpha, got[last][s], dz[last][s], f"row {i}")
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows,vocab", [(3, 1003), (3, 70001), (97, 40003), (97, 151936)])
+def test_hard_labels_alone_know_no_temperature(built_lib, gpu, dtype, rows, vocab):
+    """At alpha 0 no softmax at tau is part of the loss: every temperature gives the same bits."""
+    say("hard labels alone", rows, vocab, dtype)
+    z = (torch.randn((rows, vocab), generator=torch.Generator().manual_seed(rows)) * 3).to(dtype)
+    z[1, : vocab // 2] = -INF
+    ids, tl, t = (x.to(gpu) for x in _teacher(rows, 3, vocab, 5))
+    t[1] = vocab - 1
+    zd, got = z.to(gpu), []
+    for tau in (1.0, 1e-6, 0.3, 2.0, 1e6):
+        dz = torch.empty_like(zd)
+        loss = D.distill_topk(zd, ids, tl, None, dz, tau, 0.0, t)
+        only = D.distill_topk(zd, ids, tl, None, None, tau, 0.0, t)
+        got.append((loss, only, dz))
+    for other in got[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(got[0], other))
+    want = torch.logsumexp(zd.double(), 1) - zd.double().gather(1, t.long()[:, None])[:, 0]
+    assert float((got[0][0].double() - want).abs().max()) <= 1e-4
