@@ -1943,7 +1943,7 @@ int check_distill(const mebp_distill* d, int rows, const float* row_loss) {
   if ((e = check_temperature(d->temperature))) return e;
   if (!(d->alpha >= 0.f && d->alpha <= 1.f)) return fail(MEBP_EINVAL, "alpha %g not in [0, 1]", d->alpha);
   if (d->k < 1 || d->k > kMaxTop) return fail(MEBP_EUNSUPPORTED, "k %d not in [1, %d]", d->k, kMaxTop);
-  if ((e = check_words(d->ids, rows, "ids")) || (e = check_words(d->logits, rows, "teacher logits"))) return e;
+  if (d->alpha > 0.f && ((e = check_words(d->ids, rows, "ids")) || (e = check_words(d->logits, rows, "teacher logits")))) return e;
   if (d->alpha < 1.f && (e = check_words(d->targets, rows, "targets"))) return e;
   if (d->row_weight && (e = check_words(d->row_weight, rows, "row_weight"))) return e;
   return check_words(row_loss, rows, "row_loss");
@@ -2207,8 +2207,8 @@ struct Head {
     float* rl = row_loss ? row_loss : h.o.at<float>(ws, OP_ROW_LOSS);
     const int e = blocks(rows, [&](int r0, int n) {
       mebp_distill q = p;
-      q.ids += (size_t)r0 * p.k;
-      q.logits += (size_t)r0 * p.k;
+      if (q.ids) q.ids += (size_t)r0 * p.k;
+      if (q.logits) q.logits += (size_t)r0 * p.k;
       if (q.targets) q.targets += r0;
       if (q.row_weight) q.row_weight += r0;
       const mebp_logits z = block(OP_Z, n, MEBP_F32), dz = block(OP_DZ, n, MEBP_BF16);

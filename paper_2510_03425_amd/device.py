@@ -122,7 +122,7 @@ def _scores(z: torch.Tensor, n: int, targets, top_k: int, out: Optional[dict]):
 
 
 def _distill(z: torch.Tensor, n: int, ids, logits, temperature, alpha, targets, row_weight) -> L.MebpDistill:
-    k = ids.shape[-1]
+    k = 1 if ids is None else ids.shape[-1]
     return L.MebpDistill(_operand(ids, torch.int32, (n, k), z, "ids"), _operand(logits, torch.float32, (n, k), z, "logits"),
                          _operand(targets, torch.int32, (n,), z, "targets"),
                          _operand(row_weight, torch.float32, (n,), z, "row_weight"), k, temperature, alpha)
@@ -162,12 +162,12 @@ def token_logprobs_backward(z: torch.Tensor, targets: Optional[torch.Tensor], ls
 
 
 @_on_device
-def distill_topk(z: torch.Tensor, ids: torch.Tensor, logits: torch.Tensor, row_loss: Optional[torch.Tensor] = None,
+def distill_topk(z: torch.Tensor, ids: Optional[torch.Tensor], logits: Optional[torch.Tensor], row_loss: Optional[torch.Tensor] = None,
                  dz: Optional[torch.Tensor] = None, temperature: float = 1.0, alpha: float = 1.0,
                  targets: Optional[torch.Tensor] = None, row_weight: Optional[torch.Tensor] = None,
                  ws: Optional[torch.Tensor] = None) -> torch.Tensor:
     """``mebp_distill_topk``: the loss of each row against a teacher's int32 ``ids`` and fp32
-    ``logits`` [rows][k], and its gradient into ``dz`` where that is given."""
+    ``logits`` [rows][k] (None: hard labels alone, alpha 0), and its gradient into ``dz`` where that is given."""
     n = z.shape[0]
     if row_loss is None:
         row_loss = torch.empty(n, dtype=torch.float32, device=z.device)
@@ -340,7 +340,7 @@ class DeviceModel:
         return out
 
     @_on_model_device
-    def lm_head_distill(self, x: torch.Tensor, dx: torch.Tensor, ids: torch.Tensor, logits: torch.Tensor,
+    def lm_head_distill(self, x: torch.Tensor, dx: torch.Tensor, ids: Optional[torch.Tensor], logits: Optional[torch.Tensor],
                         temperature: float = 1.0, alpha: float = 1.0, targets: Optional[torch.Tensor] = None,
                         row_weight: Optional[torch.Tensor] = None, row_loss: Optional[torch.Tensor] = None):
         """Loss (into self.loss) and gradient of distilling the head's logits of x (`distill_topk`)."""
@@ -353,8 +353,8 @@ class DeviceModel:
                                         stream_handle())
 
     @_on_model_device
-    def train_step_distill(self, ids: torch.Tensor, logits: torch.Tensor, temperature: float = 1.0, alpha: float = 1.0,
-                           targets: Optional[torch.Tensor] = None, row_weight: Optional[torch.Tensor] = None,
+    def train_step_distill(self, ids: Optional[torch.Tensor], logits: Optional[torch.Tensor], temperature: float = 1.0,
+                           alpha: float = 1.0, targets: Optional[torch.Tensor] = None, row_weight: Optional[torch.Tensor] = None,
                            row_loss: Optional[torch.Tensor] = None, dx0: Optional[torch.Tensor] = None):
         """`train_step` against a teacher's int32 ids and fp32 logits [N][k]; its workspace is made by
         the first such step."""

@@ -7,6 +7,7 @@ import torch
 
 import logits_ref as R
 from gpu_util import say
+from mebp_inputs import MINI, make_inputs
 from paper_2510_03425_amd import device as D
 
 pytestmark = pytest.mark.gpu
@@ -120,3 +121,23 @@ def test_hard_labels_alone_know_no_temperature(built_lib, gpu, dtype, rows, voca
         assert all(torch.equal(a, b) for a, b in zip(got[0], other))
     want = torch.logsumexp(zd.double(), 1) - zd.double().gather(1, t.long()[:, None])[:, 0]
     assert float((got[0][0].double() - want).abs().max()) <= 1e-4
+
+
+def test_hard_labels_alone_need_no_entries(built_lib, gpu):
+    z = torch.randn((5, 3001), generator=torch.Generator().manual_seed(1)).to(gpu)
+    ids, tl, t = (x.to(gpu) for x in _teacher(5, 4, 3001, 2))
+    a, b = torch.empty_like(z), torch.empty_like(z)
+    want = D.distill_topk(z, ids, tl, None, a, 1.0, 0.0, t)
+    assert torch.equal(D.distill_topk(z, None, None, None, b, 1.0, 0.0, t), want) and torch.equal(a, b)
+    # on the head, in more than one block of rows
+    cfg = MINI.with_(name="entries", n_layers=1, hidden=128, n_heads=1, n_kv_heads=1, head_dim=128, ffn=192, vocab=50304,
+                     batch=1, seq=64)
+    dm = D.DeviceModel(make_inputs(cfg, seed=3, norm="random"), device=str(gpu))
+    rows = 1700
+    x = torch.randn((rows, 128), generator=torch.Generator().manual_seed(4)).to(gpu)
+    ids, tl, t = (v.to(gpu) for v in _teacher(rows, 4, cfg.vocab, 5))
+    a, b = torch.empty_like(x), torch.empty_like(x)
+    dm.lm_head_distill(x, a, ids, tl, 1.0, 0.0, t)
+    loss = dm.loss.clone()
+    dm.lm_head_distill(x, b, None, None, 1.0, 0.0, t)
+    assert torch.equal(loss, dm.loss) and torch.equal(a, b)
