@@ -2097,12 +2097,15 @@ HeadLayout head_layout(const mebp_config* c, int rows, int top_k) {
   h.o.place(OP_STATS, parts * sizeof(float4));
   h.o.place(OP_KEYS, parts * top_k * 8);
   h.o.place(OP_PICKED, (size_t)r * (kMaxTop + 1) * 4);
-  h.o.place(OP_HF, (size_t)r * d * 2);
-  h.o.place(OP_Z, (size_t)r * V * 4);
-  h.o.place(OP_DZ, (size_t)r * V * 2);
-  h.o.place(OP_DHF, (size_t)r * d * 4);
+  // In the order of their use: the final norm (read by the logits' product) lies where the gradient is written
+  // afterwards, the gradient's product and its planes where the logits were.
   h.plane_floats = (size_t)lm_q4_splits(r, d, V) * r * d;
-  h.o.place(OP_PLANES, h.plane_floats * 4);
+  const size_t dhf = ((size_t)r * d * 4 + 255) & ~(size_t)255;
+  h.o.place(OP_Z, std::max((size_t)r * V * 4, dhf + h.plane_floats * 4));
+  h.o.place(OP_DZ, std::max((size_t)r * V * 2, (size_t)r * d * 2));
+  h.o.off[OP_HF] = h.o.off[OP_DZ];
+  h.o.off[OP_DHF] = h.o.off[OP_Z];
+  h.o.off[OP_PLANES] = h.o.off[OP_Z] + dhf;
   h.o.place(OP_ROW_LOSS, (size_t)rows * 4);
   h.o.done();
   return h;
