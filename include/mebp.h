@@ -381,7 +381,8 @@ int mebp_lm_head_distill_backward(const mebp_config* cfg, const mebp_q4* emb, co
 /* mebp_train_step with mebp_lm_head_distill_backward as its final block: row n = b*T + t of `d` is
  * position t of sequence b (its entries and its target are of the token that follows there, and its
  * weight makes the sum a mean); T may be 1. Other arguments as in mebp_train_step; the workspace is
- * the larger one of mebp_distill_step_workspace_bytes.                                    */
+ * that of mebp_distill_step_workspace_bytes: mebp_workspace_bytes where a block of the head's logits fits where
+ * mebp_train_step has its own or its copy of the table (many tokens), and the head's added to it else. */
 size_t mebp_distill_step_workspace_bytes(const mebp_config* cfg, int32_t B, int32_t T);
 int mebp_train_step_distill(const mebp_config* cfg, const mebp_q4* emb, const mebp_layer_base* layers,
                             const float* norm_final, const mebp_layer_lora* lora, const int32_t* ids, int32_t B,

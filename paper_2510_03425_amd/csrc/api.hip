@@ -124,6 +124,9 @@ struct Layout {
   Frag frag;
   bool lm_frag;
   int frag_slot;
+  // the larger one of the slots that the cross-entropy alone uses while the final block of a training
+  // step runs (its logits, its copy of the weights)
+  size_t idle_off, idle_bytes;
 };
 
 // Split planes of a forward product on the kernels of gemm_mid.hip (where the reduction is one of
@@ -412,6 +415,9 @@ bool make_layout(const mebp_config* c, int B, int T, Layout* L, bool static_call
   };
   for (int i = 0; i < S_COUNT; ++i) L->off[i] = place(i, 0);
   for (int i = 0; i < S_COUNT; ++i) L->off1[i] = per_set(i) && !static_call ? place(i, 1) : L->off[i];
+  const int idle = sz[S_W16] > sz[S_LOGITS] ? S_W16 : S_LOGITS;
+  L->idle_off = L->off[idle];
+  L->idle_bytes = lm ? sz[idle] : 0;
   L->status_off = o;
   if (L->guards) o += 256;
   L->total = o;
@@ -2111,6 +2117,22 @@ HeadLayout head_layout(const mebp_config* c, int rows, int top_k) {
   return h;
 }
 
+// A distillation step's: the step's own, in whose idle slot the head's lies where it fits there (the layers use
+// none of it between the forward loop and the end of the final block), behind it else.
+struct DistillStepLayout {
+  HeadLayout head;
+  size_t head_off, total;
+};
+DistillStepLayout distill_step_layout(const mebp_config* c, int B, int T) {
+  Layout L;
+  make_layout(c, B, T, &L);
+  DistillStepLayout s{head_layout(c, B * T, 0), 0, 0};
+  const bool fits = s.head.o.L.total <= L.idle_bytes;
+  s.head_off = fits ? L.idle_off : L.total;
+  s.total = L.total + (fits ? 0 : s.head.o.L.total);
+  return s;
+}
+
 int check_head(const mebp_config* c, const mebp_q4* emb, const float* norm_final, const float* x, int rows) {
   int e;
   if ((e = check_config(c))) return e;
@@ -2324,9 +2346,8 @@ int mebp_lm_head_distill_backward(const mebp_config* cfg, const mebp_q4* emb, co
 }
 
 size_t mebp_distill_step_workspace_bytes(const mebp_config* cfg, int32_t B, int32_t T) {
-  const size_t step = mebp_workspace_bytes(cfg, B, T);
-  const size_t head = step ? mebp_head_workspace_bytes(cfg, B * T, 0) : 0;
-  return head ? step + head : 0;
+  if (!mebp_workspace_bytes(cfg, B, T) || !mebp_head_workspace_bytes(cfg, B * T, 0)) return 0;
+  return distill_step_layout(cfg, B, T).total;
 }
 
 int mebp_train_step_distill(const mebp_config* cfg, const mebp_q4* emb, const mebp_layer_base* layers,
@@ -2340,19 +2361,16 @@ int mebp_train_step_distill(const mebp_config* cfg, const mebp_q4* emb, const me
       (e = check_distill(d, B * T, loss)))
     return e;
   if (row_loss && !aligned(row_loss, 4)) return fail(MEBP_EINVAL, "row_loss not 4-byte aligned");
-  // the step's own layout, then the head's
-  const size_t step = mebp_workspace_bytes(cfg, B, T), need = mebp_distill_step_workspace_bytes(cfg, B, T);
-  if (ws_bytes < need) return fail(MEBP_EWORKSPACE, "workspace %zu bytes < required %zu", ws_bytes, need);
-  void* head_ws = (char*)ws + step;
-  const HeadLayout hl = head_layout(cfg, B * T, 0);
+  const DistillStepLayout s = distill_step_layout(cfg, B, T);
+  if (ws_bytes < s.total) return fail(MEBP_EWORKSPACE, "workspace %zu bytes < required %zu", ws_bytes, s.total);
   auto block = [&](const Ctx& x, const float* x_last, float* g, bf16* gb, bool hf_ready) {
-    const Head h{cfg, emb, norm_final, hl, head_ws, x.st};
-    return h.distill(x_last, hf_ready ? xs<f16>(x, S_HF) : nullptr, x.D.N, *d, loss, row_loss, g, gb);
+    const Head h{cfg, emb, norm_final, s.head, (char*)ws + s.head_off, x.st};
+    return guarded(h.h.o, h.ws, x.st, [&] {
+      return h.distill(x_last, hf_ready ? xs<f16>(x, S_HF) : nullptr, x.D.N, *d, loss, row_loss, g, gb);
+    });
   };
   return guarded(cfg, B, T, ws, stream, [&] {
-    return guarded(hl.o, head_ws, stream, [&] {
-      return train_step_impl(cfg, emb, layers, norm_final, lora, ids, B, T, ckpt, nullptr, block, grads, dx0, ws, stream);
-    });
+    return train_step_impl(cfg, emb, layers, norm_final, lora, ids, B, T, ckpt, nullptr, block, grads, dx0, ws, stream);
   });
 }
 

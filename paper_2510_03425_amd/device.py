@@ -356,19 +356,22 @@ class DeviceModel:
     def train_step_distill(self, ids: Optional[torch.Tensor], logits: Optional[torch.Tensor], temperature: float = 1.0,
                            alpha: float = 1.0, targets: Optional[torch.Tensor] = None, row_weight: Optional[torch.Tensor] = None,
                            row_loss: Optional[torch.Tensor] = None, dx0: Optional[torch.Tensor] = None):
-        """`train_step` against a teacher's int32 ids and fp32 logits [N][k]; its workspace is made by
-        the first such step."""
+        """`train_step` against a teacher's int32 ids and fp32 logits [N][k], in the model's workspace where
+        that is large enough (as it is for many tokens), else in one that the first such step makes."""
         if self.L == 0:
             raise ValueError("this input set has no layers")
         ck = self.alloc_ckpt()
         d = _distill(ck, self.N, ids, logits, temperature, alpha, targets, row_weight)
         need = L.mebp_distill_step_workspace_bytes(self.ccfg, self.B, self.T)
-        if self.distill_ws is None or self.distill_ws.numel() < need:
-            self.distill_ws = torch.empty(need, dtype=torch.uint8, device=self.device)
+        ws = self.ws
+        if need > self.ws_bytes:
+            if self.distill_ws is None or self.distill_ws.numel() < need:
+                self.distill_ws = torch.empty(need, dtype=torch.uint8, device=self.device)
+            ws = self.distill_ws
         L.mebp_train_step_distill(self.ccfg, self.emb, self.base, ptr(self.norm_final), self.lora, ptr(self.ids), self.B,
                                   self.T, d, ptr(ck), ptr(self.loss),
                                   _operand(row_loss, torch.float32, (self.N,), ck, "row_loss"), self.grads, ptr(dx0),
-                                  ptr(self.distill_ws), self.distill_ws.numel(), stream_handle())
+                                  ptr(ws), ws.numel(), stream_handle())
 
     def _x(self, x: torch.Tensor) -> int:
         return _operand(x, torch.float32, (x.shape[0], self.cfg.hidden), self.norm_final, "x")
