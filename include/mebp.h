@@ -348,14 +348,15 @@ int mebp_distill_topk(const mebp_logits* z, const mebp_distill* d, float* row_lo
  * operators above on them. Operands and products as in mebp_lm_head_ce_backward: fp16 forward,
  * bf16 backward, fp32 sums. Rows go in blocks, so that the logits and the gradient of a block (fp32
  * and bf16) take at most MEBP_LM_CHUNK_MB (environment, default 512) MiB, or those of 64 rows.
- * x, dx, norm_final 16-byte aligned; dx must not overlap x. rows = 0 enqueues nothing.     */
+ * Vocabularies below 2^20, tables up to 4 GiB. x, dx, norm_final 16-byte aligned; dx must not
+ * overlap x. rows = 0 enqueues nothing.                                                   */
 
 /* Bytes of workspace for the four calls below (top_k: that of mebp_lm_head_logprobs, else 0).
  * Pure host computation; 0 for an invalid config or shape.                               */
 size_t mebp_head_workspace_bytes(const mebp_config* cfg, int32_t rows, int32_t top_k);
 
 /* The logits themselves: z of `rows` rows and cfg->vocab columns, MEBP_F32 or MEBP_F16 (rounded to
- * it), ld a multiple of 8 below 2^20 (a block's rows times ld below 2^29), data 16-byte aligned
+ * it), ld a multiple of 8 below 2^20 (a block's rows times ld below 2^31), data 16-byte aligned
  * (written).                                                                             */
 int mebp_lm_head_logits(const mebp_config* cfg, const mebp_q4* emb, const float* norm_final, const float* x,
                         int32_t rows, const mebp_logits* z, void* ws, size_t ws_bytes, mebp_stream_t stream);

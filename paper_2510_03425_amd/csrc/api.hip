@@ -2082,11 +2082,23 @@ int mebp_distill_topk(const mebp_logits* z, const mebp_distill* d, float* row_lo
 
 namespace {
 // ------------------------------------------------------------------ the head's logits
-// Rows of a block: fp32 logits and bf16 gradients within the budget of the fused head's chunks.
+// Rows of a block: fp32 logits and bf16 gradients within the budget of the fused head's chunks, and fewer than
+// 2^30 logits whatever the budget (the products address them from each tile's first row and have no such
+// limit; matrices of more than twice that, of a caller's pitch, are refused as no test has them).
+constexpr size_t kHeadBlock = (size_t)1 << 30;
 int head_block_rows(int rows, int V) {
-  const size_t r = lm_chunk_budget() / ((size_t)V * 6);
+  const size_t r = std::min(lm_chunk_budget() / 6, kHeadBlock - 1) / V;
   const int n = (int)std::min<size_t>(r >= 256 ? r / 256 * 256 : std::max<size_t>(r / 64 * 64, 64), 1 << 16);
   return std::max(1, std::min(rows, n));
+}
+
+// The products address the rows of a tile (256 at most) and the int4 table with 32 bits.
+constexpr int kHeadColumns = 1 << 20;
+int check_head_vocab(const mebp_config* c) {
+  if (c->vocab <= 0) return fail(MEBP_EINVAL, "vocab must be > 0 for the LM head");
+  if (c->vocab >= kHeadColumns || (size_t)c->vocab * c->hidden / 2 > 0xffffffffu)
+    return fail(MEBP_EUNSUPPORTED, "vocab %d of width %d: not below 2^20, or a table above 4 GiB", c->vocab, c->hidden);
+  return MEBP_OK;
 }
 
 struct HeadLayout {
@@ -2136,8 +2148,7 @@ DistillStepLayout distill_step_layout(const mebp_config* c, int B, int T) {
 int check_head(const mebp_config* c, const mebp_q4* emb, const float* norm_final, const float* x, int rows) {
   int e;
   if ((e = check_config(c))) return e;
-  if (c->vocab <= 0) return fail(MEBP_EINVAL, "vocab must be > 0 for the LM head");
-  if ((e = check_logits_shape(rows, c->vocab, 0)) || (e = check_q4(emb, "embedding")) ||
+  if ((e = check_head_vocab(c)) || (e = check_logits_shape(rows, c->vocab, 0)) || (e = check_q4(emb, "embedding")) ||
       (e = check_act(norm_final, "norm_final")))
     return e;
   return rows ? check_act(x, "x") : MEBP_OK;
@@ -2148,9 +2159,8 @@ int check_head_logits(const mebp_config* c, int rows, const mebp_logits* z, cons
   int e;
   if ((e = check_logits(z, what))) return e;
   if (z->rows != rows || z->vocab != c->vocab) return fail(MEBP_EINVAL, "%s: not of %d rows and the config's vocab", what, rows);
-  if (z->ld % 8 || z->ld >= (1 << 20)) return fail(MEBP_EUNSUPPORTED, "%s: ld %lld not a multiple of 8 below 2^20", what, (long long)z->ld);
-  // (the products address a block with 32 bits)
-  if (z->ld * head_block_rows(rows, c->vocab) >= (1 << 29))
+  if (z->ld % 8 || z->ld >= kHeadColumns) return fail(MEBP_EUNSUPPORTED, "%s: ld %lld not a multiple of 8 below 2^20", what, (long long)z->ld);
+  if ((size_t)z->ld * head_block_rows(rows, c->vocab) >= 2 * kHeadBlock)
     return fail(MEBP_EUNSUPPORTED, "%s: ld %lld too large for blocks of %d rows", what, (long long)z->ld, head_block_rows(rows, c->vocab));
   return rows ? check_act(z->data, what) : MEBP_OK;
 }
@@ -2255,7 +2265,7 @@ extern "C" {
 
 size_t mebp_head_workspace_bytes(const mebp_config* cfg, int32_t rows, int32_t top_k) {
   std::string saved = g_last_error;
-  if (check_config(cfg) || check_logits_shape(rows, cfg->vocab, top_k)) {
+  if (check_config(cfg) || check_head_vocab(cfg) || check_logits_shape(rows, cfg->vocab, top_k)) {
     g_last_error = saved;
     return 0;
   }
@@ -2357,7 +2367,7 @@ int mebp_train_step_distill(const mebp_config* cfg, const mebp_q4* emb, const me
                             mebp_stream_t stream) {
   int e;
   if ((e = check_train_args(cfg, emb, layers, norm_final, lora, ids, B, T, loss, grads, dx0, ws, ws_bytes, false)) ||
-      (e = check_act(ckpt, "ckpt")) || (e = check_logits_shape(B * T, cfg->vocab, 0)) ||
+      (e = check_act(ckpt, "ckpt")) || (e = check_head_vocab(cfg)) || (e = check_logits_shape(B * T, cfg->vocab, 0)) ||
       (e = check_distill(d, B * T, loss)))
     return e;
   if (row_loss && !aligned(row_loss, 4)) return fail(MEBP_EINVAL, "row_loss not 4-byte aligned");
