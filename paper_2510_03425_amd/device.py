@@ -30,10 +30,15 @@ def make_config(cfg: Config) -> L.MebpConfig:
         lora_alpha=cfg.lora_alpha, lora_mask=cfg.lora_mask(), arch=cfg.arch_flags)
 
 
+# the handle alone: a torch.cuda.Stream of it takes 2.6 us to make (no public name: absent in other builds of torch)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def stream_handle() -> int:
-    """torch's current stream on the current device (its handle alone: a torch.cuda.Stream of it
-    takes 2.6 us to make)."""
-    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+    """torch's current stream on the current device."""
+    if _raw_stream is None:
+        return torch.cuda.current_stream().cuda_stream
+    return _raw_stream(torch.cuda.current_device())
 
 
 def _dev(a: np.ndarray, device) -> torch.Tensor:
