@@ -255,7 +255,8 @@ int mebp_layer_recompute_backward_static(const mebp_config* cfg, int32_t layer, 
  * What is trained on, or read off, a matrix of logits z [rows][vocab] beside the fused
  * next-token loss above. Numbers per row are fp32, sums are fp32; a temperature tau divides
  * the logits first. Logits of -inf are columns masked off: probability 0, gradient 0.
- * All calls take rows = 0 (nothing is enqueued).                                          */
+ * All calls take rows = 0 (nothing is enqueued). What a call writes lies apart from what it
+ * reads, but for a gradient in place of its logits.                                        */
 
 /* Element type of a matrix of logits or of their gradient. */
 enum { MEBP_F32 = 0, MEBP_F16 = 1, MEBP_BF16 = 2 };

@@ -1874,16 +1874,33 @@ int check_logits(const mebp_logits* z, const char* what) {
   return MEBP_OK;
 }
 
+// Memory that a call reads or writes; nothing where it is not given.
+struct Span {
+  const void* p;
+  size_t bytes;
+  const char* what;
+};
+Span span(const mebp_logits* m, const char* what) {
+  if (!m || !m->rows) return Span{nullptr, 0, what};
+  return Span{m->data, ((size_t)(m->rows - 1) * m->ld + m->vocab) * logit_size(m->dtype), what};
+}
+Span words(const void* p, size_t n, const char* what) { return Span{p, 4 * n, what}; }
+
+// Other rows' workgroups may read `others` after one has written to `out`.
+int check_apart(const Span& out, std::initializer_list<Span> others) {
+  for (const Span& o : others) {
+    const uintptr_t a = (uintptr_t)out.p, b = (uintptr_t)o.p;
+    if (a && b && a < b + o.bytes && b < a + out.bytes) return fail(MEBP_EINVAL, "%s overlaps %s", out.what, o.what);
+  }
+  return MEBP_OK;
+}
+
 int check_grad_logits(const mebp_logits* z, const mebp_logits* dz) {
   int e;
   if ((e = check_logits(dz, "dz"))) return e;
   if (dz->rows != z->rows || dz->vocab != z->vocab) return fail(MEBP_EINVAL, "dz: not of the logits' rows and vocab");
   if (!z->rows || (dz->data == z->data && dz->ld == z->ld && dz->dtype == z->dtype)) return MEBP_OK;
-  auto bytes = [](const mebp_logits* m) { return ((size_t)(m->rows - 1) * m->ld + m->vocab) * logit_size(m->dtype); };
-  const uintptr_t a = (uintptr_t)z->data, b = (uintptr_t)dz->data;
-  if (a < b + bytes(dz) && b < a + bytes(z))
-    return fail(MEBP_EINVAL, "dz overlaps the logits without being them (same data, ld and dtype)");
-  return MEBP_OK;
+  return check_apart(span(dz, "dz"), {span(z, "the logits without being them (same data, ld and dtype)")});
 }
 
 // operands of 4 bytes for each of `rows` rows, or for each of their entries
@@ -1927,20 +1944,32 @@ void set_slots(const OpLayout& o, void* ws, LogitSplit* s) {
 float exp2_scale(float tau) { return (float)(1.4426950408889634 / (double)tau); }
 float reference_lift(float c, bool unit) { return 1.0f / (unit ? std::max(c, 1.4426950408889634f) : c); }
 
-int check_scores(const int32_t* targets, float tau, int rows, int top_k, const mebp_token_scores* out) {
+// z: the logits, or the hidden states that they are made of
+int check_scores(const int32_t* targets, float tau, int rows, int top_k, const mebp_token_scores* out, const Span& z) {
   int e;
   if ((e = check_temperature(tau))) return e;
   if (!out) return fail(MEBP_EINVAL, "out is NULL");
   if (out->logp && (e = check_words(targets, rows, "targets"))) return e;
-  const void* p[5] = {out->logp, out->lse, out->entropy, out->top_ids, out->top_logp};
+  const size_t n = rows, nk = n * top_k;
+  const Span p[5] = {words(out->logp, n, "logp"), words(out->lse, n, "lse"), words(out->entropy, n, "entropy"),
+                     words(out->top_ids, nk, "top_ids"), words(out->top_logp, nk, "top_logp")};
   bool any = false;
-  for (const void* q : p) {
-    any |= q != nullptr;
-    if (q && !aligned(q, 4)) return fail(MEBP_EINVAL, "an output is not 4-byte aligned");
+  for (const Span& q : p) {
+    any |= q.p != nullptr;
+    if (!aligned(q.p, 4)) return fail(MEBP_EINVAL, "an output is not 4-byte aligned");
   }
   if (!any && rows) return fail(MEBP_EINVAL, "no output requested");
   if (!top_k && (out->top_ids || out->top_logp)) return fail(MEBP_EINVAL, "top_ids or top_logp with top_k 0");
+  for (const Span& q : p)
+    if ((e = check_apart(q, {z, words(out->logp ? targets : nullptr, n, "targets")}))) return e;
   return MEBP_OK;
+}
+
+// an output of a distillation lies apart from its operands
+int check_distill_apart(const mebp_distill* d, int rows, const Span& out) {
+  const size_t n = rows, nk = d->alpha > 0.f ? n * d->k : 0;
+  return check_apart(out, {words(d->ids, nk, "ids"), words(d->logits, nk, "the teacher's logits"),
+                           words(d->targets, d->alpha < 1.f ? n : 0, "targets"), words(d->row_weight, n, "row_weight")});
 }
 
 int check_distill(const mebp_distill* d, int rows, const float* row_loss) {
@@ -2019,7 +2048,7 @@ int mebp_token_logprobs(const mebp_logits* z, const int32_t* targets, float temp
                         const mebp_token_scores* out, void* ws, size_t ws_bytes, mebp_stream_t stream) {
   int e;
   if ((e = check_logits(z, "logits")) || (e = check_logits_shape(z->rows, z->vocab, top_k)) ||
-      (e = check_scores(targets, temperature, z->rows, top_k, out)))
+      (e = check_scores(targets, temperature, z->rows, top_k, out, span(z, "the logits"))))
     return e;
   LogitSplit s;
   const OpLayout o = logits_layout(z->rows, z->vocab, top_k, &s);
@@ -2043,6 +2072,11 @@ int mebp_token_logprobs_backward(const mebp_logits* z, const int32_t* targets, f
   if (rows && !d_logp && !d_entropy) return fail(MEBP_EINVAL, "neither d_logp nor d_entropy");
   if (d_logp && ((e = check_words(d_logp, rows, "d_logp")) || (e = check_words(targets, rows, "targets")))) return e;
   if (d_entropy && ((e = check_words(d_entropy, rows, "d_entropy")) || (e = check_words(entropy, rows, "entropy")))) return e;
+  const size_t n = rows;
+  if ((e = check_apart(span(dz, "dz"), {words(d_logp ? targets : nullptr, n, "targets"), words(lse, n, "lse"),
+                                        words(d_entropy ? entropy : nullptr, n, "entropy"), words(d_logp, n, "d_logp"),
+                                        words(d_entropy, n, "d_entropy")})))
+    return e;
   if (!z->rows) return MEBP_OK;
   ScoreGradArgs a{};
   a.z = z->data;
@@ -2066,6 +2100,10 @@ int mebp_distill_topk(const mebp_logits* z, const mebp_distill* d, float* row_lo
                       size_t ws_bytes, mebp_stream_t stream) {
   int e;
   if ((e = check_logits(z, "logits")) || (e = check_distill(d, z->rows, row_loss)) || (dz && (e = check_grad_logits(z, dz))))
+    return e;
+  const Span rl = words(row_loss, z->rows, "row_loss"), gz = span(dz, "dz");
+  if ((e = check_apart(rl, {span(z, "the logits"), gz})) || (e = check_distill_apart(d, z->rows, rl)) ||
+      (e = check_distill_apart(d, z->rows, gz)))
     return e;
   LogitSplit s;
   const OpLayout o = logits_layout(z->rows, z->vocab, 0, &s);
@@ -2317,7 +2355,7 @@ int mebp_lm_head_logprobs(const mebp_config* cfg, const mebp_q4* emb, const floa
                           const mebp_token_scores* out, void* ws, size_t ws_bytes, mebp_stream_t stream) {
   int e;
   if ((e = check_head(cfg, emb, norm_final, x, rows)) || (e = check_logits_shape(rows, cfg->vocab, top_k)) ||
-      (e = check_scores(targets, temperature, rows, top_k, out)))
+      (e = check_scores(targets, temperature, rows, top_k, out, words(x, (size_t)rows * cfg->hidden, "x"))))
     return e;
   const Head h{cfg, emb, norm_final, head_layout(cfg, rows, top_k), ws, (hipStream_t)stream};
   if ((e = check_op_ws(h.h.o, ws, ws_bytes))) return e;
@@ -2349,6 +2387,11 @@ int mebp_lm_head_distill_backward(const mebp_config* cfg, const mebp_q4* emb, co
       (e = check_head_grad(cfg, x, dx, rows)))
     return e;
   if (row_loss && !aligned(row_loss, 4)) return fail(MEBP_EINVAL, "row_loss not 4-byte aligned");
+  // (a block's outputs are written before the next one's operands are read)
+  const size_t nx = (size_t)rows * cfg->hidden;
+  const Span rl = words(row_loss, rows, "row_loss"), gx = words(dx, nx, "dx");
+  if ((e = check_apart(rl, {words(x, nx, "x"), gx})) || (e = check_distill_apart(d, rows, rl)) || (e = check_distill_apart(d, rows, gx)))
+    return e;
   const Head h{cfg, emb, norm_final, head_layout(cfg, rows, 0), ws, (hipStream_t)stream};
   if ((e = check_op_ws(h.h.o, ws, ws_bytes))) return e;
   if (!rows) return MEBP_OK;
@@ -2371,6 +2414,7 @@ int mebp_train_step_distill(const mebp_config* cfg, const mebp_q4* emb, const me
       (e = check_distill(d, B * T, loss)))
     return e;
   if (row_loss && !aligned(row_loss, 4)) return fail(MEBP_EINVAL, "row_loss not 4-byte aligned");
+  if ((e = check_distill_apart(d, B * T, words(row_loss, (size_t)B * T, "row_loss")))) return e;
   const DistillStepLayout s = distill_step_layout(cfg, B, T);
   if (ws_bytes < s.total) return fail(MEBP_EWORKSPACE, "workspace %zu bytes < required %zu", ws_bytes, s.total);
   auto block = [&](const Ctx& x, const float* x_last, float* g, bf16* gb, bool hf_ready) {
