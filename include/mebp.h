@@ -304,9 +304,10 @@ int mebp_token_logprobs(const mebp_logits* z, const int32_t* targets, float temp
  *        data, type and ld); otherwise the two must lie apart, also where rows of one would fit
  *        between rows of the other
  * A target < 0 gives its row no d_logp term, one >= vocab makes the row NaN; at a target whose logit
- * is -inf the gradient is d_logp / tau. A row whose lse is -inf gets zeros (whatever its target). Beyond
- * 128 in magnitude an fp32 lse has too few bits for q: such a row's sum is taken anew, in a pass of its
- * own (rows masked by a finite value, small temperatures). No workspace.                   */
+ * is -inf the gradient is d_logp / tau. A row whose lse is -inf gets zeros, whatever its target
+ * (nothing but -inf, or logits whose quotients by tau are below fp32's lowest); a NaN or +inf logit
+ * makes its row NaN. Beyond 128 in magnitude an fp32 lse has too few bits for q: such a row's sum is
+ * taken anew, in a pass of its own (rows masked by a finite value, small temperatures). No workspace. */
 int mebp_token_logprobs_backward(const mebp_logits* z, const int32_t* targets, float temperature, const float* lse,
                                  const float* entropy, const float* d_logp, const float* d_entropy,
                                  const mebp_logits* dz, mebp_stream_t stream);

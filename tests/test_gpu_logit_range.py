@@ -114,3 +114,34 @@ def test_wide_rows_by_parts_and_beside_ordinary_ones(built_lib, gpu):
         assert float((got - want).abs().max()) <= 2 ** -14  # (q of at most 1, 40 logits apart)
         assert bool((got.sum(1).abs() <= 2 ** -13).all())
     assert bool((buf[:, vocab:] == 7.0).all())
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("vocab", [1003, 40003])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_gradient_of_rows_without_a_softmax(built_lib, gpu, dtype, vocab, in_place):
+    """A NaN or +inf logit makes its row NaN, masked columns and all; a row of nothing but -inf is 0; the rows
+    beside them are their own."""
+    z = torch.randn((6, vocab), generator=torch.Generator().manual_seed(8)).to(dtype)
+    z[1, vocab - 1], z[2, 5], z[3], z[4, 7] = float("nan"), INF, -INF, -INF
+    z[1, 3:9] = -INF
+    t = torch.tensor([1, 2, 5, 0, 7, -1], dtype=torch.int32)
+    zd = z.to(gpu)
+    s = D.token_logprobs(zd, t.to(gpu))
+    one = torch.ones(6, device=gpu)
+    dz = zd if in_place else torch.empty_like(zd)
+    D.token_logprobs_backward(zd, t.to(gpu), s["lse"], s["entropy"], one, one, dz)
+    got = dz.double().cpu()
+    assert bool(torch.isnan(got[1:3]).all()) and bool((got[3] == 0).all())
+    # the label on a masked column: 1 there, as the header has it
+    for r, hot in ((0, 1.0), (4, 1.0), (5, 0.0)):
+        lq = torch.log_softmax(z[r].double(), 0)
+        q = lq.exp()
+        h = torch.special.entr(q)
+        want = torch.zeros(vocab, dtype=torch.float64)
+        if hot:
+            want[t[r]] = 1.0
+        want = want - hot * q + h - q * h.sum()
+        # (a lane's additions as above; fp32 numbers of the row)
+        R.close(got[r], want, (vocab / 1024 + 200) * EPS * (q * (2 + (-lq).clamp_max(104) + h.sum())) + 2 ** -18 * q
+                + R.HALF_STEP[dtype] * 1.001 * want.abs() + 2.0 ** -126 * 128 + R.TINY[dtype], f"row {r}")
