@@ -412,7 +412,8 @@ hipError_t launch_distill(DistillArgs a, int dtype, int gtype, hipStream_t st) {
     // as much of a row in registers as leaves none to spill: two exponentials' sums take more of them
     constexpr int R = SM == TWO_EXP ? 16 : 18;
     // few long rows go by parts, in two launches; from 96 of 151936 fp32 logits on a workgroup for each
-    // row is faster (64 rows 25 us by rows and 21 by parts, 96: 27 and 28, 192: 33 and 51)
+    // row is faster (64 rows 23 us by rows and 19 by parts, 96: 24 and 27, 192: 31 and 49; bf16 22 and 17, 22
+    // and 22, 25 and 37). Of 70000 .. 262144 fp32 and bf16 logits the two meet at 65 to 110 rows
     if (a.split.n > 1 && a.rows < 96 && row > R * 512 * 16) {
       stats(tp, sm, std::false_type(), IC<NT>());
       MEBP_TIMED(st, inplace ? "distill_grad_inplace" : "distill_grad", 0.0, both,

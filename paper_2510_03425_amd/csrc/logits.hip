@@ -356,7 +356,9 @@ __global__ __launch_bounds__(NT) void k_scores_grad(ScoreGradArgs p) {
 // columns each. The launch that joins them costs more than a workgroup's pass over a short row (call of
 // 8 rows of 50257 fp32 logits 15.0 us by parts and 10.7 whole, with 20 alternatives 15.3 both; of 100000
 // 15.3 and 12.9, 15.2 and 21.7), and so do the parts of many rows together (151936 fp32 logits: 128 rows
-// 19 us by parts and 23 whole, 192 rows 25 and 22; with 20 alternatives 24 and 30, 31 and 29).
+// 16 us by parts and 19 whole, 192 rows 23 and 21; with 20 alternatives 23 and 27, 29 and 29; bf16 128 rows 13
+// and 14, 192 17 and 14). Of 70000 .. 262144 fp32 and bf16 logits the two meet at 110 to 160 rows, with
+// alternatives at 110 to 260, and 160 costs no more than a fifth at any of them.
 LogitSplit logit_split(int rows, int vocab) {
   LogitSplit s{};
   const int want = rows >= 160 || vocab <= 65536 ? 1 : std::min(kLogitParts, (1024 + rows - 1) / std::max(rows, 1));
@@ -378,10 +380,10 @@ hipError_t launch_scores(ScoreArgs a, int dtype, hipStream_t st) {
                  hipLaunchKernelGGL((k_scores<T, decltype(top)::value, NT, U>), dim3(grid), dim3(NT), 0, st, a));
     };
     const bool wide = a.split.n == 1 && a.vocab > 16384;
-    // 4 loads in flight read 151936 fp32 logits of 256 rows in 25 us, 2 in 31. Beside the alternatives'
-    // work 2 are faster where several workgroups share a compute unit (64 of 2048 x 262144 bf16 196 us,
-    // with 4 206; 5 of 800 x 50257 fp16 31 and 35), 4 where a row has one to itself (20 of 256 x 151936
-    // fp32 37 us with 2, 31 with 4; 262144 56 and 47)
+    // 4 loads in flight read 151936 fp32 logits of 256 rows in 26 us, 2 in 31. Beside the alternatives'
+    // work 2 are faster where several workgroups share a compute unit (64 of 2048 x 262144 bf16 199 us,
+    // with 4 213; 5 of 800 x 50257 fp16 30 and 34, of 333 18 and 20), 4 where a row has one to itself (20 of
+    // 256 x 151936 fp32 37 us with 2, 32 with 4; 262144 57 and 47)
     if (!a.top_k)
       wide ? run(std::false_type(), IC<512>(), IC<4>()) : run(std::false_type(), IC<256>(), IC<4>());
     else if (wide && a.rows <= 256)
