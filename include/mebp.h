@@ -315,7 +315,8 @@ int mebp_token_logprobs_backward(const mebp_logits* z, const int32_t* targets, f
 /* What a student's logits are distilled from. Per row, with p = softmax(logits / tau) over
  * its entries, q = softmax(z / tau) and q1 = softmax(z) over the whole vocabulary:
  *   loss = w (alpha tau^2 sum_k p_k (ln p_k - ln q[id_k]) - (1 - alpha) ln q1[target]).
- * The teacher's top log probabilities serve as its logits as well.                         */
+ * The teacher's top log probabilities serve as its logits as well. What alpha leaves unread may be
+ * NULL; at alpha 0 the temperature changes nothing.                                        */
 typedef struct {
   const int32_t* ids;      /* [rows][k] the teacher's token ids, read if alpha > 0; < 0: no    */
                            /* entry; an id may occur twice (its probabilities add); >= vocab: */

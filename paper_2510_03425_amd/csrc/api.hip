@@ -1890,7 +1890,7 @@ Span words(const void* p, size_t n, const char* what) { return Span{p, 4 * n, wh
 int check_apart(const Span& out, std::initializer_list<Span> others) {
   for (const Span& o : others) {
     const uintptr_t a = (uintptr_t)out.p, b = (uintptr_t)o.p;
-    if (a && b && a < b + o.bytes && b < a + out.bytes) return fail(MEBP_EINVAL, "%s overlaps %s", out.what, o.what);
+    if (a && b && o.bytes && a < b + o.bytes && b < a + out.bytes) return fail(MEBP_EINVAL, "%s overlaps %s", out.what, o.what);
   }
   return MEBP_OK;
 }

@@ -43,7 +43,8 @@ def test_calls_that_lie_apart_are_taken(built_lib):
     assert _scores(logp=T + 4 * ROWS, lse=T + 8 * ROWS) == L.MEBP_EWORKSPACE
     assert _distill(targets=T, row_weight=T, logits=T) == L.MEBP_EWORKSPACE
     assert _distill(loss=T, alpha=0.0) == L.MEBP_EWORKSPACE and _distill(loss=B, alpha=1.0) == L.MEBP_EWORKSPACE
-    assert _scores(logp=0, lse=T) == L.MEBP_EWORKSPACE
+    assert _distill(loss=T - 8, alpha=0.0) == L.MEBP_EWORKSPACE and _distill(loss=B - 8, alpha=1.0) == L.MEBP_EWORKSPACE
+    assert _scores(logp=0, lse=T) == L.MEBP_EWORKSPACE and _scores(logp=0, lse=T - 8) == L.MEBP_EWORKSPACE
     assert _distill(dz=Z) == L.MEBP_EWORKSPACE  # in place
 
 
