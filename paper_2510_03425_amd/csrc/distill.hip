@@ -53,10 +53,11 @@ DEV float distill_loss(const DistillArgs& a, const Acc& st, const Teacher& t, fl
   const bool empty = st.s == 0.f;
   float loss = 0.f;
   if (t.any) {
-    // an entry whose probability rounds to 0 adds nothing
-    const float term = t.id < 0 || t.p == 0.f ? 0.f : t.p * (t.lp - (zk - st.m) * a.inv_tau);
+    // tau times the term (a distance of the size of the type's lowest value may be no number in
+    // temperatures, and is one times p); an entry whose probability rounds to 0 adds nothing
+    const float term = t.id < 0 || t.p == 0.f ? 0.f : t.p * (t.lp * a.tau) - t.p * (zk - st.m);
     const float mass = sum64(t.id < 0 ? 0.f : t.p);
-    loss = empty ? INFINITY : a.alpha * a.tau * a.tau * (sum64(term) + mass * logf(st.s));
+    loss = empty ? INFINITY : a.alpha * a.tau * (sum64(term) + mass * logf(st.s) * a.tau);
   }
   if (target >= 0) {
     const float ce = target >= a.vocab ? NAN : empty ? INFINITY : logf(two ? st.s1 : st.s) - (zt - st.m);

@@ -141,3 +141,21 @@ def test_hard_labels_alone_need_no_entries(built_lib, gpu):
     loss = dm.loss.clone()
     dm.lm_head_distill(x, b, None, None, 1.0, 0.0, t)
     assert torch.equal(loss, dm.loss) and torch.equal(a, b)
+
+
+@pytest.mark.parametrize("tau", [0.02, 0.5, 1.0, 1.7])
+@pytest.mark.parametrize("vocab", [1003, 70001])
+def test_an_unlikely_entry_at_a_students_lowest_value(built_lib, gpu, tau, vocab):
+    """Its term is alpha tau p times the distance, a number of fp32 where the distance in temperatures is none."""
+    tau = float(torch.tensor(tau, dtype=F32))
+    z = torch.randn((3, vocab), generator=torch.Generator().manual_seed(1))
+    ids, tl, t = _teacher(3, 4, vocab, 2)
+    z[torch.arange(3), ids[:, 0].long()] = torch.finfo(F32).min
+    tl[:, 0] = tl[:, 1:].amin(1) - torch.tensor([5.0, 20.0, 60.0]) * tau
+    zd, dz = z.to(gpu), torch.empty((3, vocab), device=gpu)
+    loss = D.distill_topk(zd, ids.to(gpu), tl.to(gpu), None, dz, tau, 1.0)
+    only = D.distill_topk(zd, ids.to(gpu), tl.to(gpu), None, None, tau, 1.0)
+    torch.cuda.synchronize()
+    assert bool(torch.isfinite(loss).all())
+    for got in (loss, only):
+        _close(z, ids, tl, t, tau, 1.0, got, dz, f"{tau}")
