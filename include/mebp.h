@@ -394,6 +394,127 @@ int mebp_train_step_distill(const mebp_config* cfg, const mebp_q4* emb, const me
                             const mebp_layer_lora_grad* grads, float* dx0, void* ws, size_t ws_bytes,
                             mebp_stream_t stream);
 
+/* ---------------- a forward pass over a cache ------------------------------------------
+ * What a trained model answers with: rotary positions by themselves, a paged cache of keys and values
+ * in 8 bits, attention of new tokens over it, and a layer's forward pass with them in the place of
+ * mebp_layer_forward_ckpt's attention. Numbers of sequences, lengths and pages are read on the
+ * device, so that a captured call serves as they change. rows = 0 and tokens = 0 enqueue nothing. */
+
+/* Heads of some tokens (queries, keys, values or their gradients). */
+typedef struct {
+  void* data;        /* element e of head h of token n at n * ld + h * head_ld + e, aligned to its size */
+  int64_t ld;        /* elements from one token to the next, 0 .. 2^32                      */
+  int64_t head_ld;   /* from one head to the next. Of outputs no two elements share a place */
+  int32_t tokens;    /* 0 .. 2^24                                                           */
+  int32_t heads;     /* 1 .. 1024                                                           */
+  int32_t dim;       /* 1 .. 1024                                                           */
+  int32_t dtype;     /* MEBP_F32, MEBP_F16 or MEBP_BF16                                     */
+} mebp_heads;
+
+/* Rotary positions: (cos, sin) of every position and pair, which a program keeps. */
+typedef struct {
+  float* table;      /* [n_pos][rot / 2][2] fp32, 8-byte aligned                            */
+  int32_t rot;       /* the first `rot` elements of a head turn, the others stay: even, >= 2 */
+  int32_t n_pos;     /* positions 0 .. n_pos - 1, up to 2^28                                */
+  int32_t interleaved; /* pairs are 0: elements (j, j + rot / 2), 1: (2 j, 2 j + 1)         */
+} mebp_rope;
+
+/* Its frequencies, f_j = theta^(-2 j / rot) where nothing is scaled. */
+typedef struct {
+  float theta;
+  float factor;      /* s >= 1 by which a context is longer: f_j / s, or by parts            */
+  int32_t original;  /* 0: every frequency. Else by parts: the length of the original context. A pair that */
+                     /* turns r = original f_j / 2 pi times in it gets f_j (g + (1 - g) / s),  */
+  float low, high;   /* g = clamp((r - low) / (high - low), 0, 1); 0 <= low < high            */
+  float gain;        /* cos and sin are multiplied by this (1: a rotation)                   */
+} mebp_rope_scaling;
+
+/* Fills rope->table (written): gain (cos, sin)(p f_j), angles in 64 bits, rounded to fp32. */
+int mebp_rope_positions(const mebp_rope* rope, const mebp_rope_scaling* scaling, mebp_stream_t stream);
+
+/* y = x with its pairs turned: y_a = x_a cos - x_b sin, y_b = x_b cos + x_a sin; in fp32, rounded once.
+ *   positions [tokens] int32; one outside the table makes its token's pairs NaN
+ *   y         of x's tokens, heads, dim and dtype; x itself (same data and strides), or apart from it
+ *   backward  1: the transposed map, the gradient w.r.t. x of one w.r.t. y
+ * Up to 2^31 elements.                                                                      */
+int mebp_rope_apply(const mebp_rope* rope, const mebp_heads* x, const int32_t* positions, const mebp_heads* y,
+                    int32_t backward, mebp_stream_t stream);
+
+/* The cache: a pool of pages. Of every 16 tokens and head there is a block of keys [16][dim] and one of
+ * values [dim][16] in int8, with an fp32 scale each: a number is its code times its block's scale. */
+typedef struct {
+  int8_t* pages;     /* [n_pages][heads][page_tokens / 16][2][16 * dim], 16-byte aligned     */
+  float* scales;     /* [n_pages][heads][page_tokens / 16][2], 8-byte aligned                */
+  int32_t n_pages;
+  int32_t page_tokens; /* a power of two, 16 .. 65536                                       */
+  int32_t heads;     /* kv heads, up to 1024                                                */
+  int32_t dim;       /* 64, 128 or 256                                                      */
+} mebp_kv_cache;
+
+/* Bytes of one page's codes (its scales: page_tokens / 16 * heads * 8). 0 for an invalid shape. */
+size_t mebp_kv_page_bytes(int32_t page_tokens, int32_t heads, int32_t dim);
+
+/* New tokens of some sequences: rows start[s] .. start[s + 1] - 1 of a call's operands are the tokens
+ * past[s], past[s] + 1, .. of sequence s. Rows behind start[seqs] belong to none, and what a call
+ * writes is left as it was there. */
+typedef struct {
+  const int32_t* start;  /* [seqs + 1], not falling (device memory, as the two below)       */
+  const int32_t* past;   /* [seqs] tokens that were in the cache before                     */
+  const int32_t* table;  /* [seqs][table_ld]: the page of tokens p * page_tokens .. of a sequence at  */
+                         /* column p                                                        */
+  int64_t table_ld;      /* >= max_pages                                                    */
+  int32_t max_pages;     /* columns of the table                                            */
+  int32_t seqs;          /* 0 .. 65535                                                      */
+  int32_t max_new;       /* no sequence has more new tokens (rows beyond are left as they were) */
+  int32_t max_len;       /* none is longer with them (rows from there on are NaN in an attention); up to */
+                         /* 2^30. The call's launches are laid out for these two             */
+} mebp_kv_batch;
+
+/* Appends keys and values, the keys turned by their positions (rope NULL: as they are), and turns queries
+ * beside them. A block's scale is max(scale before, max |x| / 127 in fp32), "before" 0 where the block's
+ * first token is new; codes are round(x / scale) to nearest even, and where the scale rises the block's
+ * earlier ones round(code before / after). Scales and codes are those of 64-bit arithmetic.
+ *   k, v       of the cache's heads and dim, any dtype
+ *   q, q_out   [tokens][any heads][dim] of that dtype, together or both NULL; q_out may be q
+ * A NaN or an infinity makes its block's scale NaN. Where the table has no page of the pool (an id outside
+ * 0 .. n_pages - 1, a column beyond max_pages) nothing is stored. Blocks that are written belong to one
+ * sequence of the call; whole ones before them may be shared.                               */
+int mebp_kv_append(const mebp_kv_cache* cache, const mebp_kv_batch* batch, const mebp_rope* rope, const mebp_heads* k,
+                   const mebp_heads* v, const mebp_heads* q, const mebp_heads* q_out, mebp_stream_t stream);
+
+/* Reads tokens back as numbers, code times scale: here `past` is the first token that is read of a
+ * sequence, and its rows are as many as are read. k or v may be NULL. No page: NaN.          */
+int mebp_kv_read(const mebp_kv_cache* cache, const mebp_kv_batch* batch, const mebp_heads* k, const mebp_heads* v,
+                 mebp_stream_t stream);
+
+/* Attention of the rows over what their sequences have in the cache, their own tokens included (append
+ * them first): out = softmax(scale q k^T) v over the keys j <= i of the token at position i, with a window
+ * W > 0 over i - W < j <= i; query heads of one kv head are consecutive.
+ *   q, out  fp16 or bf16 [tokens][a multiple of the cache's heads][dim]; out apart from q
+ *   lse     [tokens][q heads] fp32 log-sum-exp of the scaled scores, or NULL
+ * Products in fp16 with fp32 sums (codes are exact there, as queries are up to a power of two per row;
+ * softmax weights are rounded to fp16), softmax in fp32. A key or value that is NaN, or whose page the table
+ * does not have, makes the rows that see its block NaN, and no others.                      */
+int mebp_kv_attention(const mebp_kv_cache* cache, const mebp_kv_batch* batch, const mebp_heads* q, const mebp_heads* out,
+                      float* lse, float scale, int32_t window, void* ws, size_t ws_bytes, mebp_stream_t stream);
+
+/* Bytes of workspace of such a call. Pure host computation; 0 for an invalid shape.         */
+size_t mebp_kv_attention_workspace_bytes(int32_t seqs, int32_t max_new, int32_t max_len, int32_t q_heads, int32_t heads,
+                                         int32_t dim, int32_t window);
+
+/* mebp_layer_forward_ckpt of `rows` new tokens of the batch's sequences: their keys and values join the
+ * layer's cache, and attention is over it (scale 1 / sqrt(head_dim), the layer's window).
+ *   x_in, x_out  [rows][d] fp32, apart from each other. Rows of no sequence go through the layer without
+ *                attention
+ *   cache        this layer's, of the config's n_kv_heads and head_dim
+ *   rope         of the layer's theta; positions beyond its table give NaN
+ *   ws           mebp_cached_workspace_bytes                                                */
+int mebp_layer_forward_cached(const mebp_config* cfg, int32_t layer, const mebp_layer_base* base, const mebp_layer_lora* lora,
+                              const float* x_in, float* x_out, int32_t rows, const mebp_kv_cache* cache,
+                              const mebp_kv_batch* batch, const mebp_rope* rope, void* ws, size_t ws_bytes,
+                              mebp_stream_t stream);
+size_t mebp_cached_workspace_bytes(const mebp_config* cfg, int32_t rows, int32_t seqs, int32_t max_new, int32_t max_len);
+
 /* Message for the last non-zero status returned on the calling thread ("" if none). */
 const char* mebp_last_error(void);
 
@@ -482,7 +603,8 @@ int mebp_kernel_timing_report(char* buf, size_t len);
  * that update a buffer in place are refused with MEBP_EINVAL ("gemm_tn_act_bwd",
  * "splitk_finalize_actbwd", "rope_fwd", "qkv_post", "headnorm_bwd", "ce_chunk_stats",
  * "ce_probs", "ce_dh_accum", "ce_final", "token_scores_grad_inplace", "distill_grad_inplace",
- * "distill_row_inplace", "lora_adamw", "lora_grad_accumulate"). With timing enabled, each burst of repeated launches is bracketed by one
+ * "distill_row_inplace", "rope_apply_inplace", "kv_append_inplace", "lora_adamw",
+ * "lora_grad_accumulate"). With timing enabled, each burst of repeated launches is bracketed by one
  * event pair and reported as `times` launches, so the report's average is the kernel's
  * back-to-back in-stream duration. Host-thread-unsafe; for benchmarks only. */
 int mebp_kernel_repeat(const char* kernel, int32_t times);

@@ -27,10 +27,13 @@ EXPORTED = (
     "mebp_set_workspace_guards", "mebp_workspace_guard_check", "mebp_logits_workspace_bytes",
     "mebp_token_logprobs", "mebp_token_logprobs_backward", "mebp_distill_topk", "mebp_head_workspace_bytes",
     "mebp_lm_head_logits", "mebp_lm_head_logits_backward", "mebp_lm_head_logprobs", "mebp_lm_head_distill_backward",
-    "mebp_distill_step_workspace_bytes", "mebp_train_step_distill",
+    "mebp_distill_step_workspace_bytes", "mebp_train_step_distill", "mebp_rope_positions", "mebp_rope_apply",
+    "mebp_kv_page_bytes", "mebp_kv_append", "mebp_kv_read", "mebp_kv_attention", "mebp_kv_attention_workspace_bytes",
+    "mebp_layer_forward_cached", "mebp_cached_workspace_bytes",
 )
 
-MEBP_F32, MEBP_F16, MEBP_BF16 = 0, 1, 2  # element types of a matrix of logits
+MEBP_F32, MEBP_F16, MEBP_BF16 = 0, 1, 2  # element types of a matrix of logits, and of heads
+KV_BLOCK = 16  # tokens of a cache's block
 MAX_TOP = 64  # most alternatives, and most entries of a teacher, per row
 
 STATIC_SCRATCH_BYTES = 64 << 20  # MEBP_STATIC_SCRATCH_BYTES
@@ -95,6 +98,30 @@ class MebpDistill(C.Structure):
                 ("k", C.c_int32), ("temperature", C.c_float), ("alpha", C.c_float)]
 
 
+class MebpHeads(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("ld", C.c_int64), ("head_ld", C.c_int64), ("tokens", C.c_int32),
+                ("heads", C.c_int32), ("dim", C.c_int32), ("dtype", C.c_int32)]
+
+
+class MebpRope(C.Structure):
+    _fields_ = [("table", C.c_void_p), ("rot", C.c_int32), ("n_pos", C.c_int32), ("interleaved", C.c_int32)]
+
+
+class MebpRopeScaling(C.Structure):
+    _fields_ = [("theta", C.c_float), ("factor", C.c_float), ("original", C.c_int32), ("low", C.c_float),
+                ("high", C.c_float), ("gain", C.c_float)]
+
+
+class MebpKvCache(C.Structure):
+    _fields_ = [("pages", C.c_void_p), ("scales", C.c_void_p), ("n_pages", C.c_int32), ("page_tokens", C.c_int32),
+                ("heads", C.c_int32), ("dim", C.c_int32)]
+
+
+class MebpKvBatch(C.Structure):
+    _fields_ = [("start", C.c_void_p), ("past", C.c_void_p), ("table", C.c_void_p), ("table_ld", C.c_int64),
+                ("max_pages", C.c_int32), ("seqs", C.c_int32), ("max_new", C.c_int32), ("max_len", C.c_int32)]
+
+
 class MebpError(RuntimeError):
     def __init__(self, code: int, msg: str):
         super().__init__(f"mebp status {code}: {msg}")
@@ -157,6 +184,21 @@ def lib() -> C.CDLL:
             "mebp_train_step_distill": (C.c_int, [cfgp, C.POINTER(MebpQ4), C.POINTER(MebpLayerBase), P,
                                                   C.POINTER(MebpLayerLora), P, I32, I32, C.POINTER(MebpDistill), P, P, P,
                                                   C.POINTER(MebpLayerLoraGrad), P, P, SZ, P]),
+            "mebp_rope_positions": (C.c_int, [C.POINTER(MebpRope), C.POINTER(MebpRopeScaling), P]),
+            "mebp_rope_apply": (C.c_int, [C.POINTER(MebpRope), C.POINTER(MebpHeads), P, C.POINTER(MebpHeads), I32, P]),
+            "mebp_kv_page_bytes": (SZ, [I32, I32, I32]),
+            "mebp_kv_append": (C.c_int, [C.POINTER(MebpKvCache), C.POINTER(MebpKvBatch), C.POINTER(MebpRope),
+                                         C.POINTER(MebpHeads), C.POINTER(MebpHeads), C.POINTER(MebpHeads),
+                                         C.POINTER(MebpHeads), P]),
+            "mebp_kv_read": (C.c_int, [C.POINTER(MebpKvCache), C.POINTER(MebpKvBatch), C.POINTER(MebpHeads),
+                                       C.POINTER(MebpHeads), P]),
+            "mebp_kv_attention": (C.c_int, [C.POINTER(MebpKvCache), C.POINTER(MebpKvBatch), C.POINTER(MebpHeads),
+                                            C.POINTER(MebpHeads), P, C.c_float, I32, P, SZ, P]),
+            "mebp_kv_attention_workspace_bytes": (SZ, [I32, I32, I32, I32, I32, I32, I32]),
+            "mebp_layer_forward_cached": (C.c_int, [cfgp, I32, C.POINTER(MebpLayerBase), C.POINTER(MebpLayerLora), P, P,
+                                                    I32, C.POINTER(MebpKvCache), C.POINTER(MebpKvBatch),
+                                                    C.POINTER(MebpRope), P, SZ, P]),
+            "mebp_cached_workspace_bytes": (SZ, [cfgp, I32, I32, I32, I32]),
             "mebp_kernel_timing": (C.c_int, [I32, I32]),
             "mebp_kernel_timing_report": (C.c_int, [C.c_char_p, SZ]),
             "mebp_kernel_repeat": (C.c_int, [C.c_char_p, I32]),
@@ -337,6 +379,51 @@ def mebp_train_step_distill(cfg, emb, layers, norm_final, lora, ids, B, T, disti
     r = lib().mebp_train_step_distill(C.byref(cfg), _ref(emb), layers, norm_final, lora, ids, B, T, _ref(distill), ckpt,
                                       loss, row_loss, grads, dx0, ws, ws_bytes, stream)
     return _check(r) if check else r
+
+
+def mebp_rope_positions(rope, scaling, stream=0, check=True):
+    r = lib().mebp_rope_positions(_ref(rope), _ref(scaling), stream)
+    return _check(r) if check else r
+
+
+def mebp_rope_apply(rope, x, positions, y, backward=False, stream=0, check=True):
+    r = lib().mebp_rope_apply(_ref(rope), _ref(x), positions, _ref(y), int(backward), stream)
+    return _check(r) if check else r
+
+
+def mebp_kv_page_bytes(page_tokens: int, heads: int, dim: int) -> int:
+    return lib().mebp_kv_page_bytes(page_tokens, heads, dim)
+
+
+def mebp_kv_append(cache, batch, rope, k, v, q, q_out, stream=0, check=True):
+    r = lib().mebp_kv_append(_ref(cache), _ref(batch), _ref(rope), _ref(k), _ref(v), _ref(q), _ref(q_out), stream)
+    return _check(r) if check else r
+
+
+def mebp_kv_read(cache, batch, k, v, stream=0, check=True):
+    r = lib().mebp_kv_read(_ref(cache), _ref(batch), _ref(k), _ref(v), stream)
+    return _check(r) if check else r
+
+
+def mebp_kv_attention(cache, batch, q, out, lse, scale, window, ws, ws_bytes, stream=0, check=True):
+    r = lib().mebp_kv_attention(_ref(cache), _ref(batch), _ref(q), _ref(out), lse, scale, window, ws, ws_bytes, stream)
+    return _check(r) if check else r
+
+
+def mebp_kv_attention_workspace_bytes(seqs: int, max_new: int, max_len: int, q_heads: int, heads: int, dim: int,
+                                      window: int = 0) -> int:
+    return lib().mebp_kv_attention_workspace_bytes(seqs, max_new, max_len, q_heads, heads, dim, window)
+
+
+def mebp_layer_forward_cached(cfg, layer, base, lora, x_in, x_out, rows, cache, batch, rope, ws, ws_bytes, stream=0,
+                              check=True):
+    r = lib().mebp_layer_forward_cached(C.byref(cfg), layer, _ref(base), _ref(lora), x_in, x_out, rows, _ref(cache),
+                                        _ref(batch), _ref(rope), ws, ws_bytes, stream)
+    return _check(r) if check else r
+
+
+def mebp_cached_workspace_bytes(cfg: MebpConfig, rows: int, seqs: int, max_new: int, max_len: int) -> int:
+    return lib().mebp_cached_workspace_bytes(C.byref(cfg), rows, seqs, max_new, max_len)
 
 
 def mebp_kernel_timing(enable: bool, capacity: int = 65536) -> int:

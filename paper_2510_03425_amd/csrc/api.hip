@@ -93,9 +93,9 @@ constexpr int kMaxGuards = 2 * S_COUNT;
 
 // Slots of the workspaces of the operators on logits and of the head that runs them; their guards'
 // tags follow the others'.
-enum OpSlot { OP_STATS, OP_KEYS, OP_PICKED, OP_HF, OP_Z, OP_DZ, OP_DHF, OP_PLANES, OP_ROW_LOSS, OP_COUNT };
+enum OpSlot { OP_STATS, OP_KEYS, OP_PICKED, OP_HF, OP_Z, OP_DZ, OP_DHF, OP_PLANES, OP_ROW_LOSS, OP_KV_PARTS, OP_COUNT };
 const char* kOpSlotNames[OP_COUNT] = {"logit_stats", "logit_keys", "logit_picked", "head_hf", "head_logits",
-                                      "head_dlogits", "head_dhf", "head_planes", "head_row_loss"};
+                                      "head_dlogits", "head_dhf", "head_planes", "head_row_loss", "kv_parts"};
 constexpr int kOpTag = 2 * S_COUNT;
 
 // A layer's weights as fragments: none, one product's at a time, or all at once.
@@ -870,8 +870,16 @@ hipError_t lora_bwd(const Ctx& x, const mebp_layer_lora* lora, const mebp_layer_
   return launch_lora_outer(oa, x.aux ? x.aux : x.st);
 }
 
+// What a layer's attention over a cache is called with, but for its operands.
+struct Cached {
+  KvAppendArgs append;
+  KvAttnArgs attn;
+};
+
 // Forward of one layer. keep=false: full forward to x_out. keep=true: recompute for the
 // backward (stops after z and its LoRA down-projection; x_out unused).
+// cached: attention of the rows over a paged cache that they join, in the place of that over the
+// call's own sequences (keep is false).
 // next_norm (forward loop only): the RMSNorm weights of the next block's input norm; the
 // down projection's split-K finalize then also writes that block's normalised input (into
 // `next_out`, default the activation slot `a`; one row kernel fewer per layer), and a_ready
@@ -879,7 +887,8 @@ hipError_t lora_bwd(const Ctx& x, const mebp_layer_lora* lora, const mebp_layer_
 // finalize leaves that norm to the next layer and says so there.
 int layer_forward(const Ctx& x, int l, const mebp_layer_base* base, const mebp_layer_lora* lora, const float* x_in,
                   float* x_out, float* rope, bool keep, const float* next_norm = nullptr,
-                  bool a_ready = false, f16* next_out = nullptr, bool* next_pending = nullptr) {
+                  bool a_ready = false, f16* next_out = nullptr, bool* next_pending = nullptr,
+                  const Cached* cached = nullptr) {
   const mebp_config* c = x.c;
   const Dims& D = x.D;
   f16* a = xs<f16>(x, S_A);
@@ -905,7 +914,7 @@ int layer_forward(const Ctx& x, int l, const mebp_layer_base* base, const mebp_l
   {
     // q, k, v projections with RoPE applied to q and k on the way out
     NtSeg qs = nt_seg(x, base, lora, MEBP_Q, q, D.qd, nullptr, 0), ks = nt_seg(x, base, lora, MEBP_K, k, D.kvd, nullptr, 0);
-    qs.rope = ks.rope = qk_post ? 0 : 1;
+    qs.rope = ks.rope = qk_post || cached ? 0 : 1;
     NtArgs na = nt_args(x, a, D.d, {qs, ks, nt_seg(x, base, lora, MEBP_V, v, D.kvd, nullptr, 0)});
     na.rope_cs = rope;
     na.rope_T = x.T;
@@ -917,18 +926,32 @@ int layer_forward(const Ctx& x, int l, const mebp_layer_base* base, const mebp_l
     QkvPostArgs pa{};
     pa.n = D.N; pa.T = x.T; pa.dh = c->head_dim; pa.eps = c->rms_eps; pa.cs = rope;
     pa.job[pa.njobs++] = QkvPostJob{q, D.qd, c->n_heads, bias ? base->bias[0] : nullptr, qkn ? base->q_norm : nullptr,
-                                    xs<f16>(x, S_QPRE), 1};
+                                    xs<f16>(x, S_QPRE), cached ? 0 : 1};
     pa.job[pa.njobs++] = QkvPostJob{k, D.kvd, c->n_kv_heads, bias ? base->bias[1] : nullptr,
-                                    qkn ? base->k_norm : nullptr, xs<f16>(x, S_KPRE), 1};
+                                    qkn ? base->k_norm : nullptr, xs<f16>(x, S_KPRE), cached ? 0 : 1};
     if (bias) pa.job[pa.njobs++] = QkvPostJob{v, D.kvd, c->n_kv_heads, base->bias[2], nullptr, nullptr, 0};
     HIP_TRY(launch_qkv_post(pa, x.st));
   }
-  AttnArgs at{};
-  at.q = q; at.k = k; at.v = v; at.ldq = D.qd; at.ldk = D.kvd;
-  at.B = x.B; at.T = x.T; at.Hq = c->n_heads; at.Hkv = c->n_kv_heads; at.dh = c->head_dim;
-  at.window = is_global(c, l) ? 0 : c->window;
-  at.o = o; at.lse = xs<float>(x, S_LSE);
-  HIP_TRY(launch_attn_fwd(at, split_scratch(x), x.st));
+  if (cached) {
+    KvAppendArgs ap = cached->append;
+    KvAttnArgs at = cached->attn;
+    const HeadsView hq{q, D.qd, c->head_dim}, hk{k, D.kvd, c->head_dim}, hv{v, D.kvd, c->head_dim};
+    ap.k = hk; ap.v = hv;
+    ap.q = ap.q_out = hq;
+    ap.rest = o;  // rows that no sequence has go on with an attention output of 0
+    ap.rest_cols = D.qd;
+    HIP_TRY(launch_kv_append(ap, LOGIT_F16, x.st));
+    at.q = hq;
+    at.out = HeadsView{o, D.qd, c->head_dim};
+    HIP_TRY(launch_kv_attention(at, LOGIT_F16, x.st));
+  } else {
+    AttnArgs at{};
+    at.q = q; at.k = k; at.v = v; at.ldq = D.qd; at.ldk = D.kvd;
+    at.B = x.B; at.T = x.T; at.Hq = c->n_heads; at.Hkv = c->n_kv_heads; at.dh = c->head_dim;
+    at.window = is_global(c, l) ? 0 : c->window;
+    at.o = o; at.lse = xs<float>(x, S_LSE);
+    HIP_TRY(launch_attn_fwd(at, split_scratch(x), x.st));
+  }
   HIP_TRY(lora_down(x, lora, o, D.qd, {MEBP_O}, &lr));
   bool norm_here = sandwich;  // c = RMSNorm(h) is still to be done, with its adapters
   if (sandwich) {
@@ -2425,6 +2448,432 @@ int mebp_train_step_distill(const mebp_config* cfg, const mebp_q4* emb, const me
   };
   return guarded(cfg, B, T, ws, stream, [&] {
     return train_step_impl(cfg, emb, layers, norm_final, lora, ids, B, T, ckpt, nullptr, block, grads, dx0, ws, stream);
+  });
+}
+
+}  // extern "C"
+
+namespace {
+// ------------------------------------------------------------------ rotary positions, cache of keys and values
+constexpr int kMaxHeads = 1024, kMaxSeqs = 65535;
+
+int check_heads(const mebp_heads* x, const char* what, bool written) {
+  if (!x) return fail(MEBP_EINVAL, "%s is NULL", what);
+  if (x->tokens < 0 || x->heads < 1 || x->dim < 1)
+    return fail(MEBP_EINVAL, "%s: tokens %d < 0, heads %d or dim %d < 1", what, x->tokens, x->heads, x->dim);
+  if (x->tokens > (1 << 24) || x->heads > kMaxHeads || x->dim > 1024)
+    return fail(MEBP_EUNSUPPORTED, "%s: %d x %d x %d above 2^24 tokens, %d heads or 1024 elements", what, x->tokens, x->heads,
+                x->dim, kMaxHeads);
+  if (x->dtype < MEBP_F32 || x->dtype > MEBP_BF16) return fail(MEBP_EINVAL, "%s: dtype %d unknown", what, x->dtype);
+  const int64_t most = (int64_t)1 << 32;
+  if (x->ld < 0 || x->head_ld < 0) return fail(MEBP_EINVAL, "%s: negative ld or head_ld", what);
+  if (x->ld > most || x->head_ld > most) return fail(MEBP_EUNSUPPORTED, "%s: ld or head_ld above 2^32", what);
+  if (written) {
+    // no two elements at one address: heads within tokens, or tokens within heads
+    const int64_t t = x->tokens - 1, h = x->heads - 1;
+    const bool inner = (!h || x->head_ld >= x->dim) && (t <= 0 || x->ld >= h * x->head_ld + x->dim);
+    const bool outer = (t <= 0 || x->ld >= x->dim) && (!h || x->head_ld >= t * x->ld + x->dim);
+    if (!inner && !outer) return fail(MEBP_EINVAL, "%s: its heads overlap (ld, head_ld)", what);
+  }
+  if (x->tokens && !x->data) return fail(MEBP_EINVAL, "%s: data is NULL", what);
+  if (!aligned(x->data, logit_size(x->dtype))) return fail(MEBP_EINVAL, "%s: data not aligned to its elements", what);
+  return MEBP_OK;
+}
+Span span(const mebp_heads* x, const char* what) {
+  if (!x || !x->tokens) return Span{nullptr, 0, what};
+  return Span{x->data,
+              ((size_t)(x->tokens - 1) * x->ld + (size_t)(x->heads - 1) * x->head_ld + x->dim) * logit_size(x->dtype), what};
+}
+// Rows of one matrix side by side (queries, keys and values of one product, say): same distance of tokens,
+// and the heads of a token of one between those of the other.
+bool side_by_side(const mebp_heads* a, const mebp_heads* b) {
+  const int64_t size[2] = {(int64_t)logit_size(a->dtype), (int64_t)logit_size(b->dtype)}, ld = a->ld * size[0];
+  const int64_t la = ((a->heads - 1) * a->head_ld + a->dim) * size[0], lb = ((b->heads - 1) * b->head_ld + b->dim) * size[1];
+  if (ld != b->ld * size[1] || la > ld || lb > ld) return false;
+  const int64_t d = ((int64_t)((uintptr_t)b->data - (uintptr_t)a->data) % ld + ld) % ld;
+  return d >= la && d + lb <= ld;
+}
+int check_heads_apart(const mebp_heads* out, const char* what, const mebp_heads* x, const char* other) {
+  if (!out->tokens || !x->tokens || side_by_side(out, x)) return MEBP_OK;
+  return check_apart(span(out, what), {span(x, other)});
+}
+HeadsView view(const mebp_heads& x) { return HeadsView{x.data, x.ld, x.head_ld}; }
+bool same_view(const mebp_heads* x, const mebp_heads* y) {
+  return x->data == y->data && x->ld == y->ld && x->head_ld == y->head_ld;
+}
+int check_like(const mebp_heads* x, const char* what, int tokens, int heads, int dim, int dtype) {
+  if (x->tokens != tokens || x->heads != heads || x->dim != dim || x->dtype != dtype)
+    return fail(MEBP_EINVAL, "%s: %d x %d x %d of dtype %d, not %d x %d x %d of dtype %d", what, x->tokens, x->heads, x->dim,
+                x->dtype, tokens, heads, dim, dtype);
+  return MEBP_OK;
+}
+
+int check_rope(const mebp_rope* r) {
+  if (!r) return fail(MEBP_EINVAL, "rope is NULL");
+  if (r->rot < 2 || r->rot % 2 || r->n_pos < 1) return fail(MEBP_EINVAL, "rope: rot %d not even and >= 2, or n_pos %d < 1", r->rot, r->n_pos);
+  if (r->rot > 1024 || r->n_pos > (1 << 28)) return fail(MEBP_EUNSUPPORTED, "rope: rot %d above 1024 or n_pos %d above 2^28", r->rot, r->n_pos);
+  if (r->interleaved != 0 && r->interleaved != 1) return fail(MEBP_EINVAL, "rope: interleaved %d not 0 or 1", r->interleaved);
+  if (!r->table || !aligned(r->table, 8)) return fail(MEBP_EINVAL, "rope: table NULL or not 8-byte aligned");
+  return MEBP_OK;
+}
+int check_rope_for(const mebp_rope* r, int dim) {
+  const int e = check_rope(r);
+  if (e) return e;
+  if (r->rot > dim) return fail(MEBP_EINVAL, "rope: rot %d above the head's %d elements", r->rot, dim);
+  return MEBP_OK;
+}
+Span table_span(const mebp_rope* r) { return Span{r ? r->table : nullptr, r ? (size_t)r->n_pos * r->rot * 4 : 0, "the rope's table"}; }
+RopeView rope_view(const mebp_rope* r) {
+  return r ? RopeView{(const float2*)r->table, r->rot, r->n_pos, r->interleaved} : RopeView{};
+}
+
+int check_cache(const mebp_kv_cache* c) {
+  if (!c) return fail(MEBP_EINVAL, "cache is NULL");
+  if (c->n_pages < 1 || c->heads < 1 || c->page_tokens < 1)
+    return fail(MEBP_EINVAL, "cache: n_pages %d, heads %d or page_tokens %d < 1", c->n_pages, c->heads, c->page_tokens);
+  if (c->dim != 64 && c->dim != 128 && c->dim != 256) return fail(MEBP_EUNSUPPORTED, "cache: dim %d not in {64, 128, 256}", c->dim);
+  if (c->page_tokens < 16 || c->page_tokens > 65536 || (c->page_tokens & (c->page_tokens - 1)))
+    return fail(MEBP_EUNSUPPORTED, "cache: page_tokens %d not a power of two in [16, 65536]", c->page_tokens);
+  if (c->heads > kMaxHeads) return fail(MEBP_EUNSUPPORTED, "cache: heads %d above %d", c->heads, kMaxHeads);
+  if (!c->pages || !aligned(c->pages, 16)) return fail(MEBP_EINVAL, "cache: pages NULL or not 16-byte aligned");
+  if (!c->scales || !aligned(c->scales, 8)) return fail(MEBP_EINVAL, "cache: scales NULL or not 8-byte aligned");
+  return MEBP_OK;
+}
+size_t cache_blocks(const mebp_kv_cache* c) { return (size_t)c->n_pages * c->heads * (c->page_tokens / kKvBlock); }
+Span pages_span(const mebp_kv_cache* c) { return Span{c->pages, cache_blocks(c) * 2 * kKvBlock * c->dim, "the cache's pages"}; }
+Span scales_span(const mebp_kv_cache* c) { return words(c->scales, cache_blocks(c) * 2, "the cache's scales"); }
+KvPages pages_view(const mebp_kv_cache* c) {
+  int lb = 0;
+  while (kKvBlock << lb < c->page_tokens) ++lb;
+  return KvPages{c->pages, c->scales, c->n_pages, c->heads, c->dim, lb};
+}
+
+int check_batch_shape(int seqs, int max_new, int max_len) {
+  if (seqs < 0 || max_new < 1 || max_len < 1) return fail(MEBP_EINVAL, "batch: seqs %d < 0, max_new %d or max_len %d < 1", seqs, max_new, max_len);
+  if (seqs > kMaxSeqs || max_new > (1 << 24) || max_len > (1 << 30))
+    return fail(MEBP_EUNSUPPORTED, "batch: seqs %d above %d, max_new %d above 2^24 or max_len %d above 2^30", seqs, kMaxSeqs, max_new, max_len);
+  return MEBP_OK;
+}
+int check_batch(const mebp_kv_batch* b) {
+  int e;
+  if (!b) return fail(MEBP_EINVAL, "batch is NULL");
+  if ((e = check_batch_shape(b->seqs, b->max_new, b->max_len))) return e;
+  if (b->max_pages < 1 || b->table_ld < b->max_pages)
+    return fail(MEBP_EINVAL, "batch: max_pages %d < 1 or table_ld %lld below it", b->max_pages, (long long)b->table_ld);
+  if (b->table_ld > ((int64_t)1 << 32)) return fail(MEBP_EUNSUPPORTED, "batch: table_ld above 2^32");
+  if (!b->seqs) return MEBP_OK;
+  if ((e = check_words(b->start, 1, "batch: start")) || (e = check_words(b->past, 1, "batch: past")) ||
+      (e = check_words(b->table, 1, "batch: table")))
+    return e;
+  return MEBP_OK;
+}
+KvRows rows_view(const mebp_kv_batch* b, int rows) {
+  return KvRows{b->start, b->past, b->table, b->table_ld, b->max_pages, b->seqs, b->max_new, b->max_len, rows};
+}
+// an output lies apart from the batch's own operands
+int check_batch_apart(const mebp_kv_batch* b, const Span& out) {
+  if (!b->seqs) return MEBP_OK;
+  return check_apart(out, {words(b->start, b->seqs + 1, "batch: start"), words(b->past, b->seqs, "batch: past"),
+                           words(b->table, (size_t)(b->seqs - 1) * b->table_ld + b->max_pages, "batch: table")});
+}
+// 16-token blocks that the tokens of one sequence lie in at most
+int touched_blocks(int max_new) { return (max_new + 2 * kKvBlock - 2) / kKvBlock; }
+// workgroups of 256 along a grid's x
+int check_grid(int64_t groups) {
+  if (groups >= (int64_t)1 << 24) return fail(MEBP_EUNSUPPORTED, "more than 2^24 workgroups for max_new, max_len and heads");
+  return MEBP_OK;
+}
+
+int check_append(const mebp_kv_cache* c, const mebp_kv_batch* b, const mebp_rope* rope, int rows, int q_heads) {
+  int e;
+  if ((e = check_cache(c)) || (e = check_batch(b)) || (rope && (e = check_rope_for(rope, c->dim))) ||
+      (e = check_grid((int64_t)touched_blocks(b->max_new) * (2 * c->heads + q_heads))))
+    return e;
+  const Span pg = pages_span(c), sc = scales_span(c);
+  if ((e = check_batch_apart(b, pg)) || (e = check_batch_apart(b, sc)) || (e = check_apart(pg, {sc, table_span(rope)})) ||
+      (e = check_apart(sc, {table_span(rope)})))
+    return e;
+  (void)rows;
+  return MEBP_OK;
+}
+KvAppendArgs append_args(const mebp_kv_cache* c, const mebp_kv_batch* b, const mebp_rope* rope, int rows) {
+  KvAppendArgs a{};
+  a.c = pages_view(c);
+  a.b = rows_view(b, rows);
+  a.rope = rope_view(rope);
+  a.nblk = touched_blocks(b->max_new);
+  return a;
+}
+
+OpLayout kv_layout(const KvPlan& p, int seqs, int max_new, int q_heads, int heads, int dim) {
+  OpLayout o;
+  o.place(OP_KV_PARTS, kv_part_floats(p, seqs, max_new, q_heads, heads, dim) * 4);
+  o.done();
+  return o;
+}
+int check_attention_shape(int seqs, int max_new, int max_len, int q_heads, int heads, int dim, int window) {
+  int e;
+  if ((e = check_batch_shape(seqs, max_new, max_len))) return e;
+  if (heads < 1 || q_heads < 1 || q_heads % heads) return fail(MEBP_EINVAL, "%d query heads are no multiple of %d", q_heads, heads);
+  if (heads > kMaxHeads || q_heads > kMaxHeads) return fail(MEBP_EUNSUPPORTED, "more than %d heads", kMaxHeads);
+  if (dim != 64 && dim != 128 && dim != 256) return fail(MEBP_EUNSUPPORTED, "dim %d not in {64, 128, 256}", dim);
+  if (window < 0) return fail(MEBP_EINVAL, "window %d < 0", window);
+  const KvPlan p = kv_plan(seqs, max_new, max_len, q_heads, heads, dim, window);
+  if ((e = check_grid((int64_t)p.row_tiles * p.splits)) || (e = check_grid((int64_t)max_new * (q_heads / heads)))) return e;
+  return MEBP_OK;
+}
+KvAttnArgs attention_args(const mebp_kv_cache* c, const mebp_kv_batch* b, int rows, int q_heads, float scale, int window,
+                          const KvPlan& p) {
+  KvAttnArgs a{};
+  a.c = pages_view(c);
+  a.b = rows_view(b, rows);
+  a.q_heads = q_heads;
+  a.group = q_heads / c->heads;
+  a.window = window;
+  a.scale = (float)(1.4426950408889634 * (double)scale);
+  a.plan = p;
+  return a;
+}
+
+int check_cached_shape(const mebp_config* cfg, int rows, int seqs, int max_new, int max_len) {
+  int e;
+  if ((e = check_config(cfg)) || (e = check_shape(1, rows))) return e;
+  for (int w : {cfg->window, 0})
+    if ((e = check_attention_shape(seqs, max_new, max_len, cfg->n_heads, cfg->n_kv_heads, cfg->head_dim, w))) return e;
+  return MEBP_OK;
+}
+// the layer's slots, and behind them the attention's
+struct CachedLayout {
+  mebp_config c;  // without the vocabulary
+  size_t layer, total;
+};
+CachedLayout cached_layout(const mebp_config* cfg, int rows, int seqs, int max_new, int max_len) {
+  CachedLayout l{*cfg, 0, 0};
+  l.c.vocab = 0;
+  l.layer = (mebp_workspace_bytes(&l.c, 1, rows) + 255) & ~(size_t)255;
+  for (int w : {cfg->window, 0}) {
+    const KvPlan p = kv_plan(seqs, max_new, max_len, cfg->n_heads, cfg->n_kv_heads, cfg->head_dim, w);
+    l.total = std::max(l.total, l.layer + kv_layout(p, seqs, max_new, cfg->n_heads, cfg->n_kv_heads, cfg->head_dim).L.total);
+  }
+  return l;
+}
+}  // namespace
+
+extern "C" {
+
+int mebp_rope_positions(const mebp_rope* rope, const mebp_rope_scaling* f, mebp_stream_t stream) {
+  int e;
+  if ((e = check_rope(rope))) return e;
+  if (!f) return fail(MEBP_EINVAL, "scaling is NULL");
+  if (!(f->theta > 0.f) || !isfinite(f->theta)) return fail(MEBP_EINVAL, "rope: bad theta");
+  if (!(f->factor >= 1.f) || !isfinite(f->factor)) return fail(MEBP_EINVAL, "rope: factor %g below 1", f->factor);
+  if (!isfinite(f->gain)) return fail(MEBP_EINVAL, "rope: bad gain");
+  if (f->original < 0) return fail(MEBP_EINVAL, "rope: original %d < 0", f->original);
+  if (f->original && (!(f->low >= 0.f) || !(f->high > f->low) || !isfinite(f->high)))
+    return fail(MEBP_EINVAL, "rope: low %g and high %g not 0 <= low < high", f->low, f->high);
+  RopeTableArgs a{};
+  a.table = (float2*)rope->table;
+  a.rot = rope->rot;
+  a.n_pos = rope->n_pos;
+  a.theta = f->theta;
+  a.inv_factor = 1.0 / (double)f->factor;
+  a.gain = f->gain;
+  if (f->original) {
+    a.low = f->low;
+    a.inv_span = 1.0 / ((double)f->high - (double)f->low);
+    a.turns = (double)f->original / 6.283185307179586;
+  }
+  HIP_TRY(launch_rope_positions(a, (hipStream_t)stream));
+  return MEBP_OK;
+}
+
+int mebp_rope_apply(const mebp_rope* rope, const mebp_heads* x, const int32_t* positions, const mebp_heads* y,
+                    int32_t backward, mebp_stream_t stream) {
+  int e;
+  if ((e = check_heads(x, "x", false)) || (e = check_heads(y, "y", true)) || (e = check_rope_for(rope, x->dim)) ||
+      (e = check_like(y, "y", x->tokens, x->heads, x->dim, x->dtype)) || (e = check_words(positions, x->tokens, "positions")))
+    return e;
+  if ((int64_t)x->tokens * x->heads * x->dim > (int64_t)1 << 31) return fail(MEBP_EUNSUPPORTED, "x: more than 2^31 elements");
+  if (!x->tokens) return MEBP_OK;
+  const Span out = span(y, "y");
+  if ((!same_view(x, y) && (e = check_heads_apart(y, "y", x, "x without being it (same data, ld and head_ld)"))) ||
+      (e = check_apart(out, {words(positions, x->tokens, "positions"), table_span(rope)})))
+    return e;
+  RopeArgs a{};
+  a.x = view(*x);
+  a.y = view(*y);
+  a.rope = rope_view(rope);
+  a.pos = positions;
+  a.tokens = x->tokens;
+  a.heads = x->heads;
+  a.dim = x->dim;
+  a.backward = backward != 0;
+  HIP_TRY(launch_rope_apply(a, x->dtype, (hipStream_t)stream));
+  return MEBP_OK;
+}
+
+size_t mebp_kv_page_bytes(int32_t page_tokens, int32_t heads, int32_t dim) {
+  std::string saved = g_last_error;
+  const mebp_kv_cache c{(int8_t*)256, (float*)256, 1, page_tokens, heads, dim};
+  if (check_cache(&c)) {
+    g_last_error = saved;
+    return 0;
+  }
+  return pages_span(&c).bytes;
+}
+
+int mebp_kv_append(const mebp_kv_cache* cache, const mebp_kv_batch* batch, const mebp_rope* rope, const mebp_heads* k,
+                   const mebp_heads* v, const mebp_heads* q, const mebp_heads* q_out, mebp_stream_t stream) {
+  int e;
+  if ((e = check_heads(k, "k", false)) || (e = check_heads(v, "v", false)) ||
+      (e = check_append(cache, batch, rope, k->tokens, q ? q->heads : 0)) ||
+      (e = check_like(k, "k", k->tokens, cache->heads, cache->dim, k->dtype)) ||
+      (e = check_like(v, "v", k->tokens, cache->heads, cache->dim, k->dtype)))
+    return e;
+  if (!q != !q_out || (q && !rope)) return fail(MEBP_EINVAL, "q, q_out and the rope that turns them come together");
+  const Span pg = pages_span(cache), sc = scales_span(cache);
+  if ((e = check_apart(pg, {span(k, "k"), span(v, "v")})) || (e = check_apart(sc, {span(k, "k"), span(v, "v")}))) return e;
+  if (q) {
+    if ((e = check_heads(q, "q", false)) || (e = check_heads(q_out, "q_out", true)) ||
+        (e = check_like(q, "q", k->tokens, q->heads, cache->dim, k->dtype)) ||
+        (e = check_like(q_out, "q_out", k->tokens, q->heads, cache->dim, k->dtype)))
+      return e;
+    const Span out = span(q_out, "q_out");
+    if ((!same_view(q, q_out) && (e = check_heads_apart(q_out, "q_out", q, "q without being it (same data, ld and head_ld)"))) ||
+        (e = check_heads_apart(q_out, "q_out", k, "k")) || (e = check_heads_apart(q_out, "q_out", v, "v")) ||
+        (e = check_apart(out, {pg, sc, table_span(rope)})) || (e = check_batch_apart(batch, out)) ||
+        (e = check_apart(pg, {span(q, "q")})) || (e = check_apart(sc, {span(q, "q")})))
+      return e;
+  }
+  if (!k->tokens || !batch->seqs) return MEBP_OK;
+  KvAppendArgs a = append_args(cache, batch, rope, k->tokens);
+  a.k = view(*k);
+  a.v = view(*v);
+  if (q) {
+    a.q = view(*q);
+    a.q_out = view(*q_out);
+    a.q_heads = q->heads;
+  }
+  HIP_TRY(launch_kv_append(a, k->dtype, (hipStream_t)stream));
+  return MEBP_OK;
+}
+
+int mebp_kv_read(const mebp_kv_cache* cache, const mebp_kv_batch* batch, const mebp_heads* k, const mebp_heads* v,
+                 mebp_stream_t stream) {
+  int e;
+  if ((e = check_cache(cache)) || (e = check_batch(batch))) return e;
+  if (!k && !v) return fail(MEBP_EINVAL, "neither k nor v");
+  const mebp_heads* one = k ? k : v;
+  for (const mebp_heads* x : {k, v}) {
+    if (!x) continue;
+    const char* what = x == k ? "k" : "v";
+    if ((e = check_heads(x, what, true)) || (e = check_like(x, what, one->tokens, cache->heads, cache->dim, one->dtype)) ||
+        (e = check_apart(span(x, what), {pages_span(cache), scales_span(cache)})) || (e = check_batch_apart(batch, span(x, what))))
+      return e;
+  }
+  if (k && v && (e = check_heads_apart(k, "k", v, "v"))) return e;
+  if ((e = check_grid((int64_t)touched_blocks(batch->max_new) * 2 * cache->heads))) return e;
+  if (!one->tokens || !batch->seqs) return MEBP_OK;
+  KvReadArgs a{};
+  a.c = pages_view(cache);
+  a.b = rows_view(batch, one->tokens);
+  if (k) a.k = view(*k);
+  if (v) a.v = view(*v);
+  a.nblk = touched_blocks(batch->max_new);
+  HIP_TRY(launch_kv_read(a, one->dtype, (hipStream_t)stream));
+  return MEBP_OK;
+}
+
+size_t mebp_kv_attention_workspace_bytes(int32_t seqs, int32_t max_new, int32_t max_len, int32_t q_heads, int32_t heads,
+                                         int32_t dim, int32_t window) {
+  std::string saved = g_last_error;
+  if (check_attention_shape(seqs, max_new, max_len, q_heads, heads, dim, window)) {
+    g_last_error = saved;
+    return 0;
+  }
+  const KvPlan p = kv_plan(seqs, max_new, max_len, q_heads, heads, dim, window);
+  return kv_layout(p, seqs, max_new, q_heads, heads, dim).L.total;
+}
+
+int mebp_kv_attention(const mebp_kv_cache* cache, const mebp_kv_batch* batch, const mebp_heads* q, const mebp_heads* out,
+                      float* lse, float scale, int32_t window, void* ws, size_t ws_bytes, mebp_stream_t stream) {
+  int e;
+  if ((e = check_cache(cache)) || (e = check_batch(batch)) || (e = check_heads(q, "q", false)) || (e = check_heads(out, "out", true)) ||
+      (e = check_like(q, "q", q->tokens, q->heads, cache->dim, q->dtype)) ||
+      (e = check_like(out, "out", q->tokens, q->heads, cache->dim, q->dtype)) ||
+      (e = check_attention_shape(batch->seqs, batch->max_new, batch->max_len, q->heads, cache->heads, cache->dim, window)))
+    return e;
+  if (q->dtype == MEBP_F32) return fail(MEBP_EUNSUPPORTED, "q: dtype fp32 (attention takes fp16 and bf16)");
+  if (!isfinite(scale)) return fail(MEBP_EINVAL, "scale is not finite");
+  if (lse && !aligned(lse, 4)) return fail(MEBP_EINVAL, "lse not 4-byte aligned");
+  const Span o = span(out, "out"), l = words(lse, (size_t)q->tokens * q->heads, "lse");
+  for (const Span& w : {o, l})
+    if ((e = check_apart(w, {pages_span(cache), scales_span(cache)})) || (e = check_batch_apart(batch, w))) return e;
+  if ((e = check_heads_apart(out, "out", q, "q")) || (e = check_apart(l, {span(q, "q")})) || (e = check_apart(o, {l}))) return e;
+  const KvPlan p = kv_plan(batch->seqs, batch->max_new, batch->max_len, q->heads, cache->heads, cache->dim, window);
+  const OpLayout lay = kv_layout(p, batch->seqs, batch->max_new, q->heads, cache->heads, cache->dim);
+  if ((e = check_op_ws(lay, ws, ws_bytes))) return e;
+  const Span scratch{ws, lay.L.total, "the workspace"};
+  if ((e = check_apart(scratch, {span(q, "q"), o, l, pages_span(cache), scales_span(cache)})) || (e = check_batch_apart(batch, scratch)))
+    return e;
+  if (!q->tokens || !batch->seqs) return MEBP_OK;
+  KvAttnArgs a = attention_args(cache, batch, q->tokens, q->heads, scale, window, p);
+  a.q = view(*q);
+  a.out = view(*out);
+  a.lse = lse;
+  a.part = lay.at<float>(ws, OP_KV_PARTS);
+  return guarded(lay, ws, stream, [&] {
+    HIP_TRY(launch_kv_attention(a, q->dtype, (hipStream_t)stream));
+    return (int)MEBP_OK;
+  });
+}
+
+size_t mebp_cached_workspace_bytes(const mebp_config* cfg, int32_t rows, int32_t seqs, int32_t max_new, int32_t max_len) {
+  std::string saved = g_last_error;
+  if (check_cached_shape(cfg, rows, seqs, max_new, max_len)) {
+    g_last_error = saved;
+    return 0;
+  }
+  return cached_layout(cfg, rows, seqs, max_new, max_len).total;
+}
+
+int mebp_layer_forward_cached(const mebp_config* cfg, int32_t layer, const mebp_layer_base* base, const mebp_layer_lora* lora,
+                              const float* x_in, float* x_out, int32_t rows, const mebp_kv_cache* cache,
+                              const mebp_kv_batch* batch, const mebp_rope* rope, void* ws, size_t ws_bytes,
+                              mebp_stream_t stream) {
+  int e;
+  if ((e = check_config(cfg)) || (e = check_shape(1, rows)) || (e = check_layer(cfg, layer, base, lora)) ||
+      (e = check_act(x_in, "x_in")) || (e = check_act(x_out, "x_out")) ||
+      (e = check_append(cache, batch, rope, rows, cfg->n_heads)) || (e = check_rope(rope)) ||
+      (e = check_cached_shape(cfg, rows, batch->seqs, batch->max_new, batch->max_len)))
+    return e;
+  if (cache->heads != cfg->n_kv_heads || cache->dim != cfg->head_dim)
+    return fail(MEBP_EINVAL, "cache: %d heads of %d, the model has %d of %d", cache->heads, cache->dim, cfg->n_kv_heads, cfg->head_dim);
+  if (!batch->seqs) return fail(MEBP_EINVAL, "batch: no sequences");
+  const size_t n = (size_t)rows * cfg->hidden;
+  const Span out = words(x_out, n, "x_out"), in = words(x_in, n, "x_in");
+  const CachedLayout lay = cached_layout(cfg, rows, batch->seqs, batch->max_new, batch->max_len);
+  if (!ws) return fail(MEBP_EINVAL, "workspace is NULL");
+  if (!aligned(ws, 256)) return fail(MEBP_EINVAL, "workspace not 256-byte aligned");
+  if (ws_bytes < lay.total) return fail(MEBP_EWORKSPACE, "workspace %zu bytes < required %zu", ws_bytes, lay.total);
+  const Span scratch{ws, lay.total, "the workspace"};
+  if ((e = check_apart(out, {in, pages_span(cache), scales_span(cache), table_span(rope)})) || (e = check_batch_apart(batch, out)) ||
+      (e = check_apart(scratch, {in, out, pages_span(cache), scales_span(cache), table_span(rope)})) ||
+      (e = check_batch_apart(batch, scratch)) || (e = check_apart(pages_span(cache), {in})) || (e = check_apart(scales_span(cache), {in})))
+    return e;
+  const int window = is_global(cfg, layer) ? 0 : cfg->window;
+  const KvPlan p = kv_plan(batch->seqs, batch->max_new, batch->max_len, cfg->n_heads, cache->heads, cache->dim, window);
+  const OpLayout kv = kv_layout(p, batch->seqs, batch->max_new, cfg->n_heads, cache->heads, cache->dim);
+  char* kv_ws = (char*)ws + lay.layer;
+  Cached cached{append_args(cache, batch, rope, rows),
+                attention_args(cache, batch, rows, cfg->n_heads, 1.f / sqrtf((float)cfg->head_dim), window, p)};
+  cached.append.q_heads = cfg->n_heads;
+  cached.attn.part = kv.at<float>(kv_ws, OP_KV_PARTS);
+  return guarded(kv, kv_ws, stream, [&] {
+    return guarded(&lay.c, 1, rows, ws, stream, [&] {
+      Ctx x = make_ctx(&lay.c, 1, rows, ws, stream);
+      return layer_forward(x, layer, base, lora, x_in, x_out, nullptr, false, nullptr, false, nullptr, nullptr, &cached);
+    });
   });
 }
 

@@ -433,6 +433,84 @@ struct DistillArgs {
 };
 hipError_t launch_distill(DistillArgs a, int dtype, int gtype, hipStream_t st);
 
+// ---------------------------------------------------------------- rotary positions, cache of keys and values
+// element types as LOGIT_*; element (token n, head h, dim e) at p + n * ld + h * hld + e
+struct HeadsView {
+  void* p;
+  int64_t ld, hld;
+};
+struct RopeView {
+  const float2* table;     // [n_pos][rot / 2] (cos, sin)
+  int rot, n_pos, interleaved;
+};
+struct RopeTableArgs {
+  float2* table;
+  int rot, n_pos;
+  double theta, inv_factor, low, inv_span, turns;  // inv_span 0: every frequency times inv_factor
+  double gain;
+};
+hipError_t launch_rope_positions(const RopeTableArgs& a, hipStream_t st);
+struct RopeArgs {
+  HeadsView x, y;
+  RopeView rope;
+  const int32_t* pos;
+  int tokens, heads, dim, backward;
+};
+hipError_t launch_rope_apply(const RopeArgs& a, int dtype, hipStream_t st);
+
+// The paged cache: int8 [n_pages][heads][blocks][2][16 dim], scales [n_pages][heads][blocks][2]; page =
+// 16 << log_blocks tokens.
+constexpr int kKvBlock = 16;
+struct KvPages {
+  int8_t* codes;
+  float* scales;
+  int n_pages, heads, dim, log_blocks;
+};
+// Rows start[s] .. start[s + 1] are tokens past[s] .. of sequence s, whose pages table[s] names.
+struct KvRows {
+  const int32_t *start, *past, *table;
+  int64_t table_ld;
+  int cols, seqs, max_new, max_len, rows;
+};
+struct KvAppendArgs {
+  KvPages c;
+  KvRows b;
+  RopeView rope;           // table null: keys are not turned
+  HeadsView k, v, q, q_out;  // q.p null: none
+  int q_heads, nblk;       // nblk: blocks that a sequence's new tokens touch at most
+  f16* rest;               // [rows][rest_cols], whose rows behind the last sequence are cleared; null: nothing is
+  int rest_cols;           // a multiple of 8
+  int q_per, q_groups;     // set by the launcher
+};
+hipError_t launch_kv_append(KvAppendArgs a, int dtype, hipStream_t st);
+struct KvReadArgs {
+  KvPages c;
+  KvRows b;
+  HeadsView k, v;          // either p may be null
+  int nblk;
+};
+hipError_t launch_kv_read(const KvReadArgs& a, int dtype, hipStream_t st);
+// Launch plan of an attention: `rows` query rows (token, head of the group) per workgroup, and chunks of
+// `chunk` 64-key tiles, `splits` of them at most over a sequence (1: no partial results).
+struct KvPlan {
+  bool wide;               // k_kv_wide, else k_kv_rows
+  int rows, row_tiles, splits, chunk;
+};
+KvPlan kv_plan(int seqs, int max_new, int max_len, int q_heads, int heads, int dim, int window);
+size_t kv_part_floats(const KvPlan& p, int seqs, int max_new, int q_heads, int heads, int dim);
+struct KvAttnArgs {
+  KvPages c;
+  KvRows b;
+  HeadsView q, out;
+  float* lse;              // [rows][q_heads] or null
+  int q_heads, group, window;
+  float scale;             // times log2(e)
+  KvPlan plan;
+  float* part;             // kv_part_floats
+  int part_rows;           // set by the launcher
+};
+hipError_t launch_kv_attention(KvAttnArgs a, int dtype, hipStream_t st);
+
 // ---------------------------------------------------------------- diagnostics
 // Per-kernel event timing (see timing.hip). timer_begin returns -1 when disabled.
 // count: launches bracketed by this record (a repeated burst counts as `count` launches)

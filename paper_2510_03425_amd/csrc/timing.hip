@@ -67,6 +67,7 @@ int set_repeat(const char* name, int times) {
       "rope_fwd", "qkv_post", "headnorm_bwd",       // q, k (or dq, dk) rotated / normalised
       "ce_chunk_stats", "ce_probs", "ce_dh_accum", "ce_final",  // LM-head running state
       "token_scores_grad_inplace", "distill_grad_inplace", "distill_row_inplace",      // logits -> their gradient
+      "rope_apply_inplace", "kv_append_inplace",                                       // heads -> turned heads
       "lora_adamw", "lora_grad_accumulate"};        // parameters, moments, accumulators
   for (const char* n : in_place)
     if (!strcmp(name, n)) return -1;

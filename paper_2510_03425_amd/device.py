@@ -184,6 +184,168 @@ def distill_topk(z: torch.Tensor, ids: Optional[torch.Tensor], logits: Optional[
     return row_loss
 
 
+# ---------------------------------------------------------------- a forward pass over a cache
+def heads_struct(x: torch.Tensor, like: Optional[torch.Tensor] = None, what: str = "x") -> L.MebpHeads:
+    """[tokens][heads][dim] fp32, fp16 or bf16 whose heads' elements follow one another, with any
+    distances between tokens and heads (on the device of ``like``)."""
+    dtype = LOGIT_TYPE.get(x.dtype)
+    if dtype is None or x.dim() != 3 or (x.stride(2) != 1 and x.shape[2] > 1):
+        raise ValueError(f"{what} must be fp32, fp16 or bf16 [tokens][heads][dim] with contiguous heads")
+    if not x.is_cuda or (like is not None and x.get_device() != like.get_device()):
+        raise ValueError(f"{what} must be on {'the GPU' if like is None else like.device}")
+    t, h, d = x.shape
+    return L.MebpHeads(x.data_ptr(), x.stride(0), x.stride(1), t, h, d, dtype)
+
+
+class Rope:
+    """The (cos, sin) of positions that a program keeps: ``table`` fp32 [positions][rot / 2][2], for heads
+    whose first ``rot`` elements turn, in halves or as interleaved neighbours."""
+
+    def __init__(self, table: torch.Tensor, dim: Optional[int] = None, interleaved: bool = False):
+        if table.dtype != torch.float32 or table.dim() != 3 or table.shape[2] != 2 or not table.is_contiguous() or not table.is_cuda:
+            raise ValueError("table must be contiguous fp32 [positions][rot / 2][2] on the GPU")
+        if dim is not None and 2 * table.shape[1] > dim:
+            raise ValueError(f"table turns {2 * table.shape[1]} elements of a head of {dim}")
+        self.table = table
+        self.struct = L.MebpRope(table.data_ptr(), 2 * table.shape[1], table.shape[0], int(interleaved))
+
+    @classmethod
+    def make(cls, n_pos: int, rot: int, theta: float = 1e4, interleaved: bool = False, factor: float = 1.0, original: int = 0,
+             low: float = 1.0, high: float = 32.0, gain: float = 1.0, device="cuda") -> "Rope":
+        """``mebp_rope_positions``: positions 0 .. n_pos - 1 of frequencies theta^(-2 j / rot), for a context
+        that is longer by ``factor``: all of them divided by it, or by parts where the ``original`` length
+        is given (pairs of less than ``low`` turns in it are divided, of more than ``high`` not)."""
+        r = cls(torch.empty((n_pos, rot // 2, 2), dtype=torch.float32, device=device), None, interleaved)
+        r.struct.rot = rot
+        with torch.cuda.device(r.table.device):
+            L.mebp_rope_positions(r.struct, L.MebpRopeScaling(theta, factor, original, low, high, gain), stream_handle())
+        return r
+
+
+@_on_device
+def _rope_apply(x, rope, positions, out, backward):
+    if rope.table.get_device() != x.get_device():
+        raise ValueError(f"the rope's table must be on {x.device}")
+    L.mebp_rope_apply(rope.struct, heads_struct(x), _operand(positions, torch.int32, (x.shape[0],), x, "positions"),
+                      heads_struct(out, x, "out"), backward, stream_handle())
+    return out
+
+
+def rope_apply(rope: Rope, x: torch.Tensor, positions: torch.Tensor, out: Optional[torch.Tensor] = None,
+               backward: bool = False) -> torch.Tensor:
+    """``mebp_rope_apply``: x [tokens][heads][dim] turned by int32 ``positions`` [tokens] into ``out`` (x itself
+    for one in place) or a new tensor; with ``backward`` the gradient w.r.t. x of one w.r.t. the result."""
+    return _rope_apply(x, rope, positions, torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out, backward)
+
+
+class KvCache:
+    """A paged cache: int8 ``pages`` [pages][kv heads][page tokens / 16][2][16 dim] and fp32 ``scales``
+    [pages][kv heads][page tokens / 16][2]."""
+
+    def __init__(self, pages: torch.Tensor, scales: torch.Tensor):
+        if pages.dtype != torch.int8 or pages.dim() != 5 or pages.shape[3] != 2 or pages.shape[4] % L.KV_BLOCK or not pages.is_contiguous() \
+                or not pages.is_cuda:
+            raise ValueError("pages must be contiguous int8 [pages][heads][blocks][2][16 dim] on the GPU")
+        _operand(scales, torch.float32, pages.shape[:4], pages, "scales")
+        self.pages, self.scales = pages, scales
+        n, h, blocks = pages.shape[:3]
+        self.struct = L.MebpKvCache(pages.data_ptr(), scales.data_ptr(), n, blocks * L.KV_BLOCK, h, pages.shape[4] // L.KV_BLOCK)
+
+    @classmethod
+    def empty(cls, n_pages: int, page_tokens: int, heads: int, dim: int, device="cuda") -> "KvCache":
+        """A pool of pages. What they hold before tokens are appended is never read as such."""
+        shape = (n_pages, heads, page_tokens // L.KV_BLOCK, 2)
+        return cls(torch.empty((*shape, L.KV_BLOCK * dim), dtype=torch.int8, device=device),
+                   torch.zeros(shape, dtype=torch.float32, device=device))
+
+
+class KvBatch:
+    """New tokens of some sequences: int32 ``start`` [sequences + 1] (their rows), ``past`` [sequences]
+    (tokens that are in the cache already) and ``table`` [sequences][columns] (their pages), on the device,
+    and the most new tokens and the longest length that a sequence may have (default: what the table holds of
+    `page_tokens` tokens a page)."""
+
+    def __init__(self, start: torch.Tensor, past: torch.Tensor, table: torch.Tensor, max_new: int,
+                 max_len: Optional[int] = None, page_tokens: Optional[int] = None):
+        if not past.is_cuda or table.dim() != 2 or table.dtype != torch.int32 or (table.shape[1] > 1 and table.stride(1) != 1) \
+                or table.get_device() != past.get_device() or table.shape[0] != past.shape[0]:
+            raise ValueError("table must be int32 [sequences][columns] with contiguous rows on past's device")
+        if max_len is None:
+            if page_tokens is None:
+                raise ValueError("max_len or page_tokens")
+            max_len = table.shape[1] * page_tokens
+        seqs, cols = table.shape
+        self.start, self.past, self.table = start, past, table
+        self.struct = L.MebpKvBatch(_operand(start, torch.int32, (seqs + 1,), past, "start"),
+                                    _operand(past, torch.int32, (seqs,), past, "past"), table.data_ptr(),
+                                    table.stride(0) if seqs > 1 else cols, cols, seqs, max_new, max_len)
+
+
+def _with(x: torch.Tensor, cache: KvCache, batch: KvBatch):
+    if cache.pages.get_device() != x.get_device() or batch.past.get_device() != x.get_device():
+        raise ValueError(f"cache and batch must be on {x.device}")
+
+
+@_on_device
+def _kv_append(k, cache, batch, v, rope, q, q_out):
+    _with(k, cache, batch)
+    if rope is not None and rope.table.get_device() != k.get_device():
+        raise ValueError(f"the rope's table must be on {k.device}")
+    if q is not None and q_out is None:
+        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    L.mebp_kv_append(cache.struct, batch.struct, None if rope is None else rope.struct, heads_struct(k, None, "k"),
+                     heads_struct(v, k, "v"), None if q is None else heads_struct(q, k, "q"),
+                     None if q_out is None else heads_struct(q_out, k, "q_out"), stream_handle())
+    return q_out
+
+
+def kv_append(cache: KvCache, batch: KvBatch, k: torch.Tensor, v: torch.Tensor, rope: Optional[Rope] = None,
+              q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
+    """``mebp_kv_append``: keys (turned by ``rope``) and values [tokens][kv heads][dim] into the cache, and
+    queries, if given, turned into ``q_out`` (q itself for that in place) or a new tensor."""
+    return _kv_append(k, cache, batch, v, rope, q, q_out)
+
+
+@_on_device
+def _kv_read(one, cache, batch, k, v):
+    _with(one, cache, batch)
+    L.mebp_kv_read(cache.struct, batch.struct, None if k is None else heads_struct(k, one, "k"),
+                   None if v is None else heads_struct(v, one, "v"), stream_handle())
+
+
+def kv_read(cache: KvCache, batch: KvBatch, k: Optional[torch.Tensor], v: Optional[torch.Tensor]):
+    """``mebp_kv_read``: tokens from ``batch.past`` of each sequence on back as numbers, into k and v
+    [rows][kv heads][dim] (either may be None)."""
+    if k is None and v is None:
+        raise ValueError("neither k nor v")
+    _kv_read(v if k is None else k, cache, batch, k, v)
+
+
+@_on_device
+def _kv_attention(q, cache, batch, out, lse, scale, window, ws):
+    _with(q, cache, batch)
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    hs, c, b = heads_struct(q, None, "q"), cache.struct, batch.struct
+    if ws is None:
+        n = L.mebp_kv_attention_workspace_bytes(b.seqs, b.max_new, b.max_len, hs.heads, c.heads, c.dim, window)
+        ws = torch.empty(max(n, 256), dtype=torch.uint8, device=q.device)
+    elif ws.get_device() != q.get_device() or not ws.is_contiguous():
+        raise ValueError(f"workspace must be contiguous on {q.device}")
+    L.mebp_kv_attention(c, b, hs, heads_struct(out, q, "out"),
+                        _operand(lse, torch.float32, (hs.tokens, hs.heads), q, "lse"), c.dim ** -0.5 if scale is None else scale,
+                        window, ws.data_ptr(), ws.nbytes, stream_handle())
+    return out
+
+
+def kv_attention(cache: KvCache, batch: KvBatch, q: torch.Tensor, out: Optional[torch.Tensor] = None,
+                 lse: Optional[torch.Tensor] = None, scale: Optional[float] = None, window: int = 0,
+                 ws: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """``mebp_kv_attention`` of queries [tokens][heads][dim] in fp16 or bf16 over the cache, causal, with a
+    ``window`` if that is above 0; ``scale`` 1 / sqrt(dim) by default; ``lse`` fp32 [tokens][heads] if wanted."""
+    return _kv_attention(q, cache, batch, out, lse, scale, window, ws)
+
+
 class DeviceModel:
     """A model's inputs resident in HBM plus the ABI structs that point at them."""
 
@@ -377,6 +539,53 @@ class DeviceModel:
                                   self.T, d, ptr(ck), ptr(self.loss),
                                   _operand(row_loss, torch.float32, (self.N,), ck, "row_loss"), self.grads, ptr(dx0),
                                   ptr(ws), ws.numel(), stream_handle())
+
+    # ---------------------------------------------------------------- a forward pass over a cache
+    def kv_caches(self, n_pages: int, page_tokens: int = 64) -> List[KvCache]:
+        """A pool of pages for each layer."""
+        return [KvCache.empty(n_pages, page_tokens, self.cfg.n_kv_heads, self.cfg.head_dim, self.device) for _ in range(self.L)]
+
+    def ropes(self, n_pos: int, **scaling) -> dict:
+        """The tables of the layers' rotary positions, by theta; ``scaling`` as in `Rope.make`."""
+        with torch.cuda.device(self.ws.device):
+            return {t: Rope.make(n_pos, self.cfg.head_dim, t, device=self.device, **scaling)
+                    for t in {self.cfg.layer_theta(l) for l in range(self.L)}}
+
+    def layer_forward_cached(self, l: int, x_in: torch.Tensor, x_out: torch.Tensor, cache: KvCache, batch: KvBatch, rope: Rope,
+                             ws: torch.Tensor):
+        rows = x_in.shape[0]
+        _with(x_in, cache, batch)
+        L.mebp_layer_forward_cached(self.ccfg, l, self.base[l], self.lora[l],
+                                    _operand(x_in, torch.float32, (rows, self.cfg.hidden), self.ws, "x_in"),
+                                    _operand(x_out, torch.float32, (rows, self.cfg.hidden), self.ws, "x_out"), rows, cache.struct,
+                                    batch.struct, rope.struct, ptr(ws), ws.numel(), stream_handle())
+
+    def cached_ws(self, rows: int, batch: KvBatch) -> torch.Tensor:
+        """A workspace of ``forward_cached`` for so many rows and such a batch."""
+        b = batch.struct
+        n = L.mebp_cached_workspace_bytes(self.ccfg, rows, b.seqs, b.max_new, b.max_len)
+        if n == 0:
+            raise L.MebpError(L.MEBP_EINVAL, "invalid shape for the workspace")
+        return torch.empty(n, dtype=torch.uint8, device=self.device)
+
+    def forward_cached(self, ids: torch.Tensor, caches: List[KvCache], batch: KvBatch, ropes: dict,
+                       ws: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """The last layer's output [rows][d] of new tokens, int32 ``ids`` [rows], behind what their sequences
+        have in the layers' ``caches``, which they join; `lm_head_logprobs` of its rows has the next tokens."""
+        if self.L == 0:
+            raise ValueError("this input set has no layers")
+        with torch.cuda.device(self.ws.device):
+            rows = ids.shape[0]
+            x, y = (torch.empty((rows, self.cfg.hidden), dtype=torch.float32, device=self.device) for _ in range(2))
+            if rows == 0:
+                return x
+            if ws is None:
+                ws = self.cached_ws(rows, batch)
+            L.mebp_embed(self.ccfg, self.emb, _operand(ids, torch.int32, (rows,), self.ws, "ids"), 1, rows, ptr(x), stream_handle())
+            for l in range(self.L):
+                self.layer_forward_cached(l, x, y, caches[l], batch, ropes[self.cfg.layer_theta(l)], ws)
+                x, y = y, x
+            return x
 
     def _x(self, x: torch.Tensor) -> int:
         return _operand(x, torch.float32, (x.shape[0], self.cfg.hidden), self.norm_final, "x")
