@@ -445,7 +445,7 @@ int mebp_rope_apply(const mebp_rope* rope, const mebp_heads* x, const int32_t* p
 typedef struct {
   int8_t* pages;     /* [n_pages][heads][page_tokens / 16][2][16 * dim], 16-byte aligned     */
   float* scales;     /* [n_pages][heads][page_tokens / 16][2], 8-byte aligned                */
-  int32_t n_pages;
+  int32_t n_pages;   /* n_pages * heads * page_tokens / 16 below 2^31                       */
   int32_t page_tokens; /* a power of two, 16 .. 65536                                       */
   int32_t heads;     /* kv heads, up to 1024                                                */
   int32_t dim;       /* 64, 128 or 256                                                      */

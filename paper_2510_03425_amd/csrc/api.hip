@@ -2535,6 +2535,8 @@ int check_cache(const mebp_kv_cache* c) {
   if (c->page_tokens < 16 || c->page_tokens > 65536 || (c->page_tokens & (c->page_tokens - 1)))
     return fail(MEBP_EUNSUPPORTED, "cache: page_tokens %d not a power of two in [16, 65536]", c->page_tokens);
   if (c->heads > kMaxHeads) return fail(MEBP_EUNSUPPORTED, "cache: heads %d above %d", c->heads, kMaxHeads);
+  if ((int64_t)c->n_pages * c->heads * (c->page_tokens / kKvBlock) >= (int64_t)1 << 31)
+    return fail(MEBP_EUNSUPPORTED, "cache: 2^31 blocks or more");
   if (!c->pages || !aligned(c->pages, 16)) return fail(MEBP_EINVAL, "cache: pages NULL or not 16-byte aligned");
   if (!c->scales || !aligned(c->scales, 8)) return fail(MEBP_EINVAL, "cache: scales NULL or not 8-byte aligned");
   return MEBP_OK;
@@ -2619,7 +2621,7 @@ int check_attention_shape(int seqs, int max_new, int max_len, int q_heads, int h
   if (dim != 64 && dim != 128 && dim != 256) return fail(MEBP_EUNSUPPORTED, "dim %d not in {64, 128, 256}", dim);
   if (window < 0) return fail(MEBP_EINVAL, "window %d < 0", window);
   const KvPlan p = kv_plan(seqs, max_new, max_len, q_heads, heads, dim, window);
-  if ((e = check_grid((int64_t)p.row_tiles * p.splits)) || (e = check_grid((int64_t)max_new * (q_heads / heads)))) return e;
+  if ((e = check_grid((int64_t)p.row_tiles * p.splits * std::max(seqs, 1) * heads)) || (e = check_grid((int64_t)max_new * (q_heads / heads)))) return e;
   return MEBP_OK;
 }
 KvAttnArgs attention_args(const mebp_kv_cache* c, const mebp_kv_batch* b, int rows, int q_heads, float scale, int window,

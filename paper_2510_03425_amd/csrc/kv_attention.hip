@@ -18,6 +18,8 @@
 #include "heads.h"
 #include "kv_device.h"
 
+#define DEVM __device__ __forceinline__
+
 namespace mebp {
 namespace {
 
@@ -25,6 +27,15 @@ namespace {
 // 2^11, and 2^15 with the scale of the values, relative to a reference within 2^4 above: in fp16's range,
 // 2^-14 below which it loses bits being 2^-19 of the row's largest weight or less.
 constexpr float kBias = 5.f, kLift = 6.f, kRefUp = 16.f, kRefDown = 1.f / 256.f;
+
+// (as a scalar, so that what depends on it alone is one)
+DEV int wave_id() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
+
+// 16 bytes that are read once (1 GiB of codes in tiles: 6.9 TB/s, 6.0 with ordinary loads)
+DEV uint4 stream16(const int8_t* p) {
+  typedef uint32_t run __attribute__((ext_vector_type(4)));
+  return __builtin_bit_cast(uint4, __builtin_nontemporal_load((const run*)p));
+}
 
 // 8 codes in 2 dwords -> 8 fp16: code + 128 below the bits of 1024, less 1152; exact.
 DEV f16x8 codes_f16(uint32_t lo, uint32_t hi) {
@@ -46,16 +57,26 @@ DEV Tiles tiles_of(int lo, int hi, int window) {
   return Tiles{window ? max(lo - window + 1, 0) >> 6 : 0, (hi >> 6) + 1};
 }
 
+// Keys that the query at a position sees, as one unsigned comparison: key - lo <= span.
+struct Seen {
+  int lo;
+  unsigned span;
+};
+DEV Seen keys_seen(int pos, int window) {
+  const int lo = window ? max(pos - window + 1, 0) : 0;
+  return Seen{lo, (unsigned)(pos - lo)};
+}
+
 // A row's queries as fp16 operands, scaled by a power of two to just below fp16's end (exact but for
-// elements 2^-28 of the largest), and what a score is to be multiplied by for it: NaN where the row has
-// a NaN or an infinity.
-template <class T, int NF>
-DEV float row_queries(const T* p, bool vec, float scale, f16x8 (&f)[NF], int g4) {
-  float x[NF][8], most = 0.f;
-  int bad = 0;
+// elements 2^-28 of the largest) and by the sign of `scale`, and what a score is to be multiplied by for it,
+// not negative: NaN where the row has a NaN or an infinity.
+// at(m): the lane's first element of operand m; LANES: of one row, this many apart.
+template <class T, int NF, int LANES, class At>
+DEV float queries(const T* p, bool vec, float scale, f16x8 (&f)[NF], At&& at) {
+  float x[NF][8];
 #pragma unroll
   for (int m = 0; m < NF; ++m) {
-    const T* e = p + 64 * (m / 2) + 16 * g4 + 8 * (m & 1);
+    const T* e = p + at(m);
     if (vec) {
       load8(e, x[m]);
     } else {
@@ -63,160 +84,330 @@ DEV float row_queries(const T* p, bool vec, float scale, f16x8 (&f)[NF], int g4)
       for (int i = 0; i < 8; ++i) x[m][i] = (float)e[i];
     }
   }
+  // (bits of magnitudes are ordered as the magnitudes, infinities and NaN above all)
+  uint32_t most = 0;
 #pragma unroll
   for (int m = 0; m < NF; ++m)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      most = fmaxf(most, fabsf(x[m][i]));
-      bad |= !(fabsf(x[m][i]) < INFINITY);
-    }
+    for (int i = 0; i < 8; ++i) most = max(most, __builtin_bit_cast(uint32_t, x[m][i]) & 0x7fffffffu);
 #pragma unroll
-  for (int o = 16; o < 64; o *= 2) {
-    most = fmaxf(most, __shfl_xor(most, o, 64));
-    bad |= __shfl_xor(bad, o, 64);
+  for (int o = LANES; o < 64; o *= 2) most = max(most, (uint32_t)__shfl_xor((int)most, o, 64));
+  const bool bad = most >= 0x7f800000u;
+  const int up = most && !bad ? 14 - ilogbf(__builtin_bit_cast(float, most)) : 0;
+#pragma unroll
+  for (int m = 0; m < NF; ++m)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[m][i] = (f16)__builtin_amdgcn_ldexpf(scale < 0.f ? -x[m][i] : x[m][i], up);
+  return bad ? NAN : __builtin_amdgcn_ldexpf(fabsf(scale), -up);
+}
+template <class T, int NF>
+DEV float row_queries(const T* p, bool vec, float scale, f16x8 (&f)[NF], int g4) {
+  return queries<T, NF, 16>(p, vec, scale, f, [&](int m) { return 64 * (m / 2) + 16 * g4 + 8 * (m & 1); });
+}
+template <class T, int NF>
+DEV float wide_queries(const T* p, bool vec, float scale, f16x8 (&f)[NF], int hi) {
+  return queries<T, NF, 32>(p, vec, scale, f, [&](int m) { return 16 * m + 8 * hi; });
+}
+
+// Lengths differ, so that the tiles of all sequences, heads and row tiles (the units) are dealt out in equal
+// shares: workgroup w takes places w n .. of the units in their order, and units that more than one share
+// has are joined by k_kv_join. (A grid of chunks up to the longest length took 1.5 times as long on 48
+// sequences of 1 to 8192 tokens: which compute units get the workgroups that have nothing to do is chance.)
+// A unit has kUnitCost places before those of its tiles, for what its start and end take.
+constexpr int kUnitCost = 6;
+struct KvShare {
+  int64_t u0, u1;  // its places
+  int64_t base;    // the first place of sequence s, the first that has some of them
+  int s;
+  KvSeq seq;
+};
+// tiles that the rows of one sequence see, and places of its units
+DEV Tiles seq_tiles(const KvSeq& q, int window) { return q.n ? tiles_of(q.past, q.past + q.n - 1, window) : Tiles{0, 0}; }
+DEV int64_t seq_places(const KvAttnArgs& a, const KvSeq& q) {
+  const Tiles t = seq_tiles(q, a.window);
+  return q.n ? (int64_t)a.c.heads * a.plan.row_tiles * (t.t1 - t.t0 + kUnitCost) : 0;
+}
+DEV int64_t share_size(int64_t places, int shares) {
+  return max((places + shares - 1) / shares, (int64_t)(4 + kUnitCost));  // (a tile for each wave)
+}
+// The share of this workgroup, or false where there is none; the first also keeps where sequences begin, in
+// a.first [seqs + 1].
+DEV bool find_share(const KvAttnArgs& a, KvShare& out) {
+  __shared__ int64_t wave_sum[4];
+  const int tid = threadIdx.x, per = (a.b.seqs + 255) / 256, s0 = tid * per, s1 = min(s0 + per, a.b.seqs);
+  int64_t mine = 0;
+  KvSeq q{0, 0, 0};
+  for (int s = s0; s < s1; ++s) mine += seq_places(a, q = kv_seq(a.b, s));
+  int64_t sum = mine;
+#pragma unroll
+  for (int o = 1; o < 64; o *= 2) {
+    const int64_t v = __shfl_up(sum, o, 64);
+    if ((tid & 63) >= o) sum += v;
   }
-  const int up = most > 0.f && !bad ? 14 - ilogbf(most) : 0;
+  if ((tid & 63) == 63) wave_sum[tid >> 6] = sum;
+  __syncthreads();
+  int64_t before = 0, all = 0;
 #pragma unroll
-  for (int m = 0; m < NF; ++m)
-#pragma unroll
-    for (int i = 0; i < 8; ++i) f[m][i] = (f16)ldexpf(x[m][i], up);
-  return bad ? NAN : ldexpf(scale, -up);
+  for (int w = 0; w < 4; ++w) {
+    before += w < (tid >> 6) ? wave_sum[w] : 0;
+    all += wave_sum[w];
+  }
+  const int64_t first = before + sum - mine, n = share_size(all, a.plan.shares), u0 = blockIdx.x * n;
+  if (blockIdx.x == 0 || (u0 >= first && u0 < first + mine)) {
+    int64_t at = first;
+    for (int s = s0; s < s1; ++s) {
+      if (per > 1) q = kv_seq(a.b, s);
+      const int64_t c = seq_places(a, q);
+      if (blockIdx.x == 0) a.first[s] = at;
+      if (u0 >= at && u0 < at + c) out = KvShare{u0, min(u0 + n, all), at, s, q};
+      at += c;
+    }
+  }
+  if (blockIdx.x == 0 && tid == 0) a.first[a.b.seqs] = all;
+  __syncthreads();
+  return u0 < all;
 }
 
 // Few rows: one workgroup of 4 waves takes NR * 16 rows (token, head of the group) of one sequence and kv
-// head over a chunk of its tiles, the waves one tile in four each; their sums meet in LDS.
+// head over a chunk of its tiles, the waves one tile of KT keys in four each; their sums meet in LDS.
+// D = 256 takes 32 keys at a time, so that two waves fit a SIMD's registers with a tile in flight each.
 template <class T, int D, int NR>
 __global__ __launch_bounds__(256, D * NR > 256 ? 1 : 2) void k_kv_rows(KvAttnArgs a, bool vec) {
   constexpr int NF = D / 32, NK = D / 16, R = 16 * NR;
+  constexpr bool QL = D == 256;  // queries in LDS, in the order of the operand (no registers to spare)
+  constexpr int KT = D == 256 ? 32 : 64, NT = KT / 16, KL = KT / 4, PT = 64 / KT;  // KL: keys of a lane's scores
   __shared__ float o_lds[4][R][D + 4];
   __shared__ float m_lds[4][R], l_lds[4][R], w_lds[4][R], ref_lds[4];
-  const int z = blockIdx.x % a.plan.splits, rt = blockIdx.x / a.plan.splits, h = blockIdx.y, s = blockIdx.z;
-  const KvSeq sq = kv_seq(a.b, s);
-  const int rows = sq.n * a.group, r0 = rt * R;
-  if (r0 >= rows) return;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r16 = lane & 15, g4 = lane >> 4;
+  __shared__ uint4 q_lds[QL ? NR * NF * 64 : 1];
+  __shared__ KvShare share_lds;
+  const int tid = threadIdx.x, lane = tid & 63, wave = wave_id(), r16 = lane & 15, g4 = lane >> 4;
+  const int units = a.c.heads * a.plan.row_tiles;
+  KvShare sh;
+  if (a.plan.shares) {
+    if (!find_share(a, share_lds)) return;
+    sh = share_lds;
+  } else {
+    // a chunk of one unit
+    sh.s = blockIdx.x / (units * a.plan.splits);
+    sh.seq = kv_seq(a.b, sh.s);
+    sh.u0 = 0;
+    sh.u1 = sh.seq.n ? 1 : 0;
+  }
+  for (int64_t at = sh.u0; at < sh.u1;) {
+  const KvSeq sq = sh.seq;
+  const int s = sh.s, rows = sq.n * a.group;
+  const Tiles range = seq_tiles(sq, a.window);
+  const int nt = range.t1 - range.t0;
+  int unit, off = 0, len = nt;
+  if (a.plan.shares) {
+    const int64_t rel = at - sh.base, per = nt + kUnitCost;
+    if (!sq.n || rel >= units * per) {
+      sh.base += seq_places(a, sq);
+      if (++sh.s == a.b.seqs) return;
+      sh.seq = kv_seq(a.b, sh.s);
+      continue;
+    }
+    unit = (int)(rel / per);
+    const int from = (int)(rel - unit * per), to = (int)min(per, from + sh.u1 - at);
+    at += to - from;
+    off = max(from - kUnitCost, 0);
+    len = to - kUnitCost - off;
+    if (len <= 0) continue;
+  } else {
+    unit = (int)(blockIdx.x / a.plan.splits % units);
+    off = blockIdx.x % a.plan.splits * a.plan.chunk;
+    len = min(a.plan.chunk, nt - off);
+    if (len <= 0) return;
+    at = sh.u1;
+  }
+  const int h = unit / a.plan.row_tiles, r0 = unit % a.plan.row_tiles * R;
+  if (r0 >= rows) continue;
   // rows behind the last one repeat it
   const int last = min(r0 + R, rows) - 1;
   const int pos_lo = sq.past + r0 / a.group, pos_hi = sq.past + last / a.group;
-  const Tiles range = tiles_of(pos_lo, pos_hi, a.window);
-  const int tb = range.t0 + z * a.plan.chunk, te = min(tb + a.plan.chunk, range.t1);
-  if (tb >= te) return;
+  const int tb = range.t0 + off, te = tb + len;
   const int nblk = (sq.past + sq.n + 15) >> 4;
+  const int k1 = te * PT;  // in tiles of KT keys
 
-  f16x8 qf[NR][NF];
+  // A tile's pages are looked up two of the wave's tiles ahead of its products, its keys loaded one ahead (into
+  // the registers that the scores have just been made from), its values as its scores are made. Blocks: the
+  // lane's as a row of the keys' operand (bk), and as a lane of the scores and the values (bv).
+  const int kb = KL * (r16 >> 2), vb = KL * g4;
+  typedef uint32_t vrun __attribute__((ext_vector_type(KL / 4)));
+  int ek, ev, iv_page;
+  uint32_t iv;
+  uint4 kr[NT * (D / 64)];
+  vrun vr[NK];
+  auto look_up = [&](int tile) {
+    tile = min(tile, k1 - 1) * (KT / 16);
+    ek = kv_entry(a.c, a.b, s, min(tile + kb / 16, nblk - 1));
+    ev = kv_entry(a.c, a.b, s, min(tile + vb / 16, nblk - 1));
+  };
+  auto load_keys = [&](int tile) {
+    tile = min(tile, k1 - 1) * (KT / 16);
+    const int bk = min(tile + kb / 16, nblk - 1), bv = min(tile + vb / 16, nblk - 1);
+    const int8_t* kp = a.c.codes + (uint64_t)kv_block(a.c, max(kv_page_of(a.c, a.b, ek, bk), 0), h, bk) * (32 * D) + (kb % 16 + (r16 & 3)) * D + g4 * 16;
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int j = 0; j < D / 64; ++j) kr[t * (D / 64) + j] = stream16(kp + t * 4 * D + j * 64);
+    iv_page = kv_page_of(a.c, a.b, ev, bv);
+    iv = kv_block(a.c, max(iv_page, 0), h, bv);
+  };
+  int tile = tb * PT + wave;
+  look_up(tile);
+  load_keys(tile);
+  look_up(tile + 4);
+
+  f16x8 qf[NR][QL ? 1 : NF];
   float qs[NR];
-  int pos[NR];
+  Seen see[NR];
 #pragma unroll
   for (int n = 0; n < NR; ++n) {
     const int r = min(r0 + n * 16 + r16, last), i = r / a.group, g = r - i * a.group;
-    pos[n] = sq.past + i;
+    see[n] = keys_seen(sq.past + i, a.window);
     const T* p = (const T*)a.q.p + (int64_t)(sq.row + i) * a.q.ld + (int64_t)(h * a.group + g) * a.q.hld;
-    qs[n] = row_queries(p, vec, a.scale, qf[n], g4);
+    if constexpr (QL) {
+      f16x8 f[NF];
+      qs[n] = row_queries(p, vec, a.scale, f, g4);
+      // (every wave has made the same ones)
+      if (wave == 0) {
+#pragma unroll
+        for (int i = 0; i < NF; ++i) q_lds[(n * NF + i) * 64 + lane] = __builtin_bit_cast(uint4, f[i]);
+      }
+    } else {
+      qs[n] = row_queries(p, vec, a.scale, qf[n], g4);
+    }
   }
+  if (QL) __syncthreads();
+  auto query = [&](int n, int i) {
+    if constexpr (QL)
+      return __builtin_bit_cast(f16x8, q_lds[(n * NF + i) * 64 + lane]);
+    else
+      return qf[n][i];
+  };
   f32x4 acc[NR][NK];
-  float m[NR], l[NR], ref = 1.f;
+  // As in k_kv_wide, the sums are scaled in an outer loop.
+  float m[NR], l[NR], by[NR], ref = 1.f;
 #pragma unroll
   for (int n = 0; n < NR; ++n) {
     m[n] = -FLT_MAX;
     l[n] = 0.f;
+    by[n] = 1.f;
 #pragma unroll
     for (int d = 0; d < NK; ++d) acc[n][d] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
-
-  for (int tile = tb + wave; tile < te; tile += 4) {
-    // the lane's block as a row of the keys' operand, and as a lane of the scores and the values
-    const int bk = min(tile * 4 + (r16 >> 2), nblk - 1), bv = min(tile * 4 + g4, nblk - 1);
-    const int pk = kv_page(a.c, a.b, s, bk), pv = kv_page(a.c, a.b, s, bv);
-    const int64_t ik = kv_block(a.c, max(pk, 0), h, bk), iv = kv_block(a.c, max(pv, 0), h, bv);
-    const int8_t* kp = a.c.codes + ik * (32 * D) + (r16 & 3) * D + g4 * 16;
-    const int8_t* vp = a.c.codes + iv * (32 * D) + 16 * D + r16 * 16;
-    float2 sc = ((const float2*)a.c.scales)[iv];
-    uint4 kr[NK], vr[NK];
+  bool fresh = true;  // (nothing to scale yet)
+  while (tile < k1) {
 #pragma unroll
-    for (int t = 0; t < 4; ++t)
+    for (int n = 0; n < NR; ++n)
 #pragma unroll
-      for (int j = 0; j < D / 64; ++j) kr[t * (D / 64) + j] = *(const uint4*)(kp + t * 4 * D + j * 64);
+      for (int d = 0; d < NK; ++d) acc[n][d] *= by[n];
+    do {
+      const int8_t* vp = a.c.codes + (uint64_t)iv * (32 * D) + 16 * D + r16 * 16 + vb % 16;
+      const float2 sc = ((const float2*)a.c.scales)[iv];
 #pragma unroll
-    for (int d = 0; d < NK; ++d) vr[d] = *(const uint4*)(vp + d * 256);
-    if (pv < 0) sc.x = sc.y = NAN;
-    f32x4 sa[NR][4];
+      for (int d = 0; d < NK; ++d) vr[d] = __builtin_nontemporal_load((const vrun*)(vp + d * 256));
+      __builtin_amdgcn_sched_barrier(0);  // (in flight while the scores are made)
+      f32x4 sa[NR][NT];
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {
+      for (int t = 0; t < NT; ++t)
 #pragma unroll
-      for (int n = 0; n < NR; ++n) sa[n][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int n = 0; n < NR; ++n) sa[n][t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int j = 0; j < D / 64; ++j) {
-        const uint4 c = kr[t * (D / 64) + j];
-        const f16x8 c0 = codes_f16(c.x, c.y), c1 = codes_f16(c.z, c.w);
+        f16x8 q[NR][2];
 #pragma unroll
         for (int n = 0; n < NR; ++n) {
-          sa[n][t] = mfma16(c0, qf[n][2 * j], sa[n][t]);
-          sa[n][t] = mfma16(c1, qf[n][2 * j + 1], sa[n][t]);
+          q[n][0] = query(n, 2 * j);
+          q[n][1] = query(n, 2 * j + 1);
+        }
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          const uint4 c = kr[t * (D / 64) + j];
+          const f16x8 c0 = codes_f16(c.x, c.y), c1 = codes_f16(c.z, c.w);
+#pragma unroll
+          for (int n = 0; n < NR; ++n) {
+            sa[n][t] = mfma16(c0, q[n][0], sa[n][t]);
+            sa[n][t] = mfma16(c1, q[n][1], sa[n][t]);
+          }
         }
       }
-    }
-    // the values' reference follows their scales
-    const bool masked = tile * 64 + 63 > pos_lo || (a.window && tile * 64 <= pos_hi - a.window);
-    const float sv = masked && !(tile * 64 + 16 * g4 <= pos_hi) ? 0.f : sc.y;
-    if (__ballot(sv > ref * kRefUp) || (!__ballot(sv > ref * kRefDown) && __ballot(sv > 0.f))) {
-      float mv = sv < INFINITY ? sv : 0.f;  // (NaN: no reference)
-      mv = fmaxf(mv, __shfl_xor(mv, 16, 64));
-      mv = fmaxf(mv, __shfl_xor(mv, 32, 64));
-      const float next = mv > 0.f ? ldexpf(1.f, ilogbf(mv)) : ref, by = ref / next;
-#pragma unroll
-      for (int n = 0; n < NR; ++n)
-#pragma unroll
-        for (int d = 0; d < NK; ++d) acc[n][d] *= by;
-      ref = next;
-    }
-    const float svr = sv / ref;
-    uint32_t pw[NR][8];
-#pragma unroll
-    for (int n = 0; n < NR; ++n) {
-      float x[16];
-      const float f = sc.x * qs[n];
-      float mx = -INFINITY;
-#pragma unroll
-      for (int k = 0; k < 16; ++k) {
-        x[k] = sa[n][k >> 2][k & 3] * f;
-        if (masked) {
-          const int key = tile * 64 + 16 * g4 + k;
-          if (key > pos[n] || (a.window && key <= pos[n] - a.window)) x[k] = -INFINITY;
-        }
-        mx = fmaxf(mx, x[k]);
-      }
-      if (__ballot(mx > m[n] + kLift)) {
-        mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-        mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-        const float next = fmaxf(m[n], mx), by = exp2_fast(m[n] - next);
-        m[n] = next;
-        l[n] *= by;
-#pragma unroll
-        for (int d = 0; d < NK; ++d) acc[n][d] *= by;
-      }
-      const float lift = kBias - m[n];
-#pragma unroll
-      for (int k = 0; k < 16; k += 2) {
-        const float p0 = exp2_fast(x[k] + lift), p1 = exp2_fast(x[k + 1] + lift);
-        l[n] += p0 + p1;
-        float w0 = p0 * svr, w1 = p1 * svr;
-        if (masked) {
-          // (the scale of a block that the row does not see may be NaN)
-          if (x[k] == -INFINITY) w0 = 0.f;
-          if (x[k + 1] == -INFINITY) w1 = 0.f;
-        }
-        pw[n][k / 2] = pack_f16x2(w0, w1);
-      }
-    }
-#pragma unroll
-    for (int d = 0; d < NK; ++d) {
-      const f16x8 v0 = codes_f16(vr[d].x, vr[d].y), v1 = codes_f16(vr[d].z, vr[d].w);
+      // the values' reference follows their scales, a row's its scores
+      const bool masked = tile * KT + KT - 1 > pos_lo || (a.window && tile * KT <= pos_hi - a.window);
+      const float sx = iv_page < 0 ? NAN : sc.x, sv = masked && tile * KT + vb > pos_hi ? 0.f : iv_page < 0 ? NAN : sc.y;
+      const bool far = __ballot(sv > ref * kRefUp) || (!__ballot(sv > ref * kRefDown) && __ballot(sv > 0.f));
+      bool move = far;
+      float mx[NR];
 #pragma unroll
       for (int n = 0; n < NR; ++n) {
-        acc[n][d] = mfma16(v0, __builtin_bit_cast(f16x8, make_uint4(pw[n][0], pw[n][1], pw[n][2], pw[n][3])), acc[n][d]);
-        acc[n][d] = mfma16(v1, __builtin_bit_cast(f16x8, make_uint4(pw[n][4], pw[n][5], pw[n][6], pw[n][7])), acc[n][d]);
+        const float f = sx * qs[n];
+        const int k0 = tile * KT + vb - see[n].lo;
+        mx[n] = -INFINITY;
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) sa[n][t][i] *= f;
+        if (masked) {
+#pragma unroll
+          for (int k = 0; k < KL; ++k)
+            sa[n][k >> 2][k & 3] = (unsigned)(k0 + k) <= see[n].span ? sa[n][k >> 2][k & 3] : -INFINITY;
+        }
+#pragma unroll
+        for (int k = 0; k < KL; ++k) mx[n] = fmaxf(mx[n], sa[n][k >> 2][k & 3]);
+        move |= __ballot(mx[n] > m[n] + kLift) != 0;
       }
-    }
+      if (move) {
+        float mv = sv < INFINITY ? sv : 0.f, next = ref;  // (NaN: no reference)
+        mv = fmaxf(mv, __shfl_xor(mv, 16, 64));
+        mv = fmaxf(mv, __shfl_xor(mv, 32, 64));
+        if (far && mv > 0.f) next = ldexpf(1.f, ilogbf(mv));
+#pragma unroll
+        for (int n = 0; n < NR; ++n) {
+          float x = fmaxf(mx[n], __shfl_xor(mx[n], 16, 64));
+          x = fmaxf(m[n], fmaxf(x, __shfl_xor(x, 32, 64)));
+          const float down = exp2_fast(m[n] - x);
+          m[n] = x;
+          l[n] *= down;
+          by[n] = down * (ref / next);
+        }
+        ref = next;
+        if (!fresh) break;
+      }
+      fresh = false;
+      const bool bad = masked && sv != sv;
+      const float svr = bad ? 0.f : sv / ref;
+      load_keys(tile + 4);
+      look_up(tile + 8);
+      __builtin_amdgcn_sched_barrier(0);
+      uint32_t pw[NR][KL / 2];
+#pragma unroll
+      for (int n = 0; n < NR; ++n) {
+        const float lift = kBias - m[n];
+#pragma unroll
+        for (int k = 0; k < KL; k += 2) {
+          const float p0 = exp2_fast(sa[n][k >> 2][k & 3] + lift), p1 = exp2_fast(sa[n][k >> 2][(k & 3) + 1] + lift);
+          l[n] += p0 + p1;
+          pw[n][k / 2] = pack_f16x2(p0 * svr, p1 * svr);
+        }
+        if (masked && __ballot(bad)) {
+          // values of NaN reach the rows that see one of their block's keys, and no others
+#pragma unroll
+          for (int k = 0; k < KL; ++k)
+            if (bad && sa[n][k >> 2][k & 3] != -INFINITY) pw[n][k / 2] |= k & 1 ? 0x7e000000u : 0x7e00u;
+        }
+      }
+#pragma unroll
+      for (int d = 0; d < NK; ++d)
+#pragma unroll
+        for (int u = 0; u < KL / 8; ++u) {
+          const f16x8 v = codes_f16(vr[d][2 * u], vr[d][2 * u + 1]);
+#pragma unroll
+          for (int n = 0; n < NR; ++n)
+            acc[n][d] = mfma16(v, __builtin_bit_cast(f16x8, make_uint4(pw[n][4 * u], pw[n][4 * u + 1], pw[n][4 * u + 2], pw[n][4 * u + 3])), acc[n][d]);
+        }
+      tile += 4;
+    } while (tile < k1);
   }
   // the waves' sums meet: lane holds dims 16 d + 4 g4 .. + 4 of its row
 #pragma unroll
@@ -245,14 +436,17 @@ __global__ __launch_bounds__(256, D * NR > 256 ? 1 : 2) void k_kv_rows(KvAttnArg
     l_lds[0][tid] = ll;
   }
   __syncthreads();
-  const int64_t part = ((((int64_t)s * a.c.heads + h) * a.plan.row_tiles + rt) * a.plan.splits + z) * a.part_rows;
+  // All of the unit's tiles: its rows are done. Else what there is of them is a part: a chunk's, or a share's
+  // first or second, the one for a unit that began before it, the other for one that goes on behind it.
+  const bool whole = a.plan.shares ? len == nt : a.plan.splits == 1;
+  const int64_t part = (a.plan.shares ? (int64_t)blockIdx.x * 2 + (off ? 0 : 1) : (int64_t)blockIdx.x) * a.part_rows;
   for (int i = tid; i < R * (D / 4); i += 256) {
     const int r = i / (D / 4), e = (i % (D / 4)) * 4;
     if (r0 + r > last) continue;
     f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int w = 0; w < 4; ++w) o += *(const f32x4*)&o_lds[w][r][e] * w_lds[w][r];
-    if (a.plan.splits > 1) {
+    if (!whole) {
       *(f32x4*)(a.part + (part + r) * (D + 4) + e) = o;
       if (e == 0) {
         a.part[(part + r) * (D + 4) + D] = m_lds[0][r];
@@ -269,42 +463,370 @@ __global__ __launch_bounds__(256, D * NR > 256 ? 1 : 2) void k_kv_rows(KvAttnArg
       a.lse[(int64_t)(sq.row + i_tok) * a.q_heads + h * a.group + g] =
           sq.past + i_tok >= a.b.max_len ? NAN : (m_lds[0][r] - kBias + log2f(ll)) * 0.6931471805599453f;
   }
+  __syncthreads();  // (before the next one's sums)
+  }
 }
 
-// Joins the chunks of each row: one workgroup a row.
-template <class T, int D, int R>
+// Many rows: one workgroup of 4 waves takes 128 rows, 32 a wave, whose queries and sums stay in registers; the
+// waves share tiles of KT keys [KT][D] and values [D][KT] in LDS, turned to fp16 there once. Products on
+// 32x32x16: S^T = K Q^T with row r of 32 as key r with bits 2 and 3 exchanged, so that a lane's 8 results
+// are 8 successive keys, the other operand of O^T += V^T P^T. A wave's products and its other work follow one
+// another unless they are of different tiles: the scores of tile t + 1 are made beside the weights of t, and
+// tile t + 2 is turned to fp16 beside the output's products of t, with three copies of the tile in LDS.
+DEV int bits23(int r) { return (r & ~12) | (r & 4) << 1 | (r & 8) >> 1; }
+
+template <int D>
+struct WideTile {
+  static constexpr int KT = D == 64 ? 64 : 32;  // (two sets of scores beside the sums)
+  // in 16 bytes: a row of keys, and of values, and one more, an odd number, so that the same column of 16 rows
+  // is in 16 bank groups
+  static constexpr int KC = D / 8 + 1, VC = KT / 8 + 1;
+  uint4 k[KT * KC], v[D * VC];
+  float2 sc[KT / 16];
+};
+
+// N products in a row, their LDS operands read FA products ahead, and behind each a piece of other work, which
+// runs beside it. (The order is held as it is written: left to itself the scheduler puts the products in one
+// row, each behind the wait for its own operand, and the other work behind them.)
+template <int N, class Read, class Mul, class Other>
+DEV void streamed(Read&& read, Mul&& mul, Other&& other) {
+  constexpr int FA = 4;
+  uint4 f[FA];
+#pragma unroll
+  for (int i = 0; i < FA; ++i) f[i] = read(i);
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const uint4 x = f[i % FA];
+    mul(i, x);
+    if (i + FA < N) f[i % FA] = read(i + FA);
+    other(i);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+}
+
+template <class T, int D>
+__global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_kv_wide(KvAttnArgs a, bool vec) {
+  using W = WideTile<D>;
+  constexpr int KT = W::KT, NU = KT / 32, NB = KT / 16, NF = D / 16, NO = D / 32, NC = KT * D / 4096, R = 128;
+  __shared__ W buf[3];
+  // Sequences and heads first, so that (where they are a multiple of 8) all row tiles of one run on one XCD and
+  // share its L2; the row tiles with the most keys begin. (With a head's row tiles behind one another, on one
+  // XCD too, the last head's longest begin late: 2 x 8192 tokens, 12 heads of 128, 730 us, so 566.)
+  const int pairs = a.c.heads * a.b.seqs, pair = blockIdx.x % pairs, x_id = blockIdx.x / pairs;
+  const int z = x_id % a.plan.splits, rt = a.plan.row_tiles - 1 - x_id / a.plan.splits, h = pair % a.c.heads, s = pair / a.c.heads;
+  const KvSeq sq = kv_seq(a.b, s);
+  const int rows = sq.n * a.group, r0 = rt * R;
+  if (r0 >= rows) return;
+  const int tid = threadIdx.x, lane = tid & 63, wave = wave_id(), c32 = lane & 31, hi = lane >> 5;
+  const int last = min(r0 + R, rows) - 1;
+  const int pos_lo = sq.past + r0 / a.group, pos_hi = sq.past + last / a.group;
+  const Tiles range = tiles_of(pos_lo, pos_hi, a.window);
+  const int tb = range.t0 + z * a.plan.chunk, te = min(tb + a.plan.chunk, range.t1);
+  if (tb >= te) return;
+  const int nblk = (sq.past + sq.n + 15) >> 4;
+  // in tiles of KT keys
+  const int k0 = tb * (64 / KT), k1 = min(te * (64 / KT), pos_hi / KT + 1);
+
+  const int row = min(r0 + wave * 32 + c32, last), tok = row / a.group, pos = sq.past + tok;
+  const int w_lo = sq.past + min(r0 + wave * 32, last) / a.group, w_hi = sq.past + min(r0 + wave * 32 + 31, last) / a.group;
+  // A tile goes through three stages: its pages looked up, its codes and scales loaded, both turned and
+  // written to LDS; a tile's products run beside all three of those behind it.
+  // Chunk i of this thread: 16 dims of a key, and 16 keys of a dim of values, of block (tid + 256 i) / D, which is
+  // the same for a wave. The scales of a block are written by the first lane of one wave that has it.
+  auto block_of = [&](int tile, int i) { return min(tile * NB + (wave * 64 + 256 * i) / D, nblk - 1); };
+  const int sc_i = NC > 1 ? wave & 1 : 0, sc_b = NC > 1 ? wave & 1 : wave * 64 / D;
+  const bool sc_mine = lane == 0 && (NC > 1 ? wave < 2 : wave * 64 % D == 0);
+  struct Raw {
+    uint4 k[NC], v[NC];
+    float2 sc;
+    bool ok;
+  } raw;
+  struct Entries {
+    int e[NC];
+  } next_pages;
+  auto look_up = [&](int tile) {
+    Entries pg;
+#pragma unroll
+    for (int i = 0; i < NC; ++i) pg.e[i] = kv_entry(a.c, a.b, s, block_of(tile, i));
+    return pg;
+  };
+  auto load = [&](Raw& r, const Entries& pg, int tile) {
+    uint32_t at = 0;
+#pragma unroll
+    for (int i = 0; i < NC; ++i) {
+      const int blk = block_of(tile, i), page = kv_page_of(a.c, a.b, __builtin_amdgcn_readfirstlane(pg.e[i]), blk);
+      const uint32_t x = kv_block(a.c, max(page, 0), h, blk);
+      const int8_t* p = a.c.codes + (uint64_t)x * (32 * D) + (uint32_t)((tid + 256 * i) % D * 16);
+      r.k[i] = *(const uint4*)p;
+      r.v[i] = *(const uint4*)(p + 16 * D);
+      if (i == sc_i) {
+        at = x;
+        r.ok = page >= 0;
+      }
+    }
+    r.sc = ((const float2*)a.c.scales)[at];
+  };
+  // piece j of 4 NC
+  auto store = [&](W& t, const Raw& r, int j) {
+    const int i = j >> 2, key = (tid + 256 * i) / (D / 16), c = (tid + 256 * i) % (D / 16) * 2;
+    const int dim = (tid + 256 * i) % D, b = (tid + 256 * i) / D * 2;
+    uint4* to = j & 2 ? &t.v[dim * W::VC + b] : &t.k[key * W::KC + c];
+    const uint4 x = j & 2 ? r.v[i] : r.k[i];
+    to[j & 1] = __builtin_bit_cast(uint4, j & 1 ? codes_f16(x.z, x.w) : codes_f16(x.x, x.y));
+  };
+  auto store_scales = [&](W& t, const Raw& r) {
+    if (sc_mine) t.sc[sc_b] = r.ok ? r.sc : make_float2(NAN, NAN);
+  };
+  auto store_all = [&](W& t, const Raw& r) {
+#pragma unroll
+    for (int j = 0; j < 4 * NC; ++j) store(t, r, j);
+    store_scales(t, r);
+  };
+  // (behind the last tile: that one again, for nobody)
+  auto tile_at = [&](int t) { return min(t, k1 - 1); };
+  // (the first three at once, and the queries' own loads beside them)
+  const Entries e0 = look_up(k0), e1 = look_up(tile_at(k0 + 1)), e2 = look_up(tile_at(k0 + 2));
+  next_pages = look_up(tile_at(k0 + 3));
+  Raw first, second;
+  load(first, e0, k0);
+  load(second, e1, tile_at(k0 + 1));
+  load(raw, e2, tile_at(k0 + 2));
+  f16x8 qf[NF];
+  const float qs = wide_queries<T, NF>((const T*)a.q.p + (int64_t)(sq.row + tok) * a.q.ld +
+                                           (int64_t)(h * a.group + row - tok * a.group) * a.q.hld, vec, a.scale, qf, hi);
+  store_all(buf[0], first);
+  store_all(buf[1], second);
+  f32x16 acc[NO];
+#pragma unroll
+  for (int d = 0; d < NO; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) acc[d][i] = 0.f;
+  const Seen see = keys_seen(pos, a.window);
+  float m = -FLT_MAX, l = 0.f, ref = 1.f, inv_ref = 1.f;
+
+  auto scores = [&](const W& t, f32x16 (&sa)[NU], auto&& other) {
+#pragma unroll
+    for (int u = 0; u < NU; ++u)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) sa[u][i] = 0.f;
+    streamed<NU * NF>(
+        [&](int i) { return t.k[(i % NU * 32 + bits23(c32)) * W::KC + 2 * (i / NU) + hi]; },
+        [&](int i, uint4 x) { sa[i % NU] = mfma32<OpF16>(x, __builtin_bit_cast(uint4, qf[i / NU]), sa[i % NU]); }, other);
+  };
+  f32x16 sn[NU];
+  __syncthreads();
+  scores(buf[0], sn, [](int) {});
+  // The sums are scaled in the outer loop, which a tile whose references have to move falls back to: inside the
+  // inner one nothing but the products touches them, so that they stay in the registers of the products
+  // (moving 128 of them there and back takes a third of a tile's time).
+  float by = 1.f;
+  bool moved = false;
+  int tile = k0, at = 0;
+  float x[NU][16], f[NB], sv[NB];
+  bool masked, bad;
+  // scores and scales of the tile, and whether a reference has to move for it
+  auto look = [&] {
+    const W& t = buf[at];
+    float most = 0.f;
+    masked = tile * KT + KT - 1 > w_lo || (a.window && tile * KT <= w_hi - a.window);
+    bad = false;  // a block of the tile has values of NaN
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      const float2 sc = t.sc[b];
+      f[b] = sc.x * qs;
+      sv[b] = masked && tile * KT + 16 * b > w_hi ? 0.f : sc.y;
+      bad |= sv[b] != sv[b];
+      most = fmaxf(most, sv[b] < INFINITY ? sv[b] : 0.f);
+    }
+#pragma unroll
+    for (int u = 0; u < NU; ++u)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) x[u][i] = sn[u][i] * f[2 * u + (i >> 3)];
+    if (masked) {
+#pragma unroll
+      for (int u = 0; u < NU; ++u)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int key = tile * KT + hi * 8 + u * 32 + (i >> 3) * 16 + (i & 7);
+          x[u][i] = (unsigned)(key - see.lo) <= see.span ? x[u][i] : -INFINITY;
+        }
+    }
+    float mx = -INFINITY;
+#pragma unroll
+    for (int u = 0; u < NU; ++u)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) mx = fmaxf(mx, x[u][i]);
+    const bool far = most > ref * kRefUp || (most > 0.f && most < ref * kRefDown);
+    if (!__ballot(mx > m + kLift || far)) return false;
+    const float nr = far ? ldexpf(1.f, ilogbf(most)) : ref;
+    mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+    const float nm = fmaxf(m, mx), down = exp2_fast(m - nm);
+    m = nm;
+    l *= down;
+    by = down * (ref / nr);
+    ref = nr;
+    inv_ref = 1.f / nr;
+    return true;
+  };
+  look();
+  while (tile < k1) {
+#pragma unroll
+    for (int d = 0; d < NO; ++d) acc[d] *= by;
+    do {
+      const int at1 = at == 2 ? 0 : at + 1, at2 = at == 0 ? 2 : at - 1;
+      const float lift = kBias - m;
+      uint32_t pw[NU * 8];
+      float up[NB], p0;
+#pragma unroll
+      for (int b = 0; b < NB; ++b) up[b] = masked && sv[b] != sv[b] ? 0.f : sv[b] * inv_ref;
+      constexpr int PS = 16 / NF > 1 ? 16 / NF : 1;  // weights to a product
+      scores(buf[at1], sn, [&](int j) {
+#pragma unroll
+        for (int i = j * PS; i < min((j + 1) * PS, NU * 16); ++i) {
+          const float p = exp2_fast(x[i >> 4][i & 15] + lift);
+          l += p;
+          if (i & 1)
+            pw[i >> 1] = pack_f16x2(p0 * up[i >> 3], p * up[i >> 3]);
+          else
+            p0 = p;
+        }
+      });
+      if (__ballot(masked && bad)) {
+        // values of NaN reach the rows that see one of their block's keys, and no others
+#pragma unroll
+        for (int u = 0; u < NU; ++u)
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            if (sv[2 * u + (i >> 3)] != sv[2 * u + (i >> 3)] && x[u][i] != -INFINITY)
+              pw[u * 8 + i / 2] |= i & 1 ? 0x7e000000u : 0x7e00u;
+      }
+      const W& t = buf[at];
+      constexpr int EV = NO * NB / (4 * NC);  // products to a piece of the tile after the next
+      streamed<NO * NB>(
+          [&](int i) { return t.v[(i % NO * 32 + c32) * W::VC + 2 * (i / NO) + hi]; },
+          [&](int i, uint4 v) {
+            const int u = 4 * (i / NO);
+            acc[i % NO] = mfma32<OpF16>(v, make_uint4(pw[u], pw[u + 1], pw[u + 2], pw[u + 3]), acc[i % NO]);
+          },
+          [&](int i) {
+            if (i % EV == 0) store(buf[at2], raw, i / EV);
+            if (i == NO * NB - 1) {
+              store_scales(buf[at2], raw);
+              load(raw, next_pages, tile_at(tile + 3));
+              next_pages = look_up(tile_at(tile + 4));
+            }
+          });
+      __syncthreads();
+      at = at1;
+      if (++tile == k1) break;
+      moved = look();
+    } while (!moved);
+  }
+  l += __shfl_xor(l, 32, 64);
+  if (r0 + wave * 32 + c32 > last) return;
+  // lane holds dims 32 d + 8 (q / 4) + 4 hi + q % 4 of its row
+  if (a.plan.splits > 1) {
+    float* p = a.part + (((((int64_t)s * a.c.heads + h) * a.plan.row_tiles + rt) * a.plan.splits + z) * a.part_rows + row - r0) * (D + 4);
+#pragma unroll
+    for (int d = 0; d < NO; ++d)
+#pragma unroll
+      for (int q = 0; q < 16; q += 4)
+        *(f32x4*)(p + d * 32 + 2 * q + 4 * hi) = f32x4{acc[d][q], acc[d][q + 1], acc[d][q + 2], acc[d][q + 3]} * ref;
+    if (hi == 0) {
+      p[D] = m;
+      p[D + 1] = l;
+    }
+    return;
+  }
+  const bool beyond = pos >= a.b.max_len;
+  const float inv = beyond ? NAN : l == 0.f ? 0.f : ref / l;
+  const int hq = h * a.group + row - tok * a.group;
+  T* o = (T*)a.out.p + (int64_t)(sq.row + tok) * a.out.ld + (int64_t)hq * a.out.hld;
+  typedef T run __attribute__((ext_vector_type(4)));
+  const bool runs = ((uintptr_t)o & 7) == 0;
+#pragma unroll
+  for (int d = 0; d < NO; ++d)
+#pragma unroll
+    for (int q = 0; q < 16; q += 4) {
+      run v;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = (T)(acc[d][q + i] * inv);
+      T* at = o + d * 32 + 2 * q + 4 * hi;
+      if (runs) {
+        *(run*)at = v;
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) at[i] = v[i];
+      }
+    }
+  if (hi == 0 && a.lse)
+    a.lse[(int64_t)(sq.row + tok) * a.q_heads + hq] = beyond ? NAN : (m - kBias + log2f(l)) * 0.6931471805599453f;
+}
+
+// Joins the parts of each row: one workgroup a row.
+template <class T, int D>
 __global__ __launch_bounds__(256) void k_kv_join(KvAttnArgs a) {
-  __shared__ float o_lds[256 / (D / 4)][D];
-  const int r = blockIdx.x, h = blockIdx.y, s = blockIdx.z;
+  constexpr int G = 256 / (D / 4);
+  __shared__ float o_lds[G][D];
+  __shared__ float l_lds[G];
+  const int R = a.plan.rows, r = blockIdx.x, h = blockIdx.y, s = blockIdx.z;
   const KvSeq sq = kv_seq(a.b, s);
   const int rows = sq.n * a.group;
   if (r >= rows) return;
-  const int rt = r / R, r0 = rt * R, last = min(r0 + R, rows) - 1;
-  const Tiles range = tiles_of(sq.past + r0 / a.group, sq.past + last / a.group, a.window);
-  const int nz = min((range.t1 - range.t0 + a.plan.chunk - 1) / a.plan.chunk, a.plan.splits);
-  const float* p = a.part + (((((int64_t)s * a.c.heads + h) * a.plan.row_tiles + rt) * a.plan.splits) * a.part_rows + r - r0) * (D + 4);
+  const int rt = r / R, r0 = rt * R;
   const int64_t step = (int64_t)a.part_rows * (D + 4);
-  constexpr int G = 256 / (D / 4);
+  const float *p, *p0;  // parts 1 .. and part 0
+  int nz;
+  if (a.plan.shares) {
+    const Tiles range = seq_tiles(sq, a.window);
+    const int nt = range.t1 - range.t0;
+    const int64_t n = share_size(a.first[a.b.seqs], a.plan.shares),
+                  u = a.first[s] + (int64_t)(h * a.plan.row_tiles + rt) * (nt + kUnitCost) + kUnitCost, w0 = u / n;
+    nz = (int)((u + nt - 1) / n - w0) + 1;
+    if (nz == 1) return;  // (one share has all of it, and has written it)
+    p = a.part + w0 * 2 * step + (int64_t)(r - r0) * (D + 4);
+    p0 = p + step;
+  } else {
+    const int last = min(r0 + R, rows) - 1;
+    const Tiles range = a.plan.wide ? tiles_of(sq.past + r0 / a.group, sq.past + last / a.group, a.window) : seq_tiles(sq, a.window);
+    nz = min((range.t1 - range.t0 + a.plan.chunk - 1) / a.plan.chunk, a.plan.splits);
+    p0 = p = a.part + ((((int64_t)s * a.c.heads + h) * a.plan.row_tiles + rt) * a.plan.splits) * step + (int64_t)(r - r0) * (D + 4);
+  }
+  const int64_t stride = a.plan.shares ? 2 * step : step;
+  auto at = [&](int z) { return z ? p + z * stride : p0; };
   const int e = (threadIdx.x % (D / 4)) * 4, zg = threadIdx.x / (D / 4);
   float mm = -FLT_MAX;
-  for (int z = threadIdx.x & 63; z < nz; z += 64) mm = fmaxf(mm, p[z * step + D]);
+  for (int z = threadIdx.x & 63; z < nz; z += 64) mm = fmaxf(mm, at(z)[D]);
   mm = wave_max(mm);
   f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
   float ll = 0.f;
-  for (int z = zg; z < nz; z += G) {
-    const float w = exp2_fast(p[z * step + D] - mm);
-    o += *(const f32x4*)(p + z * step + e) * w;
-    ll += w * p[z * step + D + 1];
+  constexpr int U = 4;  // parts in flight
+  for (int z0 = zg; z0 < nz; z0 += G * U) {
+    f32x4 x[U];
+    float2 ml[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const float* c = at(min(z0 + u * G, nz - 1));
+      x[u] = *(const f32x4*)(c + e);
+      ml[u] = *(const float2*)(c + D);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (z0 + u * G >= nz) break;
+      const float w = exp2_fast(ml[u].x - mm);
+      o += x[u] * w;
+      ll += w * ml[u].y;
+    }
   }
   *(f32x4*)&o_lds[zg][e] = o;
-  __shared__ float lz[G];
-  if (e == 0) lz[zg] = ll;
+  if (e == 0) l_lds[zg] = ll;
   __syncthreads();
   if (threadIdx.x >= D) return;
   float sum = 0.f, tot = 0.f;
+#pragma unroll
   for (int g = 0; g < G; ++g) {
     sum += o_lds[g][threadIdx.x];
-    tot += lz[g];
+    tot += l_lds[g];
   }
   const int i = r / a.group, g = r - i * a.group;
   const bool beyond = sq.past + i >= a.b.max_len;
@@ -317,20 +839,22 @@ __global__ __launch_bounds__(256) void k_kv_join(KvAttnArgs a) {
 template <class T, int D>
 hipError_t kv_attention(const KvAttnArgs& a, hipStream_t st) {
   const bool vec = vectors(a.q, 2);
-  const dim3 grid((unsigned)a.plan.row_tiles * a.plan.splits, (unsigned)a.c.heads, (unsigned)a.b.seqs);
   // (what it reads depends on lengths that are on the device)
   const double most = (double)a.b.seqs * a.b.max_len * a.c.heads * 2 * D;
-  if (a.plan.rows == 16)
-    MEBP_TIMED(st, "kv_rows", 0.0, most, hipLaunchKernelGGL((k_kv_rows<T, D, 1>), grid, dim3(256), 0, st, a, vec));
-  else
-    MEBP_TIMED(st, "kv_rows", 0.0, most, hipLaunchKernelGGL((k_kv_rows<T, D, 2>), grid, dim3(256), 0, st, a, vec));
+  if (a.plan.wide) {
+    const dim3 grid((unsigned)a.plan.row_tiles * a.plan.splits * a.c.heads * a.b.seqs);
+    MEBP_TIMED(st, "kv_wide", 0.0, most, hipLaunchKernelGGL((k_kv_wide<T, D>), grid, dim3(256), 0, st, a, vec));
+  } else {
+    const dim3 grid(a.plan.shares ? (unsigned)a.plan.shares : (unsigned)(a.b.seqs * a.c.heads * a.plan.row_tiles * a.plan.splits));
+    if (a.plan.rows == 16)
+      MEBP_TIMED(st, "kv_rows", 0.0, most, hipLaunchKernelGGL((k_kv_rows<T, D, 1>), grid, dim3(256), 0, st, a, vec));
+    else if constexpr (D == 64)
+      MEBP_TIMED(st, "kv_rows", 0.0, most, hipLaunchKernelGGL((k_kv_rows<T, D, 2>), grid, dim3(256), 0, st, a, vec));
+  }
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess || a.plan.splits == 1) return e;
+  if (e != hipSuccess || (a.plan.splits == 1 && !a.plan.shares)) return e;
   const dim3 rows((unsigned)a.b.max_new * a.group, (unsigned)a.c.heads, (unsigned)a.b.seqs);
-  if (a.plan.rows == 16)
-    MEBP_TIMED(st, "kv_join", 0.0, 0.0, hipLaunchKernelGGL((k_kv_join<T, D, 16>), rows, dim3(256), 0, st, a));
-  else
-    MEBP_TIMED(st, "kv_join", 0.0, 0.0, hipLaunchKernelGGL((k_kv_join<T, D, 32>), rows, dim3(256), 0, st, a));
+  MEBP_TIMED(st, "kv_join", 0.0, 0.0, hipLaunchKernelGGL((k_kv_join<T, D>), rows, dim3(256), 0, st, a));
   return hipGetLastError();
 }
 }  // namespace
@@ -338,29 +862,36 @@ hipError_t kv_attention(const KvAttnArgs& a, hipStream_t st) {
 KvPlan kv_plan(int seqs, int max_new, int max_len, int q_heads, int heads, int dim, int window) {
   KvPlan p{};
   const int64_t rows = (int64_t)max_new * (q_heads / heads);
-  p.rows = rows <= 16 ? 16 : 32;
+  p.wide = rows > 64;
+  p.rows = p.wide ? 128 : rows <= 16 || dim > 64 ? 16 : 32;
   p.row_tiles = (int)((rows + p.rows - 1) / p.rows);
+  p.splits = 1;
   // tiles that a row tile's queries see at most
-  const int64_t span = window ? std::min<int64_t>((int64_t)window + p.rows + 126, max_len) : max_len;
-  const int64_t tiles = (span + 63) / 64;
-  const int64_t groups = (int64_t)p.row_tiles * heads * std::max(seqs, 1);
-  // about 1024 workgroups, a tile to each wave at least
-  const int64_t want = std::max<int64_t>(1, 1024 / groups);
-  int64_t chunk = (tiles + want - 1) / want;
-  chunk = std::max<int64_t>(4, (chunk + 3) / 4 * 4);
+  const int64_t span = window ? std::min<int64_t>((int64_t)window + (p.wide ? p.rows : max_new) + 126, max_len) : max_len;
+  const int64_t tiles = (span + 63) / 64, groups = (int64_t)p.row_tiles * heads * std::max(seqs, 1);
+  // few rows of several sequences that are more than two workgroups a compute unit: equal shares
+  if (!p.wide && seqs > 1 && groups * ((tiles + 3) / 4) > 512) {
+    p.shares = 512;
+    return p;
+  }
+  const int64_t want = std::max<int64_t>(1, 256 / groups);
+  int64_t chunk = std::max<int64_t>(4, (tiles + want - 1) / want);
+  if (!p.wide) chunk = (chunk + 3) / 4 * 4;
   p.chunk = (int)chunk;
   p.splits = (int)((tiles + chunk - 1) / chunk);
   return p;
 }
 
+// the parts, and behind them (shares) the places of the sequences' first tiles
 size_t kv_part_floats(const KvPlan& p, int seqs, int max_new, int q_heads, int heads, int dim) {
-  if (p.splits <= 1) return 0;
-  const size_t part_rows = std::min<int64_t>(p.rows, (int64_t)max_new * (q_heads / heads));
-  return (size_t)seqs * heads * p.row_tiles * p.splits * part_rows * (dim + 4);
+  const size_t part_rows = std::min<int64_t>(p.rows, (int64_t)max_new * (q_heads / heads)), row = part_rows * (dim + 4);
+  if (p.shares) return (size_t)p.shares * 2 * row + ((size_t)seqs + 1) * 2;
+  return p.splits <= 1 ? 0 : (size_t)seqs * heads * p.row_tiles * p.splits * row;
 }
 
 hipError_t launch_kv_attention(KvAttnArgs a, int dtype, hipStream_t st) {
   a.part_rows = (int)std::min<int64_t>(a.plan.rows, (int64_t)a.b.max_new * a.group);
+  a.first = (int64_t*)(a.part + (size_t)a.plan.shares * 2 * a.part_rows * (a.c.dim + 4));
   auto go = [&](auto d) {
     constexpr int D = decltype(d)::value;
     return dtype == LOGIT_F16 ? kv_attention<f16, D>(a, st) : kv_attention<bf16, D>(a, st);

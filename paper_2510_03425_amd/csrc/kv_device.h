@@ -23,9 +23,17 @@ DEV int kv_page(const KvPages& c, const KvRows& b, int s, int blk) {
   const int p = b.table[s * b.table_ld + col];
   return (unsigned)p < (unsigned)c.n_pages ? p : -1;
 }
-// Index of a block of head h among all blocks of the pool.
-DEV int64_t kv_block(const KvPages& c, int page, int h, int blk) {
-  return (((int64_t)page * c.heads + h) << c.log_blocks) + (blk & ((1 << c.log_blocks) - 1));
+// The same in two steps, for lookups ahead of their use: what the table says (of its nearest column), and what
+// that is worth.
+DEV int kv_entry(const KvPages& c, const KvRows& b, int s, int blk) {
+  return b.table[s * b.table_ld + min(blk >> c.log_blocks, b.cols - 1)];
+}
+DEV int kv_page_of(const KvPages& c, const KvRows& b, int entry, int blk) {
+  return (blk >> c.log_blocks) < b.cols && (unsigned)entry < (unsigned)c.n_pages ? entry : -1;
+}
+// Index of a block of head h among all blocks of the pool, fewer than 2^31 (its bytes take 64 bits).
+DEV uint32_t kv_block(const KvPages& c, int page, int h, int blk) {
+  return (((uint32_t)page * c.heads + h) << c.log_blocks) + (blk & ((1 << c.log_blocks) - 1));
 }
 
 }  // namespace mebp

@@ -183,7 +183,7 @@ __global__ __launch_bounds__(256) void k_kv_append(KvAppendArgs a, bool vk, bool
   const int h = key ? role : role - a.c.heads;
   const int page = kv_page(a.c, a.b, s, blk);
   if (page < 0) return;
-  const int64_t block = kv_block(a.c, page, h, blk);
+  const uint64_t block = kv_block(a.c, page, h, blk);
   int8_t* out = a.c.codes + block * (2 * 16 * D) + (key ? 0 : 16 * D);
   float* scale_at = a.c.scales + block * 2 + (key ? 0 : 1);
   const float old = t_lo > 0 ? *scale_at : 0.f;
@@ -281,7 +281,7 @@ __global__ __launch_bounds__(256) void k_kv_read(KvReadArgs a) {
   const HeadsView& v = key ? a.k : a.v;
   if (!v.p) return;
   const int page = kv_page(a.c, a.b, s, blk);
-  const int64_t at = kv_block(a.c, max(page, 0), h, blk);
+  const uint64_t at = kv_block(a.c, max(page, 0), h, blk);
   const int8_t* in = a.c.codes + at * (2 * 16 * D) + (key ? 0 : 16 * D);
   const float scale = page < 0 ? NAN : a.c.scales[at * 2 + (key ? 0 : 1)];
   for (int i = threadIdx.x; i < 16 * D; i += 256) {

@@ -490,11 +490,12 @@ struct KvReadArgs {
   int nblk;
 };
 hipError_t launch_kv_read(const KvReadArgs& a, int dtype, hipStream_t st);
-// Launch plan of an attention: `rows` query rows (token, head of the group) per workgroup, and chunks of
-// `chunk` 64-key tiles, `splits` of them at most over a sequence (1: no partial results).
+// Launch plan of an attention: `rows` query rows (token, head of the group) per workgroup. k_kv_rows: all
+// tiles of 64 keys in so many shares (0: a workgroup for each row tile). k_kv_wide: chunks of `chunk` tiles,
+// `splits` of them at most over a sequence (1: no partial results).
 struct KvPlan {
-  bool wide;               // k_kv_wide, else k_kv_rows
-  int rows, row_tiles, splits, chunk;
+  bool wide;
+  int rows, row_tiles, shares, splits, chunk;
 };
 KvPlan kv_plan(int seqs, int max_new, int max_len, int q_heads, int heads, int dim, int window);
 size_t kv_part_floats(const KvPlan& p, int seqs, int max_new, int q_heads, int heads, int dim);
@@ -507,7 +508,8 @@ struct KvAttnArgs {
   float scale;             // times log2(e)
   KvPlan plan;
   float* part;             // kv_part_floats
-  int part_rows;           // set by the launcher
+  int part_rows;           // set by the launcher, as first
+  int64_t* first;
 };
 hipError_t launch_kv_attention(KvAttnArgs a, int dtype, hipStream_t st);
 
