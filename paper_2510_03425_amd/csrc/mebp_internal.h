@@ -480,7 +480,7 @@ struct KvAppendArgs {
   int q_heads, nblk;       // nblk: blocks that a sequence's new tokens touch at most
   f16* rest;               // [rows][rest_cols], whose rows behind the last sequence are cleared; null: nothing is
   int rest_cols;           // a multiple of 8
-  int q_per, q_groups;     // set by the launcher
+  int q_groups;            // set by the launcher
 };
 hipError_t launch_kv_append(KvAppendArgs a, int dtype, hipStream_t st);
 struct KvReadArgs {

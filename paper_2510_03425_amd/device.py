@@ -185,16 +185,29 @@ def distill_topk(z: torch.Tensor, ids: Optional[torch.Tensor], logits: Optional[
 
 
 # ---------------------------------------------------------------- a forward pass over a cache
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
 def heads_struct(x: torch.Tensor, like: Optional[torch.Tensor] = None, what: str = "x") -> L.MebpHeads:
     """[tokens][heads][dim] fp32, fp16 or bf16 whose heads' elements follow one another, with any
     distances between tokens and heads (on the device of ``like``)."""
     dtype = LOGIT_TYPE.get(x.dtype)
-    if dtype is None or x.dim() != 3 or (x.stride(2) != 1 and x.shape[2] > 1):
-        raise ValueError(f"{what} must be fp32, fp16 or bf16 [tokens][heads][dim] with contiguous heads")
+    if dtype is None or x.dim() != 3:
+        raise ValueError(f"{what} must be fp32, fp16 or bf16 [tokens][heads][dim]")
+    ld, head_ld, one = x.stride()
+    t, h, d = x.shape
+    if one != 1 and d > 1:
+        raise ValueError(f"{what} must have contiguous heads")
     if not x.is_cuda or (like is not None and x.get_device() != like.get_device()):
         raise ValueError(f"{what} must be on {'the GPU' if like is None else like.device}")
-    t, h, d = x.shape
-    return L.MebpHeads(x.data_ptr(), x.stride(0), x.stride(1), t, h, d, dtype)
+    return L.MebpHeads(x.data_ptr(), ld, head_ld, t, h, d, dtype)
+
+
+def _stream_of(x: torch.Tensor) -> int:
+    """torch's current stream on the device of x."""
+    if _raw_stream is None:
+        return torch.cuda.current_stream(x.device).cuda_stream
+    return _raw_stream(x.get_device())
 
 
 class Rope:
@@ -222,20 +235,21 @@ class Rope:
         return r
 
 
-@_on_device
-def _rope_apply(x, rope, positions, out, backward):
-    if rope.table.get_device() != x.get_device():
-        raise ValueError(f"the rope's table must be on {x.device}")
-    L.mebp_rope_apply(rope.struct, heads_struct(x), _operand(positions, torch.int32, (x.shape[0],), x, "positions"),
-                      heads_struct(out, x, "out"), backward, stream_handle())
-    return out
-
-
 def rope_apply(rope: Rope, x: torch.Tensor, positions: torch.Tensor, out: Optional[torch.Tensor] = None,
                backward: bool = False) -> torch.Tensor:
     """``mebp_rope_apply``: x [tokens][heads][dim] turned by int32 ``positions`` [tokens] into ``out`` (x itself
     for one in place) or a new tensor; with ``backward`` the gradient w.r.t. x of one w.r.t. the result."""
-    return _rope_apply(x, rope, positions, torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out, backward)
+    xs = heads_struct(x)
+    if x.get_device() != _current_device():
+        with torch.cuda.device(x.device):
+            return rope_apply(rope, x, positions, out, backward)
+    if rope.table.get_device() != x.get_device():
+        raise ValueError(f"the rope's table must be on {x.device}")
+    if out is None:
+        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    L.mebp_rope_apply(rope.struct, xs, _operand(positions, torch.int32, (xs.tokens,), x, "positions"),
+                      xs if out is x else heads_struct(out, x, "out"), backward, _stream_of(x))
+    return out
 
 
 class KvCache:
@@ -282,60 +296,46 @@ class KvBatch:
 
 
 def _with(x: torch.Tensor, cache: KvCache, batch: KvBatch):
-    if cache.pages.get_device() != x.get_device() or batch.past.get_device() != x.get_device():
+    dev = x.get_device()
+    if cache.pages.get_device() != dev or batch.past.get_device() != dev:
         raise ValueError(f"cache and batch must be on {x.device}")
-
-
-@_on_device
-def _kv_append(k, cache, batch, v, rope, q, q_out):
-    _with(k, cache, batch)
-    if rope is not None and rope.table.get_device() != k.get_device():
-        raise ValueError(f"the rope's table must be on {k.device}")
-    if q is not None and q_out is None:
-        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    L.mebp_kv_append(cache.struct, batch.struct, None if rope is None else rope.struct, heads_struct(k, None, "k"),
-                     heads_struct(v, k, "v"), None if q is None else heads_struct(q, k, "q"),
-                     None if q_out is None else heads_struct(q_out, k, "q_out"), stream_handle())
-    return q_out
 
 
 def kv_append(cache: KvCache, batch: KvBatch, k: torch.Tensor, v: torch.Tensor, rope: Optional[Rope] = None,
               q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
     """``mebp_kv_append``: keys (turned by ``rope``) and values [tokens][kv heads][dim] into the cache, and
     queries, if given, turned into ``q_out`` (q itself for that in place) or a new tensor."""
-    return _kv_append(k, cache, batch, v, rope, q, q_out)
-
-
-@_on_device
-def _kv_read(one, cache, batch, k, v):
-    _with(one, cache, batch)
-    L.mebp_kv_read(cache.struct, batch.struct, None if k is None else heads_struct(k, one, "k"),
-                   None if v is None else heads_struct(v, one, "v"), stream_handle())
+    ks = heads_struct(k, None, "k")
+    if k.get_device() != _current_device():
+        with torch.cuda.device(k.device):
+            return kv_append(cache, batch, k, v, rope, q, q_out)
+    _with(k, cache, batch)
+    if rope is not None and rope.table.get_device() != k.get_device():
+        raise ValueError(f"the rope's table must be on {k.device}")
+    qs = os = None
+    if q is not None:
+        qs = heads_struct(q, k, "q")
+        if q_out is None:
+            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    if q_out is not None:
+        os = qs if q_out is q else heads_struct(q_out, k, "q_out")
+    L.mebp_kv_append(cache.struct, batch.struct, None if rope is None else rope.struct, ks, heads_struct(v, k, "v"), qs, os,
+                     _stream_of(k))
+    return q_out
 
 
 def kv_read(cache: KvCache, batch: KvBatch, k: Optional[torch.Tensor], v: Optional[torch.Tensor]):
     """``mebp_kv_read``: tokens from ``batch.past`` of each sequence on back as numbers, into k and v
     [rows][kv heads][dim] (either may be None)."""
-    if k is None and v is None:
+    one = v if k is None else k
+    if one is None:
         raise ValueError("neither k nor v")
-    _kv_read(v if k is None else k, cache, batch, k, v)
-
-
-@_on_device
-def _kv_attention(q, cache, batch, out, lse, scale, window, ws):
-    _with(q, cache, batch)
-    if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    hs, c, b = heads_struct(q, None, "q"), cache.struct, batch.struct
-    if ws is None:
-        n = L.mebp_kv_attention_workspace_bytes(b.seqs, b.max_new, b.max_len, hs.heads, c.heads, c.dim, window)
-        ws = torch.empty(max(n, 256), dtype=torch.uint8, device=q.device)
-    elif ws.get_device() != q.get_device() or not ws.is_contiguous():
-        raise ValueError(f"workspace must be contiguous on {q.device}")
-    L.mebp_kv_attention(c, b, hs, heads_struct(out, q, "out"),
-                        _operand(lse, torch.float32, (hs.tokens, hs.heads), q, "lse"), c.dim ** -0.5 if scale is None else scale,
-                        window, ws.data_ptr(), ws.nbytes, stream_handle())
-    return out
+    ks, vs = (None if x is None else heads_struct(x, one, w) for x, w in ((k, "k"), (v, "v")))
+    if one.get_device() != _current_device():
+        with torch.cuda.device(one.device):
+            return kv_read(cache, batch, k, v)
+    _with(one, cache, batch)
+    L.mebp_kv_read(cache.struct, batch.struct, ks, vs, _stream_of(one))
 
 
 def kv_attention(cache: KvCache, batch: KvBatch, q: torch.Tensor, out: Optional[torch.Tensor] = None,
@@ -343,7 +343,22 @@ def kv_attention(cache: KvCache, batch: KvBatch, q: torch.Tensor, out: Optional[
                  ws: Optional[torch.Tensor] = None) -> torch.Tensor:
     """``mebp_kv_attention`` of queries [tokens][heads][dim] in fp16 or bf16 over the cache, causal, with a
     ``window`` if that is above 0; ``scale`` 1 / sqrt(dim) by default; ``lse`` fp32 [tokens][heads] if wanted."""
-    return _kv_attention(q, cache, batch, out, lse, scale, window, ws)
+    qs = heads_struct(q, None, "q")
+    if q.get_device() != _current_device():
+        with torch.cuda.device(q.device):
+            return kv_attention(cache, batch, q, out, lse, scale, window, ws)
+    _with(q, cache, batch)
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    c, b = cache.struct, batch.struct
+    if ws is None:
+        n = L.mebp_kv_attention_workspace_bytes(b.seqs, b.max_new, b.max_len, qs.heads, c.heads, c.dim, window)
+        ws = torch.empty(max(n, 256), dtype=torch.uint8, device=q.device)
+    elif ws.get_device() != q.get_device() or not ws.is_contiguous():
+        raise ValueError(f"workspace must be contiguous on {q.device}")
+    L.mebp_kv_attention(c, b, qs, heads_struct(out, q, "out"), _operand(lse, torch.float32, (qs.tokens, qs.heads), q, "lse"),
+                        c.dim ** -0.5 if scale is None else scale, window, ws.data_ptr(), ws.nbytes, _stream_of(q))
+    return out
 
 
 class DeviceModel:
