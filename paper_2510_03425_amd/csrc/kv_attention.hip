@@ -71,19 +71,30 @@ DEV Seen keys_seen(int pos, int window) {
 // elements 2^-28 of the largest) and by the sign of `scale`, and what a score is to be multiplied by for it,
 // not negative: NaN where the row has a NaN or an infinity.
 // at(m): the lane's first element of operand m; LANES: of one row, this many apart.
-template <class T, int NF, int LANES, class At>
-DEV float queries(const T* p, bool vec, float scale, f16x8 (&f)[NF], At&& at) {
-  float x[NF][8];
+template <class T>
+struct Eight {
+  typedef T run __attribute__((ext_vector_type(8)));
+};
+template <class T, int NF, class At>
+DEV void load_queries(const T* p, bool vec, typename Eight<T>::run (&x)[NF], At&& at) {
 #pragma unroll
   for (int m = 0; m < NF; ++m) {
     const T* e = p + at(m);
     if (vec) {
-      load8(e, x[m]);
+      x[m] = *(const typename Eight<T>::run*)e;
     } else {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) x[m][i] = (float)e[i];
+      for (int i = 0; i < 8; ++i) x[m][i] = e[i];
     }
   }
+}
+template <class T, int NF, int LANES>
+DEV float queries(const typename Eight<T>::run (&raw)[NF], float scale, f16x8 (&f)[NF]) {
+  float x[NF][8];
+#pragma unroll
+  for (int m = 0; m < NF; ++m)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[m][i] = (float)raw[m][i];
   // (bits of magnitudes are ordered as the magnitudes, infinities and NaN above all)
   uint32_t most = 0;
 #pragma unroll
@@ -102,11 +113,9 @@ DEV float queries(const T* p, bool vec, float scale, f16x8 (&f)[NF], At&& at) {
 }
 template <class T, int NF>
 DEV float row_queries(const T* p, bool vec, float scale, f16x8 (&f)[NF], int g4) {
-  return queries<T, NF, 16>(p, vec, scale, f, [&](int m) { return 64 * (m / 2) + 16 * g4 + 8 * (m & 1); });
-}
-template <class T, int NF>
-DEV float wide_queries(const T* p, bool vec, float scale, f16x8 (&f)[NF], int hi) {
-  return queries<T, NF, 32>(p, vec, scale, f, [&](int m) { return 16 * m + 8 * hi; });
+  typename Eight<T>::run x[NF];
+  load_queries<T, NF>(p, vec, x, [&](int m) { return 64 * (m / 2) + 16 * g4 + 8 * (m & 1); });
+  return queries<T, NF, 16>(x, scale, f);
 }
 
 // Lengths differ, so that the tiles of all sequences, heads and row tiles (the units) are dealt out in equal
@@ -176,6 +185,10 @@ __global__ __launch_bounds__(256, D * NR > 256 ? 1 : 2) void k_kv_rows(KvAttnArg
   constexpr int NF = D / 32, NK = D / 16, R = 16 * NR;
   constexpr bool QL = D == 256;  // queries in LDS, in the order of the operand (no registers to spare)
   constexpr int KT = D == 256 ? 32 : 64, NT = KT / 16, KL = KT / 4, PT = 64 / KT;  // KL: keys of a lane's scores
+  // Single tokens' weights as two fp16, so that fp16 outputs are as near as their own rounding: the products have the
+  // time (48 sequences of up to 8192 tokens, 4 heads of 256: 81 us, with one 80; of 32 rows, 36 and 30). bf16's own
+  // rounding is 8 times a weight's.
+  constexpr bool FINE = __is_same(T, f16) && NR == 1;
   __shared__ float o_lds[4][R][D + 4];
   __shared__ float m_lds[4][R], l_lds[4][R], w_lds[4][R], ref_lds[4];
   __shared__ uint4 q_lds[QL ? NR * NF * 64 : 1];
@@ -380,7 +393,7 @@ __global__ __launch_bounds__(256, D * NR > 256 ? 1 : 2) void k_kv_rows(KvAttnArg
       load_keys(tile + 4);
       look_up(tile + 8);
       __builtin_amdgcn_sched_barrier(0);
-      uint32_t pw[NR][KL / 2];
+      uint32_t pw[NR][KL / 2], pl[FINE ? NR : 1][FINE ? KL / 2 : 1];
 #pragma unroll
       for (int n = 0; n < NR; ++n) {
         const float lift = kBias - m[n];
@@ -388,7 +401,9 @@ __global__ __launch_bounds__(256, D * NR > 256 ? 1 : 2) void k_kv_rows(KvAttnArg
         for (int k = 0; k < KL; k += 2) {
           const float p0 = exp2_fast(sa[n][k >> 2][k & 3] + lift), p1 = exp2_fast(sa[n][k >> 2][(k & 3) + 1] + lift);
           l[n] += p0 + p1;
-          pw[n][k / 2] = pack_f16x2(p0 * svr, p1 * svr);
+          const float w0 = p0 * svr, w1 = p1 * svr;
+          pw[n][k / 2] = pack_f16x2(w0, w1);
+          if constexpr (FINE) pl[n][k / 2] = pack_f16x2(w0 - f16_lo(pw[n][k / 2]), w1 - f16_hi(pw[n][k / 2]));
         }
         if (masked && __ballot(bad)) {
           // values of NaN reach the rows that see one of their block's keys, and no others
@@ -403,8 +418,11 @@ __global__ __launch_bounds__(256, D * NR > 256 ? 1 : 2) void k_kv_rows(KvAttnArg
         for (int u = 0; u < KL / 8; ++u) {
           const f16x8 v = codes_f16(vr[d][2 * u], vr[d][2 * u + 1]);
 #pragma unroll
-          for (int n = 0; n < NR; ++n)
+          for (int n = 0; n < NR; ++n) {
             acc[n][d] = mfma16(v, __builtin_bit_cast(f16x8, make_uint4(pw[n][4 * u], pw[n][4 * u + 1], pw[n][4 * u + 2], pw[n][4 * u + 3])), acc[n][d]);
+            if constexpr (FINE)
+              acc[n][d] = mfma16(v, __builtin_bit_cast(f16x8, make_uint4(pl[n][4 * u], pl[n][4 * u + 1], pl[n][4 * u + 2], pl[n][4 * u + 3])), acc[n][d]);
+          }
         }
       tile += 4;
     } while (tile < k1);
@@ -504,8 +522,35 @@ DEV void streamed(Read&& read, Mul&& mul, Other&& other) {
   }
 }
 
+// A wave's 32 rows of D, of which a lane holds four dims of row lane % 32 at a time, value(d, q) those at 32 d + 2 q +
+// 4 (lane / 32): through LDS, so that stores are 256 bytes in a row. at(r): where row r goes.
+template <class E, int D, class Value, class At>
+DEV void rows_out(uint8_t* lds, int n, Value&& value, At&& at) {
+  constexpr int RB = D * sizeof(E) < 256 ? D * sizeof(E) : 256, ND = RB / sizeof(E), LR = RB / 16, ST = RB + 16;
+  static_assert(32 * ST * 4 <= 3 * sizeof(WideTile<D>), "a wave's rows in its part of the tiles");
+  typedef E run __attribute__((ext_vector_type(4)));
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int p = 0; p < D / ND; ++p) {
+#pragma unroll
+    for (int d = p * ND / 32; d < (p + 1) * ND / 32; ++d)
+#pragma unroll
+      for (int q = 0; q < 16; q += 4)
+        *(run*)(lds + (lane & 31) * ST + (d * 32 - p * ND + 2 * q + (lane >> 5) * 4) * sizeof(E)) = value(d, q);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+    for (int i = 0; i < 32 * LR / 64; ++i) {
+      const int r = i * (64 / LR) + lane / LR, c = lane % LR * 16;
+      uint8_t* to = (uint8_t*)at(r) + p * RB + c;
+      const uint4 x = *(const uint4*)(lds + r * ST + c);
+      if (r < n) *(uint4*)to = x;
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  }
+}
+
 template <class T, int D>
-__global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_kv_wide(KvAttnArgs a, bool vec) {
+__global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_kv_wide(KvAttnArgs a, bool vec, bool vec_out) {
   using W = WideTile<D>;
   constexpr int KT = W::KT, NU = KT / 32, NB = KT / 16, NF = D / 16, NO = D / 32, NC = KT * D / 4096, R = 128;
   __shared__ W buf[3];
@@ -584,16 +629,19 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_kv_wide(KvAttnArgs a,
   };
   // (behind the last tile: that one again, for nobody)
   auto tile_at = [&](int t) { return min(t, k1 - 1); };
-  // (the first three at once, and the queries' own loads beside them)
+  // (the first three at once, and the queries' own loads beside their pages)
   const Entries e0 = look_up(k0), e1 = look_up(tile_at(k0 + 1)), e2 = look_up(tile_at(k0 + 2));
   next_pages = look_up(tile_at(k0 + 3));
+  typename Eight<T>::run qr[NF];
+  load_queries<T, NF>((const T*)a.q.p + (int64_t)(sq.row + tok) * a.q.ld + (int64_t)(h * a.group + row - tok * a.group) * a.q.hld,
+                      vec, qr, [&](int m) { return 16 * m + 8 * hi; });
+  __builtin_amdgcn_sched_barrier(0);
   Raw first, second;
   load(first, e0, k0);
   load(second, e1, tile_at(k0 + 1));
   load(raw, e2, tile_at(k0 + 2));
   f16x8 qf[NF];
-  const float qs = wide_queries<T, NF>((const T*)a.q.p + (int64_t)(sq.row + tok) * a.q.ld +
-                                           (int64_t)(h * a.group + row - tok * a.group) * a.q.hld, vec, a.scale, qf, hi);
+  const float qs = queries<T, NF, 32>(qr, a.scale, qf);
   store_all(buf[0], first);
   store_all(buf[1], second);
   f32x16 acc[NO];
@@ -723,53 +771,48 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_kv_wide(KvAttnArgs a,
     } while (!moved);
   }
   l += __shfl_xor(l, 32, 64);
-  if (r0 + wave * 32 + c32 > last) return;
-  // lane holds dims 32 d + 8 (q / 4) + 4 hi + q % 4 of its row
+  const int n_rows = last + 1 - (r0 + wave * 32);  // (may be none)
+  const bool mine = c32 < n_rows;
+  uint8_t* lds = (uint8_t*)buf + wave * (sizeof(buf) / 64 * 16);
   if (a.plan.splits > 1) {
-    float* p = a.part + (((((int64_t)s * a.c.heads + h) * a.plan.row_tiles + rt) * a.plan.splits + z) * a.part_rows + row - r0) * (D + 4);
-#pragma unroll
-    for (int d = 0; d < NO; ++d)
-#pragma unroll
-      for (int q = 0; q < 16; q += 4)
-        *(f32x4*)(p + d * 32 + 2 * q + 4 * hi) = f32x4{acc[d][q], acc[d][q + 1], acc[d][q + 2], acc[d][q + 3]} * ref;
-    if (hi == 0) {
-      p[D] = m;
-      p[D + 1] = l;
-    }
+    float* p = a.part + (((((int64_t)s * a.c.heads + h) * a.plan.row_tiles + rt) * a.plan.splits + z) * a.part_rows + wave * 32) * (D + 4);
+    rows_out<float, D>(
+        lds, n_rows, [&](int d, int q) { return f32x4{acc[d][q], acc[d][q + 1], acc[d][q + 2], acc[d][q + 3]} * ref; },
+        [&](int r) { return p + r * (D + 4); });
+    if (mine && hi == 0) *(float2*)(p + c32 * (D + 4) + D) = make_float2(m, l);
     return;
   }
   const bool beyond = pos >= a.b.max_len;
   const float inv = beyond ? NAN : l == 0.f ? 0.f : ref / l;
   const int hq = h * a.group + row - tok * a.group;
-  T* o = (T*)a.out.p + (int64_t)(sq.row + tok) * a.out.ld + (int64_t)hq * a.out.hld;
+  const int64_t off = (int64_t)(sq.row + tok) * a.out.ld + (int64_t)hq * a.out.hld;
   typedef T run __attribute__((ext_vector_type(4)));
-  const bool runs = ((uintptr_t)o & 7) == 0;
+  auto value = [&](int d, int q) { return run{(T)(acc[d][q] * inv), (T)(acc[d][q + 1] * inv), (T)(acc[d][q + 2] * inv), (T)(acc[d][q + 3] * inv)}; };
+  if (vec_out) {
+    rows_out<T, D>(lds, n_rows, value, [&](int r) { return (T*)a.out.p + __shfl(off, r, 64); });
+  } else if (mine) {
 #pragma unroll
-  for (int d = 0; d < NO; ++d)
+    for (int d = 0; d < NO; ++d)
 #pragma unroll
-    for (int q = 0; q < 16; q += 4) {
-      run v;
+      for (int q = 0; q < 16; q += 4) {
+        const run v = value(d, q);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) v[i] = (T)(acc[d][q + i] * inv);
-      T* at = o + d * 32 + 2 * q + 4 * hi;
-      if (runs) {
-        *(run*)at = v;
-      } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) at[i] = v[i];
+        for (int i = 0; i < 4; ++i) ((T*)a.out.p)[off + d * 32 + 2 * q + 4 * hi + i] = v[i];
       }
-    }
-  if (hi == 0 && a.lse)
+  }
+  if (mine && hi == 0 && a.lse)
     a.lse[(int64_t)(sq.row + tok) * a.q_heads + hq] = beyond ? NAN : (m - kBias + log2f(l)) * 0.6931471805599453f;
 }
 
-// Joins the parts of each row: one workgroup a row.
-template <class T, int D>
-__global__ __launch_bounds__(256) void k_kv_join(KvAttnArgs a) {
-  constexpr int G = 256 / (D / 4);
-  __shared__ float o_lds[G][D];
-  __shared__ float l_lds[G];
-  const int R = a.plan.rows, r = blockIdx.x, h = blockIdx.y, s = blockIdx.z;
+// Joins the parts of each row with W waves a row, 4 or 1: D / 4 lanes a part, the lanes of the others meeting by
+// shuffles and (4) through LDS.
+template <class T, int D, int W>
+__global__ __launch_bounds__(256) void k_kv_join(KvAttnArgs a, bool vec) {
+  constexpr int LP = D / 4, G = 64 / LP * W;
+  __shared__ float o_lds[W == 4 ? 4 : 1][D];
+  __shared__ float2 ml_lds[4];
+  const int tid = threadIdx.x, lane = tid & 63, wave = wave_id();
+  const int R = a.plan.rows, r = W == 4 ? (int)blockIdx.x : (int)blockIdx.x * 4 + wave, h = blockIdx.y, s = blockIdx.z;
   const KvSeq sq = kv_seq(a.b, s);
   const int rows = sq.n * a.group;
   if (r >= rows) return;
@@ -794,16 +837,14 @@ __global__ __launch_bounds__(256) void k_kv_join(KvAttnArgs a) {
   }
   const int64_t stride = a.plan.shares ? 2 * step : step;
   auto at = [&](int z) { return z ? p + z * stride : p0; };
-  const int e = (threadIdx.x % (D / 4)) * 4, zg = threadIdx.x / (D / 4);
-  float mm = -FLT_MAX;
-  for (int z = threadIdx.x & 63; z < nz; z += 64) mm = fmaxf(mm, at(z)[D]);
-  mm = wave_max(mm);
+  const int e = lane % LP * 4, zg = lane / LP + (W == 4 ? wave * (64 / LP) : 0);
+  constexpr int U = W == 4 ? 8 : 4;  // parts in flight
   f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
-  float ll = 0.f;
-  constexpr int U = 4;  // parts in flight
+  float m = -FLT_MAX, l = 0.f;
   for (int z0 = zg; z0 < nz; z0 += G * U) {
     f32x4 x[U];
     float2 ml[U];
+    float most = m;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const float* c = at(min(z0 + u * G, nz - 1));
@@ -811,39 +852,70 @@ __global__ __launch_bounds__(256) void k_kv_join(KvAttnArgs a) {
       ml[u] = *(const float2*)(c + D);
     }
 #pragma unroll
+    for (int u = 0; u < U; ++u) most = fmaxf(most, ml[u].x);
+    const float down = exp2_fast(m - most);
+    m = most;
+    o *= down;
+    l *= down;
+#pragma unroll
     for (int u = 0; u < U; ++u) {
       if (z0 + u * G >= nz) break;
-      const float w = exp2_fast(ml[u].x - mm);
+      const float w = exp2_fast(ml[u].x - m);
       o += x[u] * w;
-      ll += w * ml[u].y;
+      l += w * ml[u].y;
     }
   }
-  *(f32x4*)&o_lds[zg][e] = o;
-  if (e == 0) l_lds[zg] = ll;
-  __syncthreads();
-  if (threadIdx.x >= D) return;
-  float sum = 0.f, tot = 0.f;
 #pragma unroll
-  for (int g = 0; g < G; ++g) {
-    sum += o_lds[g][threadIdx.x];
-    tot += l_lds[g];
+  for (int d = LP; d < 64; d *= 2) {
+    const float mo = __shfl_xor(m, d, 64), most = fmaxf(m, mo), w = exp2_fast(m - most), wo = exp2_fast(mo - most);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] = o[i] * w + __shfl_xor(o[i], d, 64) * wo;
+    l = l * w + __shfl_xor(l, d, 64) * wo;
+    m = most;
   }
+  if constexpr (W == 4) {
+    if (lane < LP) *(f32x4*)&o_lds[wave][e] = o;
+    if (lane == 0) ml_lds[wave] = make_float2(m, l);
+    __syncthreads();
+    if (tid >= LP) return;
+    float most = ml_lds[0].x;
+#pragma unroll
+    for (int w = 1; w < 4; ++w) most = fmaxf(most, ml_lds[w].x);
+    m = most;
+    o = f32x4{0.f, 0.f, 0.f, 0.f};
+    l = 0.f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const float f = exp2_fast(ml_lds[w].x - most);
+      o += *(const f32x4*)&o_lds[w][e] * f;
+      l += ml_lds[w].y * f;
+    }
+  }
+  if (lane >= LP) return;
   const int i = r / a.group, g = r - i * a.group;
   const bool beyond = sq.past + i >= a.b.max_len;
-  const float inv = beyond ? NAN : tot == 0.f ? 0.f : 1.f / tot;
-  ((T*)a.out.p)[(int64_t)(sq.row + i) * a.out.ld + (int64_t)(h * a.group + g) * a.out.hld + threadIdx.x] = (T)(sum * inv);
-  if (threadIdx.x == 0 && a.lse)
-    a.lse[(int64_t)(sq.row + i) * a.q_heads + h * a.group + g] = beyond ? NAN : (mm - kBias + log2f(tot)) * 0.6931471805599453f;
+  const float inv = beyond ? NAN : l == 0.f ? 0.f : 1.f / l;
+  const float x[4] = {o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
+  T* to = (T*)a.out.p + (int64_t)(sq.row + i) * a.out.ld + (int64_t)(h * a.group + g) * a.out.hld + e;
+  typedef T run __attribute__((ext_vector_type(4)));
+  if (vec) {
+    *(run*)to = run{(T)x[0], (T)x[1], (T)x[2], (T)x[3]};
+  } else {
+#pragma unroll
+    for (int d = 0; d < 4; ++d) to[d] = (T)x[d];
+  }
+  if (lane == 0 && a.lse)
+    a.lse[(int64_t)(sq.row + i) * a.q_heads + h * a.group + g] = beyond ? NAN : (m - kBias + log2f(l)) * 0.6931471805599453f;
 }
 
 template <class T, int D>
 hipError_t kv_attention(const KvAttnArgs& a, hipStream_t st) {
-  const bool vec = vectors(a.q, 2);
+  const bool vec = vectors(a.q, 2), vec_out = vectors(a.out, 2);
   // (what it reads depends on lengths that are on the device)
   const double most = (double)a.b.seqs * a.b.max_len * a.c.heads * 2 * D;
   if (a.plan.wide) {
     const dim3 grid((unsigned)a.plan.row_tiles * a.plan.splits * a.c.heads * a.b.seqs);
-    MEBP_TIMED(st, "kv_wide", 0.0, most, hipLaunchKernelGGL((k_kv_wide<T, D>), grid, dim3(256), 0, st, a, vec));
+    MEBP_TIMED(st, "kv_wide", 0.0, most, hipLaunchKernelGGL((k_kv_wide<T, D>), grid, dim3(256), 0, st, a, vec, vec_out));
   } else {
     const dim3 grid(a.plan.shares ? (unsigned)a.plan.shares : (unsigned)(a.b.seqs * a.c.heads * a.plan.row_tiles * a.plan.splits));
     if (a.plan.rows == 16)
@@ -853,21 +925,26 @@ hipError_t kv_attention(const KvAttnArgs& a, hipStream_t st) {
   }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || (a.plan.splits == 1 && !a.plan.shares)) return e;
-  const dim3 rows((unsigned)a.b.max_new * a.group, (unsigned)a.c.heads, (unsigned)a.b.seqs);
-  MEBP_TIMED(st, "kv_join", 0.0, 0.0, hipLaunchKernelGGL((k_kv_join<T, D>), rows, dim3(256), 0, st, a));
+  const unsigned rows = (unsigned)a.b.max_new * a.group, heads = (unsigned)a.c.heads, seqs = (unsigned)a.b.seqs;
+  if (a.plan.shares || a.plan.splits > 8)
+    MEBP_TIMED(st, "kv_join", 0.0, 0.0, hipLaunchKernelGGL((k_kv_join<T, D, 4>), dim3(rows, heads, seqs), dim3(256), 0, st, a, vec_out));
+  else
+    MEBP_TIMED(st, "kv_join", 0.0, 0.0, hipLaunchKernelGGL((k_kv_join<T, D, 1>), dim3((rows + 3) / 4, heads, seqs), dim3(256), 0, st, a, vec_out));
   return hipGetLastError();
 }
 }  // namespace
 
 KvPlan kv_plan(int seqs, int max_new, int max_len, int q_heads, int heads, int dim, int window) {
   KvPlan p{};
-  const int64_t rows = (int64_t)max_new * (q_heads / heads);
+  const int group = q_heads / heads;
+  const int64_t rows = (int64_t)max_new * group;
   p.wide = rows > 64;
   p.rows = p.wide ? 128 : rows <= 16 || dim > 64 ? 16 : 32;
   p.row_tiles = (int)((rows + p.rows - 1) / p.rows);
   p.splits = 1;
   // tiles that a row tile's queries see at most
-  const int64_t span = window ? std::min<int64_t>((int64_t)window + (p.wide ? p.rows : max_new) + 126, max_len) : max_len;
+  const int64_t tokens = p.wide ? std::min<int64_t>(max_new, p.rows / group + 2) : max_new,
+                span = window ? std::min<int64_t>((int64_t)window + tokens + 126, max_len) : max_len;
   const int64_t tiles = (span + 63) / 64, groups = (int64_t)p.row_tiles * heads * std::max(seqs, 1);
   // few rows of several sequences that are more than two workgroups a compute unit: equal shares
   if (!p.wide && seqs > 1 && groups * ((tiles + 3) / 4) > 512) {
@@ -875,7 +952,7 @@ KvPlan kv_plan(int seqs, int max_new, int max_len, int q_heads, int heads, int d
     return p;
   }
   const int64_t want = std::max<int64_t>(1, 256 / groups);
-  int64_t chunk = std::max<int64_t>(4, (tiles + want - 1) / want);
+  int64_t chunk = std::max<int64_t>(p.wide ? 2 : 4, (tiles + want - 1) / want);
   if (!p.wide) chunk = (chunk + 3) / 4 * 4;
   p.chunk = (int)chunk;
   p.splits = (int)((tiles + chunk - 1) / chunk);
