@@ -248,3 +248,68 @@ def test_nothing_to_do(built_lib, gpu):
     assert bool((out == 3.0).all())
     empty = torch.zeros(0, 2, 64, dtype=F16, device=gpu)
     assert D.kv_attention(t.cache, t.batch, empty).shape == (0, 2, 64)
+
+
+@pytest.mark.parametrize("seqs,longest,most", [(300, 700, 1), (300, 400, 3), (2, 20000, 1), (33, 3000, 2)])
+@pytest.mark.parametrize("hkv,hq,dim,page,dtype", [(1, 7, 64, 32, F16), (2, 14, 64, 64, BF16), (1, 5, 128, 16, F16), (1, 8, 256, 64, BF16)])
+def test_ragged_batches_in_equal_shares(built_lib, gpu, seqs, longest, most, hkv, hq, dim, page, dtype):
+    """Many sequences of all lengths, some without a new token: each workgroup's share begins and ends inside them."""
+    say("shares", seqs, longest, most, hkv, hq, dim)
+    gen = torch.Generator().manual_seed(seqs + dim)
+    new = torch.randint(0, most + 1, (seqs,), generator=gen).tolist() if seqs > 2 else [1, 1]
+    past = torch.randint(0, longest, (seqs,), generator=gen).tolist()
+    new[0], past[0], past[-1] = most, longest, 0
+    t = Setup(gpu, hkv, dim, page, past, new, seed=dim, tail=2)
+    q = t.heads_of(hq, dtype)
+    for window in (0, 300):
+        out, lse = _run(t, q, window)
+        _check(t, q, out, lse, window)
+        again, e2 = _run(t, q, window)
+        assert torch.equal(out, again) and torch.equal(lse, e2)
+
+
+@pytest.mark.parametrize("hq,new", [(1, 70), (1, 200), (3, 50), (3, 130), (5, 97), (12, 40), (100, 3), (200, 1)])
+def test_window_of_many_rows_in_parts(built_lib, gpu, hq, new):
+    """The tiles that a row tile sees, by windows of all sizes: no part of them is left out, whatever the heads in a group."""
+    t = Setup(gpu, 1, 64, 64, [2000], [new], seed=hq, max_len=2300)
+    q = t.heads_of(hq, F16)
+    for window in (1, 2, 63, 64, 65, 127, 128, 129, 191, 257, 700):
+        out, lse = _run(t, q, window)
+        _check(t, q, out, lse, window)
+
+
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("past,new", [(0, 33), (0, 100), (5000, 40), (5000, 1), (200, 64)])
+def test_outputs_at_odd_addresses(built_lib, gpu, dim, past, new):
+    """Rows whose elements no vector reaches, out of one workgroup and joined, are what they are elsewhere."""
+    t = Setup(gpu, 1, dim, 64, [past], [new], seed=dim)
+    q = t.heads_of(4, BF16)
+    want = _run(t, q)
+    whole = torch.full((new, 4 * dim + 3), 3.0, dtype=BF16, device=gpu)
+    out = whole[:, 1:1 + 4 * dim].view(new, 4, dim)
+    lse = torch.zeros(new, 4, device=gpu)
+    D.kv_attention(t.cache, t.batch, q.to(gpu), out, lse)
+    assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
+    assert bool((whole[:, 0] == 3.0).all()) and bool((whole[:, 1 + 4 * dim:] == 3.0).all())
+
+
+def test_two_graphs_and_one_workspace(built_lib, gpu):
+    """Graphs of different calls that were given the same scratch, replayed in turn on one stream."""
+    cases = []
+    ws = torch.empty(64 << 20, dtype=torch.uint8, device=gpu)
+    for new, past, window in ((1, 9000, 0), (200, 700, 256), (1, 3000, 100)):
+        t = Setup(gpu, 1, 128, 64, [past, 100], [new, 1], seed=new)
+        q = t.heads_of(4, F16)
+        want = _run(t, q, window)
+        qd, out, lse = q.to(gpu), torch.zeros_like(want[0]), torch.zeros_like(want[1])
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            D.kv_attention(t.cache, t.batch, qd, out, lse, None, window, ws)
+        cases.append((t, graph, want, out, lse, qd))
+    for _ in range(3):
+        for t, graph, want, out, lse, _ in cases:
+            out.zero_()
+            graph.replay()
+        torch.cuda.synchronize()
+        for t, graph, want, out, lse, _ in cases:
+            assert torch.equal(out, want[0]) and torch.equal(lse, want[1])

@@ -170,6 +170,55 @@ def test_values_at_their_ends(built_lib, gpu):
     assert int(t.ref.scales.isnan().sum()) == 6
 
 
+@pytest.mark.parametrize("dim", [64, 128, 256])
+def test_values_beside_the_borders_of_codes(built_lib, gpu, dim):
+    """Quotients on the border of two codes, and one and a few steps of fp32 to either side of it."""
+    n = 16 * 40
+    t = Setup(gpu, 2, dim, 16, [0], [n])
+    both = []
+    for _ in range(2):
+        most = torch.exp(8 * torch.randn(n // 16, 1, 2, 1, generator=t.gen, dtype=torch.float64)).float()
+        scale = (most.double() / 127).float().double()
+        x = ((torch.randint(-127, 127, (n // 16, 16, 2, dim), generator=t.gen) + 0.5) * scale).float()
+        step = torch.randint(-3, 4, x.shape, generator=t.gen, dtype=torch.int32)
+        x = (x.view(torch.int32) + step).view(torch.float32)
+        x = torch.minimum(torch.maximum(x, -most), most)
+        x[:, 3, :, 7] = most[:, 0, :, 0]
+        both.append(x.reshape(n, 2, dim))
+    D.kv_append(t.cache, t.batch, both[0].to(gpu), both[1].to(gpu))
+    t.append_ref(*both)
+    t.same()
+
+
+def test_two_graphs_of_one_cache(built_lib, gpu):
+    """Steps of different widths, each a graph, in turn: each continues what the other wrote."""
+    t = Setup(gpu, 2, 128, 32, [0, 0], [0, 0], max_new=5, max_len=128)
+    tab = R.table(128, 128, 1e4).float()
+    rope = D.Rope(tab.to(gpu), 128)
+    steps = []
+    for new in ([3, 5], [1, 1]):
+        rows = sum(new)
+        k, v = (torch.zeros(rows, 2, 128, dtype=F16, device=gpu) for _ in range(2))
+        b = t.make_batch([0, new[0], rows], [0, 0])
+        steps.append([new, k, v, b, None])
+    for st in steps:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            D.kv_append(t.cache, st[3], st[1], st[2], rope)
+        st[4] = graph
+    past = [0, 0]
+    for i in range(12):
+        new, k, v, b, graph = steps[i % 2]
+        kh, vh = (torch.randn(*k.shape, generator=t.gen).mul_(1 + i % 4).half() for _ in range(2))
+        k.copy_(kh), v.copy_(vh), b.past.copy_(torch.tensor(past, dtype=torch.int32))
+        graph.replay()
+        torch.cuda.synchronize()
+        t.past, t.new, t.start = list(past), new, [0, new[0], sum(new)]
+        t.append_ref(kh, vh, tab)
+        t.same()
+        past = [a + c for a, c in zip(past, new)]
+
+
 def test_scale_that_was_nan_or_zero(built_lib, gpu):
     t = Setup(gpu, 1, 64, 16, [4, 4, 0], [2, 2, 2])
     for s, x in ((0, math.nan), (1, 0.0), (2, math.nan)):  # (of the last the block's first token is new)
