@@ -464,7 +464,7 @@ typedef struct {
                          /* column p                                                        */
   int64_t table_ld;      /* >= max_pages                                                    */
   int32_t max_pages;     /* columns of the table                                            */
-  int32_t seqs;          /* 0 .. 65535                                                      */
+  int32_t seqs;          /* 0 .. 65534                                                      */
   int32_t max_new;       /* no sequence has more new tokens (rows beyond are left as they were) */
   int32_t max_len;       /* none is longer with them (rows from there on are NaN in an attention); up to */
                          /* 2^30. The call's launches are laid out for these two             */
@@ -504,8 +504,8 @@ size_t mebp_kv_attention_workspace_bytes(int32_t seqs, int32_t max_new, int32_t 
 
 /* mebp_layer_forward_ckpt of `rows` new tokens of the batch's sequences: their keys and values join the
  * layer's cache, and attention is over it (scale 1 / sqrt(head_dim), the layer's window).
- *   x_in, x_out  [rows][d] fp32, apart from each other. Rows of no sequence go through the layer without
- *                attention
+ *   x_in, x_out  [rows][d] fp32, apart from each other. Rows of no sequence, and those behind a
+ *                sequence's max_new, go through the layer without attention
  *   cache        this layer's, of the config's n_kv_heads and head_dim
  *   rope         of the layer's theta; positions beyond its table give NaN
  *   ws           mebp_cached_workspace_bytes                                                */

@@ -2455,7 +2455,7 @@ int mebp_train_step_distill(const mebp_config* cfg, const mebp_q4* emb, const me
 
 namespace {
 // ------------------------------------------------------------------ rotary positions, cache of keys and values
-constexpr int kMaxHeads = 1024, kMaxSeqs = 65535;
+constexpr int kMaxHeads = 1024, kMaxSeqs = 65534;  // (a grid's y takes 65535: the layer's has one more)
 
 int check_heads(const mebp_heads* x, const char* what, bool written) {
   if (!x) return fail(MEBP_EINVAL, "%s is NULL", what);
@@ -2624,6 +2624,7 @@ int check_attention_shape(int seqs, int max_new, int max_len, int q_heads, int h
   if ((e = check_grid((int64_t)p.row_tiles * p.splits * std::max(seqs, 1) * heads)) || (e = check_grid((int64_t)max_new * (q_heads / heads)))) return e;
   return MEBP_OK;
 }
+float exponent_scale(float scale) { return (float)(1.4426950408889634 * (double)scale); }
 KvAttnArgs attention_args(const mebp_kv_cache* c, const mebp_kv_batch* b, int rows, int q_heads, float scale, int window,
                           const KvPlan& p) {
   KvAttnArgs a{};
@@ -2632,7 +2633,7 @@ KvAttnArgs attention_args(const mebp_kv_cache* c, const mebp_kv_batch* b, int ro
   a.q_heads = q_heads;
   a.group = q_heads / c->heads;
   a.window = window;
-  a.scale = (float)(1.4426950408889634 * (double)scale);
+  a.scale = exponent_scale(scale);
   a.plan = p;
   return a;
 }
@@ -2806,7 +2807,7 @@ int mebp_kv_attention(const mebp_kv_cache* cache, const mebp_kv_batch* batch, co
       (e = check_attention_shape(batch->seqs, batch->max_new, batch->max_len, q->heads, cache->heads, cache->dim, window)))
     return e;
   if (q->dtype == MEBP_F32) return fail(MEBP_EUNSUPPORTED, "q: dtype fp32 (attention takes fp16 and bf16)");
-  if (!isfinite(scale)) return fail(MEBP_EINVAL, "scale is not finite");
+  if (!isfinite(scale) || !isfinite(exponent_scale(scale))) return fail(MEBP_EINVAL, "scale %g, or its multiple by log2 e, is not finite", scale);
   if (lse && !aligned(lse, 4)) return fail(MEBP_EINVAL, "lse not 4-byte aligned");
   const Span o = span(out, "out"), l = words(lse, (size_t)q->tokens * q->heads, "lse");
   for (const Span& w : {o, l})

@@ -130,10 +130,13 @@ struct KvShare {
   int s;
   KvSeq seq;
 };
-// tiles that the rows of one sequence see, and places of its units
-DEV Tiles seq_tiles(const KvSeq& q, int window) { return q.n ? tiles_of(q.past, q.past + q.n - 1, window) : Tiles{0, 0}; }
+// Tiles that the rows of one sequence see, and places of its units. (Positions from max_len on have no result, and
+// whatever `past` says no work.)
+DEV Tiles seq_tiles(const KvAttnArgs& a, const KvSeq& q) {
+  return q.n ? tiles_of(min(q.past, a.b.max_len - 1), min(q.past + q.n, a.b.max_len) - 1, a.window) : Tiles{0, 0};
+}
 DEV int64_t seq_places(const KvAttnArgs& a, const KvSeq& q) {
-  const Tiles t = seq_tiles(q, a.window);
+  const Tiles t = seq_tiles(a, q);
   return q.n ? (int64_t)a.c.heads * a.plan.row_tiles * (t.t1 - t.t0 + kUnitCost) : 0;
 }
 DEV int64_t share_size(int64_t places, int shares) {
@@ -209,7 +212,7 @@ __global__ __launch_bounds__(256, D * NR > 256 ? 1 : 2) void k_kv_rows(KvAttnArg
   for (int64_t at = sh.u0; at < sh.u1;) {
   const KvSeq sq = sh.seq;
   const int s = sh.s, rows = sq.n * a.group;
-  const Tiles range = seq_tiles(sq, a.window);
+  const Tiles range = seq_tiles(a, sq);
   const int nt = range.t1 - range.t0;
   int unit, off = 0, len = nt;
   if (a.plan.shares) {
@@ -821,7 +824,7 @@ __global__ __launch_bounds__(256) void k_kv_join(KvAttnArgs a, bool vec) {
   const float *p, *p0;  // parts 1 .. and part 0
   int nz;
   if (a.plan.shares) {
-    const Tiles range = seq_tiles(sq, a.window);
+    const Tiles range = seq_tiles(a, sq);
     const int nt = range.t1 - range.t0;
     const int64_t n = share_size(a.first[a.b.seqs], a.plan.shares),
                   u = a.first[s] + (int64_t)(h * a.plan.row_tiles + rt) * (nt + kUnitCost) + kUnitCost, w0 = u / n;
@@ -831,7 +834,7 @@ __global__ __launch_bounds__(256) void k_kv_join(KvAttnArgs a, bool vec) {
     p0 = p + step;
   } else {
     const int last = min(r0 + R, rows) - 1;
-    const Tiles range = a.plan.wide ? tiles_of(sq.past + r0 / a.group, sq.past + last / a.group, a.window) : seq_tiles(sq, a.window);
+    const Tiles range = a.plan.wide ? tiles_of(sq.past + r0 / a.group, sq.past + last / a.group, a.window) : seq_tiles(a, sq);
     nz = min((range.t1 - range.t0 + a.plan.chunk - 1) / a.plan.chunk, a.plan.splits);
     p0 = p = a.part + ((((int64_t)s * a.c.heads + h) * a.plan.row_tiles + rt) * a.plan.splits) * step + (int64_t)(r - r0) * (D + 4);
   }

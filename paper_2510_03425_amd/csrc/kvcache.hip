@@ -262,9 +262,18 @@ __global__ __launch_bounds__(256) void k_kv_append(KvAppendArgs a, bool vk, bool
   const int roles = 2 * a.c.heads + a.q_groups;
   const int role = blockIdx.x % roles, nb = blockIdx.x / roles, s = blockIdx.y;
   if (s == a.b.seqs) {
-    // (one more than the sequences where there is something to clear)
-    for (int64_t r = max(a.b.start[s], 0) + (int64_t)blockIdx.x; r < a.b.rows; r += gridDim.x)
-      for (int e = threadIdx.x; e < a.rest_cols / 8; e += 256) ((uint4*)(a.rest + r * a.rest_cols))[e] = make_uint4(0, 0, 0, 0);
+    // (one more than the sequences where rows that none has are to be cleared: around all of them, and behind the
+    // max_new of one)
+    auto clear = [&](int64_t r, int64_t end, int step) {
+      for (; r < end; r += step)
+        for (int e = threadIdx.x; e < a.rest_cols / 8; e += 256) ((uint4*)(a.rest + r * a.rest_cols))[e] = make_uint4(0, 0, 0, 0);
+    };
+    clear(blockIdx.x, min(a.b.start[0], a.b.rows), gridDim.x);
+    clear(max(a.b.start[s], 0) + (int64_t)blockIdx.x, a.b.rows, gridDim.x);
+    for (int i = blockIdx.x; i < a.b.seqs; i += gridDim.x) {
+      const KvSeq q = kv_seq(a.b, i);
+      clear(q.row + q.n, min(a.b.start[i + 1], a.b.rows), 1);
+    }
     return;
   }
   const KvSeq q = kv_seq(a.b, s);

@@ -110,6 +110,32 @@ def test_rows_of_no_sequence(built_lib, gpu):
     assert rel_l2(to_np(outs[2]), to_np(outs[0][:30])) <= 1e-3
 
 
+def test_rows_around_sequences(built_lib, gpu):
+    """Rows before the first sequence and those behind a sequence's max_new have no attention either."""
+    cfg = MINI.with_(vocab=0)
+    dm = D.DeviceModel(make_inputs(cfg, seed=6), device=str(gpu))
+    x = torch.randn(40, cfg.hidden, generator=torch.Generator().manual_seed(2)).to(gpu)
+    rope = D.Rope.make(64, 64, cfg.layer_theta(1), device=gpu)
+    outs = []
+    # the same tokens of two sequences: with rows around them, and those rows behind all
+    for fill, start, new in ((0xFF, [3, 17, 40], 9), (0, [3, 17, 40], 9), (0x7B, [0, 9, 18], 9)):
+        cache = dm.kv_caches(2, 64)[0]
+        batch = D.KvBatch(_i32(gpu, start), _i32(gpu, [0, 3]), _i32(gpu, [[0], [1]]), new, 64)
+        order = list(range(40)) if start[0] else [*range(3, 12), *range(17, 26), *range(0, 3), *range(12, 17), *range(26, 40)]
+        rows = torch.tensor(order, device=gpu)
+        ws = dm.cached_ws(40, batch)
+        ws.fill_(fill)
+        cache.pages.fill_(1)
+        cache.scales.fill_(0.1)
+        y = torch.empty_like(x)
+        dm.layer_forward_cached(1, x[rows].contiguous(), y, cache, batch, rope, ws)
+        back = torch.empty_like(y)
+        back[rows] = y
+        outs.append(back)
+    assert torch.equal(outs[0], outs[1]) and outs[0].isfinite().all()
+    assert rel_l2(to_np(outs[2]), to_np(outs[0])) <= 1e-3
+
+
 def test_guarded_and_captured_steps(built_lib, gpu):
     cfg = MINI
     inp = make_inputs(cfg, seed=7)

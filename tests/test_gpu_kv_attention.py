@@ -313,3 +313,24 @@ def test_two_graphs_and_one_workspace(built_lib, gpu):
         torch.cuda.synchronize()
         for t, graph, want, out, lse, _ in cases:
             assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
+
+
+@pytest.mark.parametrize("seqs", [3, 40])
+def test_lengths_beyond_max_len_in_a_batch(built_lib, gpu, seqs):
+    """Whatever a sequence's past says, the others are what they are, and its rows from max_len on are NaN."""
+    past = [2 ** 31 - 1 if s % 3 == 1 else 4000 + 10 * s for s in range(seqs)]
+    t = Setup(gpu, 1, 64, 64, [min(p, 5000) for p in past], [2] * seqs, max_len=4399)
+    t.batch = t.make_batch(t.start, past)
+    q = t.heads_of(4, F16)
+    for window in (0, 100):
+        out, lse = _run(t, q, window)
+        for s, p in enumerate(past):
+            for i in range(2):
+                r = 2 * s + i
+                if p + i >= 4399:
+                    assert out[r].isnan().all() and lse[r].isnan().all()
+                    continue
+                k, v = t.ref.read(t.table[s], 0, p + i + 1)
+                o, e, ob, eb = R.attention(q[r:r + 1], k, v, p + i, 0.125, window)
+                R.check(lse[r:r + 1], e, eb, "lse")
+                R.check(out[r:r + 1], o, ob + o.abs() * 2.0 ** -11 + 2.0 ** -25, "out")

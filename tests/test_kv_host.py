@@ -182,6 +182,7 @@ def test_attention_refused(built_lib):
     assert _attend(q=_heads(Q, **f32), out=_heads(OUT, **f32)) == L.MEBP_EUNSUPPORTED
     assert _attend(out=_heads(OUT, heads=4, dtype=L.MEBP_BF16)) == L.MEBP_EINVAL and _attend(out=_heads(OUT, heads=4, tokens=5)) == L.MEBP_EINVAL
     assert _attend(scale=math.nan) == L.MEBP_EINVAL and _attend(scale=math.inf) == L.MEBP_EINVAL
+    assert _attend(scale=3e38) == L.MEBP_EINVAL and _attend(scale=-3e38) == L.MEBP_EINVAL  # (times log2 e)
     assert _attend(window=-1) == L.MEBP_EINVAL and _attend(lse=LSE + 2) == L.MEBP_EINVAL
     assert _attend(ws=0) == L.MEBP_EINVAL and _attend(ws=WS + 16) == L.MEBP_EINVAL
     need = L.mebp_kv_attention_workspace_bytes(2, 4, 5000, 4, 2, 64)
