@@ -130,6 +130,10 @@ struct KvShare {
   int s;
   KvSeq seq;
 };
+// Tiles that rows r0 .. r0 + R - 1 of a sequence see.
+DEV Tiles row_tiles_of(const KvAttnArgs& a, const KvSeq& q, int r0, int R) {
+  return tiles_of(q.past + r0 / a.group, q.past + (min(r0 + R, q.n * a.group) - 1) / a.group, a.window);
+}
 // Tiles that the rows of one sequence see, and places of its units. (Positions from max_len on have no result, and
 // whatever `past` says no work.)
 DEV Tiles seq_tiles(const KvAttnArgs& a, const KvSeq& q) {
@@ -184,7 +188,7 @@ DEV bool find_share(const KvAttnArgs& a, KvShare& out) {
 // head over a chunk of its tiles, the waves one tile of KT keys in four each; their sums meet in LDS.
 // D = 256 takes 32 keys at a time, so that two waves fit a SIMD's registers with a tile in flight each.
 template <class T, int D, int NR>
-__global__ __launch_bounds__(256, D * NR > 256 ? 1 : 2) void k_kv_rows(KvAttnArgs a, bool vec) {
+__global__ __launch_bounds__(256, 2) void k_kv_rows(KvAttnArgs a, bool vec) {
   constexpr int NF = D / 32, NK = D / 16, R = 16 * NR;
   constexpr bool QL = D == 256;  // queries in LDS, in the order of the operand (no registers to spare)
   constexpr int KT = D == 256 ? 32 : 64, NT = KT / 16, KL = KT / 4, PT = 64 / KT;  // KL: keys of a lane's scores
@@ -212,10 +216,11 @@ __global__ __launch_bounds__(256, D * NR > 256 ? 1 : 2) void k_kv_rows(KvAttnArg
   for (int64_t at = sh.u0; at < sh.u1;) {
   const KvSeq sq = sh.seq;
   const int s = sh.s, rows = sq.n * a.group;
-  const Tiles range = seq_tiles(a, sq);
-  const int nt = range.t1 - range.t0;
-  int unit, off = 0, len = nt;
+  Tiles range;
+  int unit, off, len;
   if (a.plan.shares) {
+    range = seq_tiles(a, sq);
+    const int nt = range.t1 - range.t0;
     const int64_t rel = at - sh.base, per = nt + kUnitCost;
     if (!sq.n || rel >= units * per) {
       sh.base += seq_places(a, sq);
@@ -231,12 +236,14 @@ __global__ __launch_bounds__(256, D * NR > 256 ? 1 : 2) void k_kv_rows(KvAttnArg
     if (len <= 0) continue;
   } else {
     unit = (int)(blockIdx.x / a.plan.splits % units);
+    if (unit % a.plan.row_tiles * R >= rows) return;
+    range = row_tiles_of(a, sq, unit % a.plan.row_tiles * R, R);
     off = blockIdx.x % a.plan.splits * a.plan.chunk;
-    len = min(a.plan.chunk, nt - off);
+    len = min(a.plan.chunk, range.t1 - range.t0 - off);
     if (len <= 0) return;
     at = sh.u1;
   }
-  const int h = unit / a.plan.row_tiles, r0 = unit % a.plan.row_tiles * R;
+  const int h = unit / a.plan.row_tiles, r0 = unit % a.plan.row_tiles * R, nt = range.t1 - range.t0;
   if (r0 >= rows) continue;
   // rows behind the last one repeat it
   const int last = min(r0 + R, rows) - 1;
@@ -808,7 +815,9 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_kv_wide(KvAttnArgs a,
 }
 
 // Joins the parts of each row with W waves a row, 4 or 1: D / 4 lanes a part, the lanes of the others meeting by
-// shuffles and (4) through LDS.
+// shuffles and (4) through LDS. Latency bounds it: 128 parts of 12 rows take 5.1 us by four waves a row and 16.8 by
+// one, 16 parts 4.1 and 3.8; of the many rows that k_kv_wide splits, 6660 in 4 parts, 5.8 by one and 11.4 by a
+// workgroup a row.
 template <class T, int D, int W>
 __global__ __launch_bounds__(256) void k_kv_join(KvAttnArgs a, bool vec) {
   constexpr int LP = D / 4, G = 64 / LP * W;
@@ -833,8 +842,7 @@ __global__ __launch_bounds__(256) void k_kv_join(KvAttnArgs a, bool vec) {
     p = a.part + w0 * 2 * step + (int64_t)(r - r0) * (D + 4);
     p0 = p + step;
   } else {
-    const int last = min(r0 + R, rows) - 1;
-    const Tiles range = a.plan.wide ? tiles_of(sq.past + r0 / a.group, sq.past + last / a.group, a.window) : seq_tiles(a, sq);
+    const Tiles range = row_tiles_of(a, sq, r0, R);
     nz = min((range.t1 - range.t0 + a.plan.chunk - 1) / a.plan.chunk, a.plan.splits);
     p0 = p = a.part + ((((int64_t)s * a.c.heads + h) * a.plan.row_tiles + rt) * a.plan.splits) * step + (int64_t)(r - r0) * (D + 4);
   }
@@ -940,21 +948,31 @@ hipError_t kv_attention(const KvAttnArgs& a, hipStream_t st) {
 KvPlan kv_plan(int seqs, int max_new, int max_len, int q_heads, int heads, int dim, int window) {
   KvPlan p{};
   const int group = q_heads / heads;
-  const int64_t rows = (int64_t)max_new * group;
-  p.wide = rows > 64;
-  p.rows = p.wide ? 128 : rows <= 16 || dim > 64 ? 16 : 32;
-  p.row_tiles = (int)((rows + p.rows - 1) / p.rows);
-  p.splits = 1;
+  const int64_t rows = (int64_t)max_new * group, pairs = (int64_t)heads * std::max(seqs, 1);
   // tiles that a row tile's queries see at most
-  const int64_t tokens = p.wide ? std::min<int64_t>(max_new, p.rows / group + 2) : max_new,
-                span = window ? std::min<int64_t>((int64_t)window + tokens + 126, max_len) : max_len;
-  const int64_t tiles = (span + 63) / 64, groups = (int64_t)p.row_tiles * heads * std::max(seqs, 1);
-  // few rows of several sequences that are more than two workgroups a compute unit: equal shares
-  if (!p.wide && seqs > 1 && groups * ((tiles + 3) / 4) > 512) {
+  auto tiles_seen = [&] {
+    const int64_t tokens = std::min<int64_t>(max_new, p.rows / group + 2);
+    return ((window ? std::min<int64_t>((int64_t)window + tokens + 126, max_len) : max_len) + 63) / 64;
+  };
+  auto shape = [&](int r) {
+    p.rows = r;
+    p.row_tiles = (int)((rows + r - 1) / r);
+  };
+  // Few rows by k_kv_rows, and as many as leave its workgroups of four tiles in three rounds of the chip: it starts
+  // sooner than k_kv_wide, but each row tile reads the cache again. (Of heads of 128, groups of 6, in us: one
+  // sequence of 1256 tokens, 256 of them new, 960 workgroups, 18 and 33; of 8064, 64 new, 1536, 30 and 31; of 8128,
+  // 128 new, 3072, 42 and 38.)
+  shape(rows <= 16 || dim > 64 ? 16 : 32);
+  const int64_t fours = p.row_tiles * pairs * ((tiles_seen() + 3) / 4);
+  p.wide = p.row_tiles > 2 && fours > 1536;
+  if (p.wide) shape(128);
+  p.splits = 1;
+  // one or two row tiles of several sequences that are more than two workgroups a compute unit: equal shares
+  if (!p.wide && p.row_tiles <= 2 && seqs > 1 && fours > 512) {
     p.shares = 512;
     return p;
   }
-  const int64_t want = std::max<int64_t>(1, 256 / groups);
+  const int64_t tiles = tiles_seen(), want = std::max<int64_t>(1, 256 / (p.row_tiles * pairs));
   int64_t chunk = std::max<int64_t>(p.wide ? 2 : 4, (tiles + want - 1) / want);
   if (!p.wide) chunk = (chunk + 3) / 4 * 4;
   p.chunk = (int)chunk;

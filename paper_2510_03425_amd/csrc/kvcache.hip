@@ -252,8 +252,8 @@ struct Codes {
 // One workgroup: a 16-token block of one kv head (its keys or its values), or the queries of those tokens and Q
 // heads. Thread: token tid / 16, 1/16 of the head. Bytes bound it where there are many tokens, and the way from the
 // sequence's numbers to the row and the page, three loads after one another, where there are few. 8 x 2048 tokens,
-// 4 heads of 256 and 4 of queries: 57 us, 4.1 TB/s. (Four blocks after one another in a workgroup, the next one's
-// numbers on their way: 77 us.)
+// 4 heads of 256 and 8 of queries: 69 us, 3.4 TB/s; 57 with its inputs in the cache behind the L2s. (Four blocks
+// after one another in a workgroup, the next one's numbers on their way: 77 instead of 57.)
 template <class T, int D, int Q>
 __global__ __launch_bounds__(256) void k_kv_append(KvAppendArgs a, bool vk, bool vv, bool vq) {
   constexpr int E = D / 32;

@@ -59,6 +59,29 @@ def test_attention(built_lib, gpu, past, new, hkv, hq, dim, page, dtype):
     assert torch.equal(out, again) and torch.equal(lse, e2)
 
 
+@pytest.mark.parametrize("past,new", BATCHES)
+@pytest.mark.parametrize("hkv,hq,dim,page,dtype", SHAPES)
+def test_attention_laid_out_for_long_sequences(built_lib, gpu, past, new, hkv, hq, dim, page, dtype):
+    """The same with room for 2^20 tokens, which has many rows by large tiles and several sequences in shares."""
+    say("long", past, new, hkv, hq, dim, page, dtype)
+    t = Setup(gpu, hkv, dim, page, past, new, seed=sum(past) + hq, tail=3, max_len=1 << 20)
+    q = t.heads_of(hq, dtype)
+    for window in (0, 70):
+        out, lse = _run(t, q, window)
+        _check(t, q, out, lse, window)
+
+
+@pytest.mark.parametrize("hkv,hq,dim,new", [(1, 24, 128, 400), (1, 25, 256, 390), (16, 48, 64, 260), (3, 33, 128, 300)])
+def test_windows_of_many_rows(built_lib, gpu, hkv, hq, dim, new):
+    """Enough rows for large tiles, their windows in parts; the first of them at the sequence's beginning, or far behind it."""
+    for past in (0, 1500):
+        t = Setup(gpu, hkv, dim, 64, [past], [new], seed=hq)
+        q = t.heads_of(hq, F16)
+        for window in (450, 513, 700):
+            out, lse = _run(t, q, window)
+            _check(t, q, out, lse, window)
+
+
 @pytest.mark.parametrize("window", [1, 5, 16, 64, 65, 100, 1000])
 @pytest.mark.parametrize("hkv,hq,dim,page,dtype", SHAPES[1:5])
 def test_window(built_lib, gpu, window, hkv, hq, dim, page, dtype):
