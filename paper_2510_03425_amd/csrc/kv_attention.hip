@@ -118,7 +118,7 @@ DEV float row_queries(const T* p, bool vec, float scale, f16x8 (&f)[NF], int g4)
   return queries<T, NF, 16>(x, scale, f);
 }
 
-// Lengths differ, so that the tiles of all sequences, heads and row tiles (the units) are dealt out in equal
+// Where lengths differ the tiles of all sequences, heads and row tiles (the units) are dealt out in equal
 // shares: workgroup w takes places w n .. of the units in their order, and units that more than one share
 // has are joined by k_kv_join. (A grid of chunks up to the longest length took 1.5 times as long on 48
 // sequences of 1 to 8192 tokens: which compute units get the workgroups that have nothing to do is chance.)
@@ -958,22 +958,26 @@ KvPlan kv_plan(int seqs, int max_new, int max_len, int q_heads, int heads, int d
     p.rows = r;
     p.row_tiles = (int)((rows + r - 1) / r);
   };
-  // Few rows by k_kv_rows, and as many as leave its workgroups of four tiles in three rounds of the chip: it starts
-  // sooner than k_kv_wide, but each row tile reads the cache again. (Of heads of 128, groups of 6, in us: one
-  // sequence of 1256 tokens, 256 of them new, 960 workgroups, 18 and 33; of 8064, 64 new, 1536, 30 and 31; of 8128,
-  // 128 new, 3072, 42 and 38.)
+  // Few rows by k_kv_rows, and as many as it has workgroups for in a round and a half of the chip, with up to 1536
+  // times four tiles to do: it starts sooner than k_kv_wide, but each row tile reads the cache again. (Of heads of 128,
+  // groups of 6, in us: one sequence of 1256 tokens, 256 of them new, 192 workgroups of 20 tiles, 18 and 33; of 8064,
+  // 64 new, 1536 fours, 30 and 31; of 8128, 128 new, 3072 fours, 42 and 38; 4 sequences of 256 new tokens, 768
+  // workgroups, 19 and 28; 40 of 68, 60 new, 1840 workgroups, 34 and 13.)
   shape(rows <= 16 || dim > 64 ? 16 : 32);
-  const int64_t fours = p.row_tiles * pairs * ((tiles_seen() + 3) / 4);
-  p.wide = p.row_tiles > 2 && fours > 1536;
+  const int64_t groups = p.row_tiles * pairs, fours = groups * ((tiles_seen() + 3) / 4);
+  p.wide = p.row_tiles > 2 && (groups > 768 || fours > 1536);
   if (p.wide) shape(128);
   p.splits = 1;
-  // one or two row tiles of several sequences that are more than two workgroups a compute unit: equal shares
-  if (!p.wide && p.row_tiles <= 2 && seqs > 1 && fours > 512) {
+  // One or two row tiles of several long sequences that are more than two workgroups a compute unit: equal shares. (48
+  // sequences of up to 8192 tokens, 4 heads of 256: 87 us, by chunks 140; 106 in a window of 1024, 2 heads of 128, 15
+  // fours at most: 31 and 20.)
+  if (!p.wide && p.row_tiles <= 2 && seqs > 1 && fours > 512 && fours > 16 * groups) {
     p.shares = 512;
     return p;
   }
   const int64_t tiles = tiles_seen(), want = std::max<int64_t>(1, 256 / (p.row_tiles * pairs));
-  int64_t chunk = std::max<int64_t>(p.wide ? 2 : 4, (tiles + want - 1) / want);
+  // (a part of fewer tiles costs more to join than it saves: 3 x 344 tokens, 12 heads of 128, 32 us by 2, 20 by 6)
+  int64_t chunk = std::max<int64_t>(p.wide ? 6 : 4, (tiles + want - 1) / want);
   if (!p.wide) chunk = (chunk + 3) / 4 * 4;
   p.chunk = (int)chunk;
   p.splits = (int)((tiles + chunk - 1) / chunk);

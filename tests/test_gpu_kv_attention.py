@@ -273,7 +273,7 @@ def test_nothing_to_do(built_lib, gpu):
     assert D.kv_attention(t.cache, t.batch, empty).shape == (0, 2, 64)
 
 
-@pytest.mark.parametrize("seqs,longest,most", [(300, 700, 1), (300, 400, 3), (2, 20000, 1), (33, 3000, 2)])
+@pytest.mark.parametrize("seqs,longest,most", [(300, 400, 1), (260, 200, 3), (2, 20000, 1), (33, 2000, 2)])
 @pytest.mark.parametrize("hkv,hq,dim,page,dtype", [(1, 7, 64, 32, F16), (2, 14, 64, 64, BF16), (1, 5, 128, 16, F16), (1, 8, 256, 64, BF16)])
 def test_ragged_batches_in_equal_shares(built_lib, gpu, seqs, longest, most, hkv, hq, dim, page, dtype):
     """Many sequences of all lengths, some without a new token: each workgroup's share begins and ends inside them."""
@@ -285,10 +285,13 @@ def test_ragged_batches_in_equal_shares(built_lib, gpu, seqs, longest, most, hkv
     t = Setup(gpu, hkv, dim, page, past, new, seed=dim, tail=2)
     q = t.heads_of(hq, dtype)
     for window in (0, 300):
-        out, lse = _run(t, q, window)
-        _check(t, q, out, lse, window)
-        again, e2 = _run(t, q, window)
-        assert torch.equal(out, again) and torch.equal(lse, e2)
+        for room in (t.max_len, 1 << 16):  # (with room for long sequences several are dealt out in shares)
+            t.max_len = room
+            t.batch = t.make_batch(t.start, t.past)
+            out, lse = _run(t, q, window)
+            again, e2 = _run(t, q, window)
+            assert torch.equal(out, again) and torch.equal(lse, e2)
+            _check(t, q, out, lse, window)
 
 
 @pytest.mark.parametrize("hq,new", [(1, 70), (1, 200), (3, 50), (3, 130), (5, 97), (12, 40), (100, 3), (200, 1)])
