@@ -975,7 +975,11 @@ KvPlan kv_plan(int seqs, int max_new, int max_len, int q_heads, int heads, int d
     p.shares = 512;
     return p;
   }
-  const int64_t tiles = tiles_seen(), want = std::max<int64_t>(1, 256 / (p.row_tiles * pairs));
+  const int64_t tiles = tiles_seen(), units = p.row_tiles * pairs;
+  // (large tiles go two to a compute unit at up to 128 dims, which pays for a join where the parts are long: 4 x 512
+  // tokens behind 4000, 12 heads of 128, 160 us in one part, 130 in two; 5 x 394, 25 and 44)
+  int64_t want = std::max<int64_t>(1, 256 / units);
+  if (p.wide && dim < 256) want = std::max(want, std::min(384 / units, tiles / 16));
   // (a part of fewer tiles costs more to join than it saves: 3 x 344 tokens, 12 heads of 128, 32 us by 2, 20 by 6)
   int64_t chunk = std::max<int64_t>(p.wide ? 6 : 4, (tiles + want - 1) / want);
   if (!p.wide) chunk = (chunk + 3) / 4 * 4;
