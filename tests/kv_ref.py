@@ -46,10 +46,12 @@ def turn(x, tab, pos, interleaved=False, backward=False):
 
 def turn_bound(x, tab, pos, interleaved, dtype):
     """Two products and a sum in fp32, one of the products possibly exact inside a fused step, and one
-    rounding to the type: 3 half steps of |x_a c| + |x_b s| and one of the result."""
+    rounding to the type: 3 half steps of |x_a c| + |x_b s| and one of the result. A half step relative to the
+    result is for normal numbers: below 2^-14 those of fp16 are all 2^-24 apart, and a rounding is off by up to half of
+    that, 2^-25, whatever the result."""
     m = turn(x.double().abs(), tab.abs() * torch.tensor([1.0, -1.0]), pos, interleaved).abs()
     m = torch.maximum(m, turn(x.double().abs(), tab.abs(), pos, interleaved).abs())
-    return m * (3 * EPS + HALF_STEP[dtype] * (1 + 2 * EPS))
+    return m * (3 * EPS + HALF_STEP[dtype] * (1 + 2 * EPS)) + (2.0 ** -25 if dtype is torch.float16 else 0.0)
 
 
 class Cache:
