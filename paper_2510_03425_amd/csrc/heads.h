@@ -35,6 +35,17 @@ DEV void store8(bf16* p, const float* v) {
   for (int i = 0; i < 8; ++i) a[i] = (bf16)v[i];
   *(bf16x8*)p = a;
 }
+// the same past the L2s, for what they would not hold until it is read
+template <class T>
+DEV void stream8(T* p, const float* v) {
+  typedef uint32_t run __attribute__((ext_vector_type(4)));
+  T t[8];
+  run a[sizeof(T) / 2];
+  store8(t, v);
+  __builtin_memcpy(a, t, sizeof(t));
+#pragma unroll
+  for (int i = 0; i < (int)sizeof(T) / 2; ++i) __builtin_nontemporal_store(a[i], (run*)p + i);
+}
 
 namespace mebp {
 inline bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }

@@ -42,8 +42,8 @@ DEV void turn(float2 cs, float sign, float& xa, float& xb) {
 }
 
 // 8 pairs (or 16 copied elements) of one token and of up to HP heads per thread, whose (cos, sin) are
-// loaded once. Bytes bound it.
-template <class T, bool INTER, int HP>
+// loaded once. Bytes bound it: 5.4 to 6.2 TB/s at 134 MB.
+template <class T, bool INTER, int HP, bool STREAM>
 __global__ __launch_bounds__(256) void k_rope_vec(RopeArgs a, int chunks, int groups) {
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
   const int c = (int)(i % chunks);
@@ -96,8 +96,13 @@ __global__ __launch_bounds__(256) void k_rope_vec(RopeArgs a, int chunks, int gr
         }
       }
     }
-    store8(y + h * a.y.hld + ea, va[k]);
-    if (two) store8(y + h * a.y.hld + eb, vb[k]);
+    if constexpr (STREAM) {
+      stream8(y + h * a.y.hld + ea, va[k]);
+      if (two) stream8(y + h * a.y.hld + eb, vb[k]);
+    } else {
+      store8(y + h * a.y.hld + ea, va[k]);
+      if (two) store8(y + h * a.y.hld + eb, vb[k]);
+    }
   }
 }
 
@@ -135,17 +140,18 @@ hipError_t rope_apply(const RopeArgs& a, hipStream_t st) {
   const int half = a.rope.rot / 2;
   if (half % 8 == 0 && a.dim % 8 == 0 && vectors(a.x, sizeof(T)) && vectors(a.y, sizeof(T)) && aligned16(a.rope.table)) {
     const int chunks = half / 8 + (a.dim - a.rope.rot + 15) / 16;
-    // (one head a thread where four would leave compute units without a workgroup: 1111 x 12 x 128 fp32, half of it
-    // turned, 5.9 us and 7.6; 4096 x 12 x 128 11.5 and 10.4)
+    // One head a thread where four would leave compute units without a workgroup: 1111 x 12 x 128 fp32, half of it
+    // turned, 5.9 us, by four 7.6; 4096 x 12 x 128 11.5 and 10.4. What the L2s cannot hold until it is read goes past
+    // them: 16384 x 8 x 256 bf16, 67 MB, 24.8 us, else 29.1; 21.5 and 22.3 with inputs in the cache behind the L2s.
     auto blocks_by = [&](int hp) { return ((int64_t)a.tokens * ((a.heads + hp - 1) / hp) * chunks + 255) / 256; };
-    auto go = [&](auto hp, auto inter) {
+    auto go = [&](auto hp, auto stream, auto inter) {
       constexpr int HP = decltype(hp)::value;
       MEBP_TIMED(st, name, 0.0, bytes,
-                 hipLaunchKernelGGL((k_rope_vec<T, decltype(inter)::value != 0, HP>), dim3((unsigned)blocks_by(HP)), dim3(256), 0, st, a, chunks,
-                                    (a.heads + HP - 1) / HP));
+                 hipLaunchKernelGGL((k_rope_vec<T, decltype(inter)::value != 0, HP, decltype(stream)::value != 0>), dim3((unsigned)blocks_by(HP)),
+                                    dim3(256), 0, st, a, chunks, (a.heads + HP - 1) / HP));
     };
-    auto by = [&](auto hp) { a.rope.interleaved ? go(hp, IC<1>{}) : go(hp, IC<0>{}); };
-    blocks_by(4) < 256 ? by(IC<1>{}) : by(IC<4>{});
+    auto by = [&](auto hp, auto stream) { a.rope.interleaved ? go(hp, stream, IC<1>{}) : go(hp, stream, IC<0>{}); };
+    blocks_by(4) < 256 ? by(IC<1>{}, IC<0>{}) : bytes / 2 > 32 << 20 ? by(IC<4>{}, IC<1>{}) : by(IC<4>{}, IC<0>{});
     return hipGetLastError();
   }
   const int64_t blocks = ((int64_t)a.tokens * a.heads * (a.dim - half) + 255) / 256;

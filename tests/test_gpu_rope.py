@@ -31,7 +31,8 @@ def test_positions(built_lib, gpu, n_pos, rot, kw):
 CASES = [  # tokens, heads, dim, rot
     (1, 14, 64, 64), (1, 1, 2, 2), (7, 3, 64, 32), (33, 5, 128, 128), (5, 2, 256, 256), (130, 12, 128, 96), (3, 4, 80, 80), (9, 7, 72, 48),
     (4, 2, 40, 16), (17, 3, 50, 26), (2, 9, 64, 6), (257, 1, 96, 96), (11, 2, 1024, 1024),
-    (2051, 13, 256, 256), (9001, 5, 128, 64),  # (several heads a thread)
+    (2051, 13, 256, 256), (9001, 5, 128, 64),  # (several heads a thread; in fp32 and 16 bits on either side of the L2s' size)
+    (30001, 5, 128, 64),
 ]
 
 
