@@ -490,9 +490,9 @@ struct KvReadArgs {
   int nblk;
 };
 hipError_t launch_kv_read(const KvReadArgs& a, int dtype, hipStream_t st);
-// Launch plan of an attention: `rows` query rows (token, head of the group) per workgroup. k_kv_rows: all
-// tiles of 64 keys in so many shares (0: a workgroup for each row tile). k_kv_wide: chunks of `chunk` tiles,
-// `splits` of them at most over a sequence (1: no partial results).
+// Launch plan of an attention: `rows` query rows (token, head of the group) per workgroup, by k_kv_wide or
+// k_kv_rows; a row tile's tiles of 64 keys in chunks of `chunk`, `splits` of them at most (1: no partial results), or,
+// k_kv_rows with `shares` above 0, all tiles of the call in so many shares.
 struct KvPlan {
   bool wide;
   int rows, row_tiles, shares, splits, chunk;
