@@ -28,6 +28,9 @@ namespace {
 // 2^-14 below which it loses bits being 2^-19 of the row's largest weight or less.
 constexpr float kBias = 5.f, kLift = 6.f, kRefUp = 16.f, kRefDown = 1.f / 256.f;
 
+// A block's scale, an infinite one as NaN: its numbers have none to go by.
+DEV float usable(float scale) { return fabsf(scale) < INFINITY ? scale : NAN; }
+
 // (as a scalar, so that what depends on it alone is one)
 DEV int wave_id() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
 
@@ -323,6 +326,7 @@ __global__ __launch_bounds__(256, 2) void k_kv_rows(KvAttnArgs a, bool vec) {
     for (int d = 0; d < NK; ++d) acc[n][d] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
   bool fresh = true;  // (nothing to scale yet)
+  bool moved = false;  // the references for this tile: once, whatever its numbers are
   while (tile < k1) {
 #pragma unroll
     for (int n = 0; n < NR; ++n)
@@ -360,7 +364,7 @@ __global__ __launch_bounds__(256, 2) void k_kv_rows(KvAttnArgs a, bool vec) {
       }
       // the values' reference follows their scales, a row's its scores
       const bool masked = tile * KT + KT - 1 > pos_lo || (a.window && tile * KT <= pos_hi - a.window);
-      const float sx = iv_page < 0 ? NAN : sc.x, sv = masked && tile * KT + vb > pos_hi ? 0.f : iv_page < 0 ? NAN : sc.y;
+      const float sx = iv_page < 0 ? NAN : usable(sc.x), sv = masked && tile * KT + vb > pos_hi ? 0.f : iv_page < 0 ? NAN : usable(sc.y);
       const bool far = __ballot(sv > ref * kRefUp) || (!__ballot(sv > ref * kRefDown) && __ballot(sv > 0.f));
       bool move = far;
       float mx[NR];
@@ -382,8 +386,8 @@ __global__ __launch_bounds__(256, 2) void k_kv_rows(KvAttnArgs a, bool vec) {
         for (int k = 0; k < KL; ++k) mx[n] = fmaxf(mx[n], sa[n][k >> 2][k & 3]);
         move |= __ballot(mx[n] > m[n] + kLift) != 0;
       }
-      if (move) {
-        float mv = sv < INFINITY ? sv : 0.f, next = ref;  // (NaN: no reference)
+      if (move && !moved) {
+        float mv = sv > 0.f ? sv : 0.f, next = ref;  // (NaN: no reference)
         mv = fmaxf(mv, __shfl_xor(mv, 16, 64));
         mv = fmaxf(mv, __shfl_xor(mv, 32, 64));
         if (far && mv > 0.f) next = ldexpf(1.f, ilogbf(mv));
@@ -397,9 +401,12 @@ __global__ __launch_bounds__(256, 2) void k_kv_rows(KvAttnArgs a, bool vec) {
           by[n] = down * (ref / next);
         }
         ref = next;
-        if (!fresh) break;
+        if (!fresh) {
+          moved = true;
+          break;
+        }
       }
-      fresh = false;
+      fresh = moved = false;
       const bool bad = masked && sv != sv;
       const float svr = bad ? 0.f : sv / ref;
       load_keys(tile + 4);
@@ -634,7 +641,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_kv_wide(KvAttnArgs a,
     to[j & 1] = __builtin_bit_cast(uint4, j & 1 ? codes_f16(x.z, x.w) : codes_f16(x.x, x.y));
   };
   auto store_scales = [&](W& t, const Raw& r) {
-    if (sc_mine) t.sc[sc_b] = r.ok ? r.sc : make_float2(NAN, NAN);
+    if (sc_mine) t.sc[sc_b] = r.ok ? make_float2(usable(r.sc.x), usable(r.sc.y)) : make_float2(NAN, NAN);
   };
   auto store_all = [&](W& t, const Raw& r) {
 #pragma unroll
@@ -718,9 +725,10 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_kv_wide(KvAttnArgs a,
     for (int u = 0; u < NU; ++u)
 #pragma unroll
       for (int i = 0; i < 16; ++i) mx = fmaxf(mx, x[u][i]);
-    const bool far = most > ref * kRefUp || (most > 0.f && most < ref * kRefDown);
+    // (a reference has a reciprocal: 2^-126 at least)
+    const bool far = most > ref * kRefUp || (most > 0.f && most < ref * kRefDown && ref > FLT_MIN);
     if (!__ballot(mx > m + kLift || far)) return false;
-    const float nr = far ? ldexpf(1.f, ilogbf(most)) : ref;
+    const float nr = far ? fmaxf(ldexpf(1.f, ilogbf(most)), FLT_MIN) : ref;
     mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
     const float nm = fmaxf(m, mx), down = exp2_fast(m - nm);
     m = nm;

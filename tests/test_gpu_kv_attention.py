@@ -360,3 +360,26 @@ def test_lengths_beyond_max_len_in_a_batch(built_lib, gpu, seqs):
                 o, e, ob, eb = R.attention(q[r:r + 1], k, v, p + i, 0.125, window)
                 R.check(lse[r:r + 1], e, eb, "lse")
                 R.check(out[r:r + 1], o, ob + o.abs() * 2.0 ** -11 + 2.0 ** -25, "out")
+
+
+@pytest.mark.parametrize("room", [0, 1 << 20])
+@pytest.mark.parametrize("hkv,hq,dim,new", [(1, 2, 64, 1), (2, 14, 64, 3), (1, 4, 128, 1), (1, 4, 256, 1), (1, 4, 64, 90), (1, 4, 128, 90), (1, 2, 256, 90)])
+def test_infinite_and_smallest_scales(built_lib, gpu, room, hkv, hq, dim, new):
+    """An infinite scale is as one of NaN, for the rows that see it; the smallest ones are numbers like others."""
+    say("infinite scales", room, hkv, hq, dim, new)
+    for case in range(4):
+        t = Setup(gpu, hkv, dim, 32, [250, 300, 140], [new] * 3, seed=case, max_len=room or None)
+        q = t.heads_of(hq, BF16)
+        if case < 3:
+            for s, tok, w in ((0, 100, 1), (1, 303 if new > 1 else 280, 0), (2, 10, 1)):
+                p, b = t.ref.where(t.table[s], tok)
+                t.ref.scales[p, 0, b, w] = math.nan
+            gives = (math.inf, -math.inf, math.nan)[case]
+            t.cache.scales.copy_(torch.where(t.ref.scales.isnan(), torch.full_like(t.ref.scales, gives), t.ref.scales))
+        else:
+            t.ref.scales[..., 1] = 2.0 ** -149 * torch.randint(1, 40, t.ref.scales.shape[:-1], generator=t.gen)
+            t.ref.scales[:, :, ::2, 1] *= 2.0 ** 3
+            t.cache.scales.copy_(t.ref.scales)
+        for window in (0, 60):
+            out, lse = _run(t, q, window)
+            _check(t, q, out, lse, window)
