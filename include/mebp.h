@@ -494,7 +494,8 @@ int mebp_kv_read(const mebp_kv_cache* cache, const mebp_kv_batch* batch, const m
  *   lse     [tokens][q heads] fp32 log-sum-exp of the scaled scores, or NULL
  * Products in fp16 with fp32 sums (codes are exact there, as queries are up to a power of two per row;
  * softmax weights are rounded to fp16), softmax in fp32. A block whose scale is NaN or infinite, or whose
- * page the table does not have, makes the rows that see it NaN, and no others.              */
+ * page the table does not have, makes the rows that see it NaN, and no others. Sums of values beyond 10^33
+ * may overflow.                                                                             */
 int mebp_kv_attention(const mebp_kv_cache* cache, const mebp_kv_batch* batch, const mebp_heads* q, const mebp_heads* out,
                       float* lse, float scale, int32_t window, void* ws, size_t ws_bytes, mebp_stream_t stream);
 

@@ -27,6 +27,9 @@ namespace {
 // 2^11, and 2^15 with the scale of the values, relative to a reference within 2^4 above: in fp16's range,
 // 2^-14 below which it loses bits being 2^-19 of the row's largest weight or less.
 constexpr float kBias = 5.f, kLift = 6.f, kRefUp = 16.f, kRefDown = 1.f / 256.f;
+// The reference of the values' scales does not fall below this times the largest one so far, whose sums, up to 2^42 in
+// its units, stay in fp32 then; smaller scales lose bits beside it.
+constexpr float kRefLeast = 0x1p-80f;
 
 // A block's scale, an infinite one as NaN: its numbers have none to go by.
 DEV float usable(float scale) { return fabsf(scale) < INFINITY ? scale : NAN; }
@@ -327,6 +330,7 @@ __global__ __launch_bounds__(256, 2) void k_kv_rows(KvAttnArgs a, bool vec) {
   }
   bool fresh = true;  // (nothing to scale yet)
   bool moved = false;  // the references for this tile: once, whatever its numbers are
+  float top = 0.f;     // the largest reference of the sums
   while (tile < k1) {
 #pragma unroll
     for (int n = 0; n < NR; ++n)
@@ -390,7 +394,8 @@ __global__ __launch_bounds__(256, 2) void k_kv_rows(KvAttnArgs a, bool vec) {
         float mv = sv > 0.f ? sv : 0.f, next = ref;  // (NaN: no reference)
         mv = fmaxf(mv, __shfl_xor(mv, 16, 64));
         mv = fmaxf(mv, __shfl_xor(mv, 32, 64));
-        if (far && mv > 0.f) next = ldexpf(1.f, ilogbf(mv));
+        if (!fresh) top = fmaxf(top, ref);
+        if (far && mv > 0.f) next = fmaxf(ldexpf(1.f, ilogbf(mv)), top * kRefLeast);
 #pragma unroll
         for (int n = 0; n < NR; ++n) {
           float x = fmaxf(mx[n], __shfl_xor(mx[n], 16, 64));
@@ -671,7 +676,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_kv_wide(KvAttnArgs a,
 #pragma unroll
     for (int i = 0; i < 16; ++i) acc[d][i] = 0.f;
   const Seen see = keys_seen(pos, a.window);
-  float m = -FLT_MAX, l = 0.f, ref = 1.f, inv_ref = 1.f;
+  float m = -FLT_MAX, l = 0.f, ref = 1.f, inv_ref = 1.f, top = 0.f;
 
   auto scores = [&](const W& t, f32x16 (&sa)[NU], auto&& other) {
 #pragma unroll
@@ -728,7 +733,8 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_kv_wide(KvAttnArgs a,
     // (a reference has a reciprocal: 2^-126 at least)
     const bool far = most > ref * kRefUp || (most > 0.f && most < ref * kRefDown && ref > FLT_MIN);
     if (!__ballot(mx > m + kLift || far)) return false;
-    const float nr = far ? fmaxf(ldexpf(1.f, ilogbf(most)), FLT_MIN) : ref;
+    if (tile > k0) top = fmaxf(top, ref);
+    const float nr = far ? fmaxf(ldexpf(1.f, ilogbf(most)), fmaxf(FLT_MIN, top * kRefLeast)) : ref;
     mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
     const float nm = fmaxf(m, mx), down = exp2_fast(m - nm);
     m = nm;

@@ -363,6 +363,26 @@ def test_lengths_beyond_max_len_in_a_batch(built_lib, gpu, seqs):
 
 
 @pytest.mark.parametrize("room", [0, 1 << 20])
+@pytest.mark.parametrize("dim,new", [(64, 1), (64, 90), (128, 1), (128, 90), (256, 1), (256, 90)])
+def test_scales_at_both_ends(built_lib, gpu, room, dim, new):
+    """Values 10^50 and 10^70 apart, the large ones first or last, or one block in the middle: no sum overflows."""
+    for case in range(5):
+        t = Setup(gpu, 1, dim, 32, [900], [new], seed=case, max_len=room or None)
+        b = torch.arange(t.ref.scales.numel() // 2).view(t.ref.scales.shape[:3])
+        order = torch.empty_like(b)
+        for i, p in enumerate(t.table[0]):
+            order[int(p)] = 2 * i + torch.arange(2)
+        size = [torch.where(order < 20, 1e25, 1e-25), torch.where(order < 20, 1e-25, 1e25), 10.0 ** (30 - 2 * order.clamp(0, 33).double()),
+                torch.where(order == 30, 1e33, 1e-37), torch.where(order == 1, 1e33, 1e-37)][case]
+        t.ref.scales[..., 1] = size.float() * t.ref.scales[..., 1]
+        t.cache.scales.copy_(t.ref.scales)
+        q = t.heads_of(4, BF16)
+        out, lse = _run(t, q)
+        assert out.isfinite().all()
+        _check(t, q, out, lse)
+
+
+@pytest.mark.parametrize("room", [0, 1 << 20])
 @pytest.mark.parametrize("hkv,hq,dim,new", [(1, 2, 64, 1), (2, 14, 64, 3), (1, 4, 128, 1), (1, 4, 256, 1), (1, 4, 64, 90), (1, 4, 128, 90), (1, 2, 256, 90)])
 def test_infinite_and_smallest_scales(built_lib, gpu, room, hkv, hq, dim, new):
     """An infinite scale is as one of NaN, for the rows that see it; the smallest ones are numbers like others."""
