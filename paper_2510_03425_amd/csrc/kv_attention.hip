@@ -27,8 +27,8 @@ namespace {
 // 2^11, and 2^15 with the scale of the values, relative to a reference within 2^4 above: in fp16's range,
 // 2^-14 below which it loses bits being 2^-19 of the row's largest weight or less.
 constexpr float kBias = 5.f, kLift = 6.f, kRefUp = 16.f, kRefDown = 1.f / 256.f;
-// The reference of the values' scales does not fall below this times the largest one so far, whose sums, up to 2^42 in
-// its units, stay in fp32 then; smaller scales lose bits beside it.
+// A row's reference of the values' scales goes by the blocks that it sees. It does not fall below this times the largest
+// one so far, whose sums, up to 2^42 in its units, stay in fp32 then; smaller scales lose bits beside it.
 constexpr float kRefLeast = 0x1p-80f;
 
 // A block's scale, an infinite one as NaN: its numbers have none to go by.
@@ -205,7 +205,7 @@ __global__ __launch_bounds__(256, 2) void k_kv_rows(KvAttnArgs a, bool vec) {
   // rounding is 8 times a weight's.
   constexpr bool FINE = __is_same(T, f16) && NR == 1;
   __shared__ float o_lds[4][R][D + 4];
-  __shared__ float m_lds[4][R], l_lds[4][R], w_lds[4][R], ref_lds[4];
+  __shared__ float m_lds[4][R], l_lds[4][R], w_lds[4][R], ref_lds[4][R];
   __shared__ uint4 q_lds[QL ? NR * NF * 64 : 1];
   __shared__ KvShare share_lds;
   const int tid = threadIdx.x, lane = tid & 63, wave = wave_id(), r16 = lane & 15, g4 = lane >> 4;
@@ -319,18 +319,18 @@ __global__ __launch_bounds__(256, 2) void k_kv_rows(KvAttnArgs a, bool vec) {
   };
   f32x4 acc[NR][NK];
   // As in k_kv_wide, the sums are scaled in an outer loop.
-  float m[NR], l[NR], by[NR], ref = 1.f;
+  float m[NR], l[NR], by[NR], ref[NR], top[NR];  // ref: the row's reference for values; top: the largest one of its sums
 #pragma unroll
   for (int n = 0; n < NR; ++n) {
     m[n] = -FLT_MAX;
     l[n] = 0.f;
-    by[n] = 1.f;
+    by[n] = ref[n] = 1.f;
+    top[n] = 0.f;
 #pragma unroll
     for (int d = 0; d < NK; ++d) acc[n][d] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
   bool fresh = true;  // (nothing to scale yet)
   bool moved = false;  // the references for this tile: once, whatever its numbers are
-  float top = 0.f;     // the largest reference of the sums
   while (tile < k1) {
 #pragma unroll
     for (int n = 0; n < NR; ++n)
@@ -366,17 +366,18 @@ __global__ __launch_bounds__(256, 2) void k_kv_rows(KvAttnArgs a, bool vec) {
           }
         }
       }
-      // the values' reference follows their scales, a row's its scores
+      // a row's references follow its scores, and the values' scales of the blocks that it sees
       const bool masked = tile * KT + KT - 1 > pos_lo || (a.window && tile * KT <= pos_hi - a.window);
-      const float sx = iv_page < 0 ? NAN : usable(sc.x), sv = masked && tile * KT + vb > pos_hi ? 0.f : iv_page < 0 ? NAN : usable(sc.y);
-      const bool far = __ballot(sv > ref * kRefUp) || (!__ballot(sv > ref * kRefDown) && __ballot(sv > 0.f));
-      bool move = far;
-      float mx[NR];
+      const float sx = iv_page < 0 ? NAN : usable(sc.x), sb = iv_page < 0 ? NAN : usable(sc.y);
+      bool move = false, far[NR];
+      float mx[NR], sv[NR];
 #pragma unroll
       for (int n = 0; n < NR; ++n) {
         const float f = sx * qs[n];
         const int k0 = tile * KT + vb - see[n].lo;
         mx[n] = -INFINITY;
+        // (0 where the row sees none of the lane's keys)
+        sv[n] = masked && (k0 + KL <= 0 || k0 > (int)see[n].span) ? 0.f : sb;
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -388,39 +389,46 @@ __global__ __launch_bounds__(256, 2) void k_kv_rows(KvAttnArgs a, bool vec) {
         }
 #pragma unroll
         for (int k = 0; k < KL; ++k) mx[n] = fmaxf(mx[n], sa[n][k >> 2][k & 3]);
-        move |= __ballot(mx[n] > m[n] + kLift) != 0;
+        // (a bit for each row from those of its four lanes)
+        auto rows_of = [](uint64_t b) {
+          b |= b >> 32;
+          return (uint32_t)(b | b >> 16) & 0xffffu;
+        };
+        const uint32_t away = rows_of(__ballot(sv[n] > ref[n] * kRefUp)) |
+                              (rows_of(__ballot(sv[n] > 0.f)) & ~rows_of(__ballot(sv[n] > ref[n] * kRefDown)));
+        far[n] = away >> r16 & 1;
+        move |= away || __ballot(mx[n] > m[n] + kLift) != 0;
       }
       if (move && !moved) {
-        float mv = sv > 0.f ? sv : 0.f, next = ref;  // (NaN: no reference)
-        mv = fmaxf(mv, __shfl_xor(mv, 16, 64));
-        mv = fmaxf(mv, __shfl_xor(mv, 32, 64));
-        if (!fresh) top = fmaxf(top, ref);
-        if (far && mv > 0.f) next = fmaxf(ldexpf(1.f, ilogbf(mv)), top * kRefLeast);
 #pragma unroll
         for (int n = 0; n < NR; ++n) {
+          float mv = sv[n] > 0.f ? sv[n] : 0.f, next = ref[n];  // (NaN: no reference)
+          mv = fmaxf(mv, __shfl_xor(mv, 16, 64));
+          mv = fmaxf(mv, __shfl_xor(mv, 32, 64));
+          if (!fresh) top[n] = fmaxf(top[n], ref[n]);
+          if (far[n] && mv > 0.f) next = fmaxf(ldexpf(1.f, ilogbf(mv)), top[n] * kRefLeast);
           float x = fmaxf(mx[n], __shfl_xor(mx[n], 16, 64));
           x = fmaxf(m[n], fmaxf(x, __shfl_xor(x, 32, 64)));
           const float down = exp2_fast(m[n] - x);
           m[n] = x;
           l[n] *= down;
-          by[n] = down * (ref / next);
+          by[n] = down * (ref[n] / next);
+          ref[n] = next;
         }
-        ref = next;
         if (!fresh) {
           moved = true;
           break;
         }
       }
       fresh = moved = false;
-      const bool bad = masked && sv != sv;
-      const float svr = bad ? 0.f : sv / ref;
       load_keys(tile + 4);
       look_up(tile + 8);
       __builtin_amdgcn_sched_barrier(0);
       uint32_t pw[NR][KL / 2], pl[FINE ? NR : 1][FINE ? KL / 2 : 1];
 #pragma unroll
       for (int n = 0; n < NR; ++n) {
-        const float lift = kBias - m[n];
+        // (a scale of NaN: so are the weights of all its keys, in a row that sees one of them)
+        const float lift = kBias - m[n], svr = sv[n] / ref[n];
 #pragma unroll
         for (int k = 0; k < KL; k += 2) {
           const float p0 = exp2_fast(sa[n][k >> 2][k & 3] + lift), p1 = exp2_fast(sa[n][k >> 2][(k & 3) + 1] + lift);
@@ -428,12 +436,6 @@ __global__ __launch_bounds__(256, 2) void k_kv_rows(KvAttnArgs a, bool vec) {
           const float w0 = p0 * svr, w1 = p1 * svr;
           pw[n][k / 2] = pack_f16x2(w0, w1);
           if constexpr (FINE) pl[n][k / 2] = pack_f16x2(w0 - f16_lo(pw[n][k / 2]), w1 - f16_hi(pw[n][k / 2]));
-        }
-        if (masked && __ballot(bad)) {
-          // values of NaN reach the rows that see one of their block's keys, and no others
-#pragma unroll
-          for (int k = 0; k < KL; ++k)
-            if (bad && sa[n][k >> 2][k & 3] != -INFINITY) pw[n][k / 2] |= k & 1 ? 0x7e000000u : 0x7e00u;
         }
       }
 #pragma unroll
@@ -461,9 +463,9 @@ __global__ __launch_bounds__(256, 2) void k_kv_rows(KvAttnArgs a, bool vec) {
     if (g4 == 0) {
       m_lds[wave][n * 16 + r16] = m[n];
       l_lds[wave][n * 16 + r16] = l[n];
+      ref_lds[wave][n * 16 + r16] = ref[n];
     }
   }
-  if (lane == 0) ref_lds[wave] = ref;
   __syncthreads();
   if (tid < R) {
     float mm = m_lds[0][tid];
@@ -472,7 +474,7 @@ __global__ __launch_bounds__(256, 2) void k_kv_rows(KvAttnArgs a, bool vec) {
     for (int w = 0; w < 4; ++w) {
       const float e = exp2_fast(m_lds[w][tid] - mm);
       ll += e * l_lds[w][tid];
-      w_lds[w][tid] = e * ref_lds[w];
+      w_lds[w][tid] = e * ref_lds[w][tid];
     }
     m_lds[0][tid] = mm;
     l_lds[0][tid] = ll;
@@ -697,19 +699,19 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_kv_wide(KvAttnArgs a,
   bool moved = false;
   int tile = k0, at = 0;
   float x[NU][16], f[NB], sv[NB];
-  bool masked, bad;
+  bool masked;
   // scores and scales of the tile, and whether a reference has to move for it
   auto look = [&] {
     const W& t = buf[at];
     float most = 0.f;
     masked = tile * KT + KT - 1 > w_lo || (a.window && tile * KT <= w_hi - a.window);
-    bad = false;  // a block of the tile has values of NaN
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
       const float2 sc = t.sc[b];
       f[b] = sc.x * qs;
-      sv[b] = masked && tile * KT + 16 * b > w_hi ? 0.f : sc.y;
-      bad |= sv[b] != sv[b];
+      // (0 where the row sees none of the block's keys; NaN else makes the weights of all of them NaN)
+      const int first = tile * KT + 16 * b - see.lo;
+      sv[b] = masked && (first + 16 <= 0 || first > (int)see.span) ? 0.f : sc.y;
       most = fmaxf(most, sv[b] < INFINITY ? sv[b] : 0.f);
     }
 #pragma unroll
@@ -754,7 +756,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_kv_wide(KvAttnArgs a,
       uint32_t pw[NU * 8];
       float up[NB], p0;
 #pragma unroll
-      for (int b = 0; b < NB; ++b) up[b] = masked && sv[b] != sv[b] ? 0.f : sv[b] * inv_ref;
+      for (int b = 0; b < NB; ++b) up[b] = sv[b] * inv_ref;
       constexpr int PS = 16 / NF > 1 ? 16 / NF : 1;  // weights to a product
       scores(buf[at1], sn, [&](int j) {
 #pragma unroll
@@ -767,15 +769,6 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_kv_wide(KvAttnArgs a,
             p0 = p;
         }
       });
-      if (__ballot(masked && bad)) {
-        // values of NaN reach the rows that see one of their block's keys, and no others
-#pragma unroll
-        for (int u = 0; u < NU; ++u)
-#pragma unroll
-          for (int i = 0; i < 16; ++i)
-            if (sv[2 * u + (i >> 3)] != sv[2 * u + (i >> 3)] && x[u][i] != -INFINITY)
-              pw[u * 8 + i / 2] |= i & 1 ? 0x7e000000u : 0x7e00u;
-      }
       const W& t = buf[at];
       constexpr int EV = NO * NB / (4 * NC);  // products to a piece of the tile after the next
       streamed<NO * NB>(
