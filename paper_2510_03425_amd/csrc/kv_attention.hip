@@ -1,8 +1,8 @@
 // Attention of new tokens over the paged 8-bit cache on gfx950: causal, grouped heads, optional window.
 //
 // With the codes k, v of a block and its scales sk, sv:  s = scale sk (q . k),  p = exp(s - m),
-// out = (sum p sv v) / (sum p): codes go into the matrix instructions as they are, exact in fp16, and the
-// scales into the scores and the weights. One pass over the cache with the running maximum and sum of a
+// out = (sum p sv v) / (sum p): codes go into the matrix instructions as they are, exact in fp16 (keys) and bf16
+// (values), and the scales into the scores and the weights. One pass over the cache with the running maximum and sum of a
 // softmax; statistics and sums in fp32.
 //
 // k_kv_rows keeps a whole 64-key tile in one wave's registers, without LDS: with S^T = K Q^T and
@@ -23,13 +23,15 @@
 namespace mebp {
 namespace {
 
-// Weights are 2^(s - m + kBias), m following a row's largest score in steps of more than kLift: at most
-// 2^11, and 2^15 with the scale of the values, relative to a reference within 2^4 above: in fp16's range,
-// 2^-14 below which it loses bits being 2^-19 of the row's largest weight or less.
-constexpr float kBias = 5.f, kLift = 6.f, kRefUp = 16.f, kRefDown = 1.f / 256.f;
-// A row's reference of the values' scales goes by the blocks that it sees. It does not fall below this times the largest
-// one so far, whose sums, up to 2^42 in its units, stay in fp32 then; smaller scales lose bits beside it.
-constexpr float kRefLeast = 0x1p-80f;
+// Weights are 2^(s - m), m a row's largest score so far and kLift more, at most 1; it moves when a score passes it.
+// Those below 2^-126 are 0.
+constexpr float kLift = 6.f;
+// A weight times its block's scale of values goes into the products as two bf16, the second what the first leaves out:
+// 2^-18 of it at any size, so that many small ones beside a large one of small values are all there (in fp16 those
+// below 2^-22 of the largest are not). fp32's range takes them and their sums as they are; a row whose scales so far are
+// all below kSmall has them over kSmallRef, where theirs have their bits too. (The second products cost what bounds
+// k_kv_wide: 8 x 2048 tokens, 8 heads of 256, 266 us instead of 243; k_kv_rows reads in the time of both.)
+constexpr float kSmall = 0x1p-20f, kSmallRef = 0x1p-100f;
 
 // A block's scale, an infinite one as NaN: its numbers have none to go by.
 DEV float usable(float scale) { return fabsf(scale) < INFINITY ? scale : NAN; }
@@ -53,6 +55,23 @@ DEV f16x8 codes_f16(uint32_t lo, uint32_t hi) {
   r.z = __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, b, 0x04010400u)) - off);
   r.w = __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, b, 0x04030402u)) - off);
   return __builtin_bit_cast(f16x8, r);
+}
+
+// The same as bf16, the upper halves of their fp32.
+DEV uint32_t codes_bf16x2(uint32_t w, int j) {
+  const float a = (float)(int8_t)(w >> 8 * j), b = (float)(int8_t)(w >> 8 * (j + 1));
+  return perm_hi16(__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b));
+}
+DEV uint4 codes_bf16(uint32_t lo, uint32_t hi) {
+  return make_uint4(codes_bf16x2(lo, 0), codes_bf16x2(lo, 2), codes_bf16x2(hi, 0), codes_bf16x2(hi, 2));
+}
+// Two numbers as bf16, and what that leaves out of them.
+struct TwoParts {
+  uint32_t hi, lo;
+};
+DEV TwoParts two_parts(float a, float b) {
+  const uint32_t hi = pack_bf16x2(a, b);
+  return TwoParts{hi, pack_bf16x2(a - bf16_lo(hi), b - bf16_hi(hi))};
 }
 
 // 64-key tiles [t0, t1) that queries at positions [lo, hi] of a sequence of `len` tokens see
@@ -200,10 +219,6 @@ __global__ __launch_bounds__(256, 2) void k_kv_rows(KvAttnArgs a, bool vec) {
   constexpr int NF = D / 32, NK = D / 16, R = 16 * NR;
   constexpr bool QL = D == 256;  // queries in LDS, in the order of the operand (no registers to spare)
   constexpr int KT = D == 256 ? 32 : 64, NT = KT / 16, KL = KT / 4, PT = 64 / KT;  // KL: keys of a lane's scores
-  // Single tokens' weights as two fp16, so that fp16 outputs are as near as their own rounding: the products have the
-  // time (48 sequences of up to 8192 tokens, 4 heads of 256: 81 us, with one 80; of 32 rows, 36 and 30). bf16's own
-  // rounding is 8 times a weight's.
-  constexpr bool FINE = __is_same(T, f16) && NR == 1;
   __shared__ float o_lds[4][R][D + 4];
   __shared__ float m_lds[4][R], l_lds[4][R], w_lds[4][R], ref_lds[4][R];
   __shared__ uint4 q_lds[QL ? NR * NF * 64 : 1];
@@ -319,18 +334,18 @@ __global__ __launch_bounds__(256, 2) void k_kv_rows(KvAttnArgs a, bool vec) {
   };
   f32x4 acc[NR][NK];
   // As in k_kv_wide, the sums are scaled in an outer loop.
-  float m[NR], l[NR], by[NR], ref[NR], top[NR];  // ref: the row's reference for values; top: the largest one of its sums
+  float m[NR], l[NR], by[NR], ref[NR];  // (the row's sums of values are in units of ref)
 #pragma unroll
   for (int n = 0; n < NR; ++n) {
     m[n] = -FLT_MAX;
     l[n] = 0.f;
-    by[n] = ref[n] = 1.f;
-    top[n] = 0.f;
+    by[n] = 1.f;
+    ref[n] = kSmallRef;
 #pragma unroll
     for (int d = 0; d < NK; ++d) acc[n][d] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
   bool fresh = true;  // (nothing to scale yet)
-  bool moved = false;  // the references for this tile: once, whatever its numbers are
+  bool moved = false;  // m or ref for this tile: once, whatever its numbers are
   while (tile < k1) {
 #pragma unroll
     for (int n = 0; n < NR; ++n)
@@ -366,10 +381,11 @@ __global__ __launch_bounds__(256, 2) void k_kv_rows(KvAttnArgs a, bool vec) {
           }
         }
       }
-      // a row's references follow its scores, and the values' scales of the blocks that it sees
+      // a row's m and ref follow its scores, and the values' scales of the blocks that it sees
       const bool masked = tile * KT + KT - 1 > pos_lo || (a.window && tile * KT <= pos_hi - a.window);
       const float sx = iv_page < 0 ? NAN : usable(sc.x), sb = iv_page < 0 ? NAN : usable(sc.y);
-      bool move = false, far[NR];
+      bool move = false;
+      uint64_t large[NR];  // lanes whose block is too large for the row's ref
       float mx[NR], sv[NR];
 #pragma unroll
       for (int n = 0; n < NR; ++n) {
@@ -389,31 +405,22 @@ __global__ __launch_bounds__(256, 2) void k_kv_rows(KvAttnArgs a, bool vec) {
         }
 #pragma unroll
         for (int k = 0; k < KL; ++k) mx[n] = fmaxf(mx[n], sa[n][k >> 2][k & 3]);
-        // (a bit for each row from those of its four lanes)
-        auto rows_of = [](uint64_t b) {
-          b |= b >> 32;
-          return (uint32_t)(b | b >> 16) & 0xffffu;
-        };
-        const uint32_t away = rows_of(__ballot(sv[n] > ref[n] * kRefUp)) |
-                              (rows_of(__ballot(sv[n] > 0.f)) & ~rows_of(__ballot(sv[n] > ref[n] * kRefDown)));
-        far[n] = away >> r16 & 1;
-        move |= away || __ballot(mx[n] > m[n] + kLift) != 0;
+        large[n] = __ballot(ref[n] < 1.f && sv[n] > kSmall);
+        move |= large[n] || __ballot(mx[n] > m[n]) != 0;
       }
       if (move && !moved) {
 #pragma unroll
         for (int n = 0; n < NR; ++n) {
-          float mv = sv[n] > 0.f ? sv[n] : 0.f, next = ref[n];  // (NaN: no reference)
-          mv = fmaxf(mv, __shfl_xor(mv, 16, 64));
-          mv = fmaxf(mv, __shfl_xor(mv, 32, 64));
-          if (!fresh) top[n] = fmaxf(top[n], ref[n]);
-          if (far[n] && mv > 0.f) next = fmaxf(ldexpf(1.f, ilogbf(mv)), top[n] * kRefLeast);
           float x = fmaxf(mx[n], __shfl_xor(mx[n], 16, 64));
-          x = fmaxf(m[n], fmaxf(x, __shfl_xor(x, 32, 64)));
+          x = fmaxf(x, __shfl_xor(x, 32, 64));
+          x = x > m[n] ? x + kLift : m[n];
           const float down = exp2_fast(m[n] - x);
           m[n] = x;
           l[n] *= down;
-          by[n] = down * (ref[n] / next);
-          ref[n] = next;
+          const uint64_t l2 = large[n] | large[n] >> 32;  // (of the row's four lanes)
+          const bool grow = (l2 | l2 >> 16) >> r16 & 1;
+          by[n] = grow ? down * kSmallRef : down;
+          ref[n] = grow ? 1.f : ref[n];
         }
         if (!fresh) {
           moved = true;
@@ -424,30 +431,28 @@ __global__ __launch_bounds__(256, 2) void k_kv_rows(KvAttnArgs a, bool vec) {
       load_keys(tile + 4);
       look_up(tile + 8);
       __builtin_amdgcn_sched_barrier(0);
-      uint32_t pw[NR][KL / 2], pl[FINE ? NR : 1][FINE ? KL / 2 : 1];
+      TwoParts pw[NR][KL / 2];
 #pragma unroll
       for (int n = 0; n < NR; ++n) {
         // (a scale of NaN: so are the weights of all its keys, in a row that sees one of them)
-        const float lift = kBias - m[n], svr = sv[n] / ref[n];
+        const float svr = ref[n] < 1.f ? sv[n] * (1.f / kSmallRef) : sv[n];
 #pragma unroll
         for (int k = 0; k < KL; k += 2) {
-          const float p0 = exp2_fast(sa[n][k >> 2][k & 3] + lift), p1 = exp2_fast(sa[n][k >> 2][(k & 3) + 1] + lift);
+          const float p0 = exp2_fast(sa[n][k >> 2][k & 3] - m[n]), p1 = exp2_fast(sa[n][k >> 2][(k & 3) + 1] - m[n]);
           l[n] += p0 + p1;
-          const float w0 = p0 * svr, w1 = p1 * svr;
-          pw[n][k / 2] = pack_f16x2(w0, w1);
-          if constexpr (FINE) pl[n][k / 2] = pack_f16x2(w0 - f16_lo(pw[n][k / 2]), w1 - f16_hi(pw[n][k / 2]));
+          pw[n][k / 2] = two_parts(p0 * svr, p1 * svr);
         }
       }
 #pragma unroll
       for (int d = 0; d < NK; ++d)
 #pragma unroll
         for (int u = 0; u < KL / 8; ++u) {
-          const f16x8 v = codes_f16(vr[d][2 * u], vr[d][2 * u + 1]);
+          const uint4 v = codes_bf16(vr[d][2 * u], vr[d][2 * u + 1]);
 #pragma unroll
           for (int n = 0; n < NR; ++n) {
-            acc[n][d] = mfma16(v, __builtin_bit_cast(f16x8, make_uint4(pw[n][4 * u], pw[n][4 * u + 1], pw[n][4 * u + 2], pw[n][4 * u + 3])), acc[n][d]);
-            if constexpr (FINE)
-              acc[n][d] = mfma16(v, __builtin_bit_cast(f16x8, make_uint4(pl[n][4 * u], pl[n][4 * u + 1], pl[n][4 * u + 2], pl[n][4 * u + 3])), acc[n][d]);
+            const TwoParts* w = &pw[n][4 * u];
+            acc[n][d] = mfma16_raw<OpBF16>(v, make_uint4(w[0].hi, w[1].hi, w[2].hi, w[3].hi), acc[n][d]);
+            acc[n][d] = mfma16_raw<OpBF16>(v, make_uint4(w[0].lo, w[1].lo, w[2].lo, w[3].lo), acc[n][d]);
           }
         }
       tile += 4;
@@ -505,18 +510,18 @@ __global__ __launch_bounds__(256, 2) void k_kv_rows(KvAttnArgs a, bool vec) {
     for (int k = 0; k < 4; ++k) p[k] = (T)(o[k] * inv);
     if (e == 0 && a.lse)
       a.lse[(int64_t)(sq.row + i_tok) * a.q_heads + h * a.group + g] =
-          sq.past + i_tok >= a.b.max_len ? NAN : (m_lds[0][r] - kBias + log2f(ll)) * 0.6931471805599453f;
+          sq.past + i_tok >= a.b.max_len ? NAN : (m_lds[0][r] + log2f(ll)) * 0.6931471805599453f;
   }
   __syncthreads();  // (before the next one's sums)
   }
 }
 
 // Many rows: one workgroup of 4 waves takes 128 rows, 32 a wave, whose queries and sums stay in registers; the
-// waves share tiles of KT keys [KT][D] and values [D][KT] in LDS, turned to fp16 there once. Products on
+// waves share tiles of KT keys [KT][D] in fp16 and values [D][KT] in bf16 in LDS, turned to them once. Products on
 // 32x32x16: S^T = K Q^T with row r of 32 as key r with bits 2 and 3 exchanged, so that a lane's 8 results
 // are 8 successive keys, the other operand of O^T += V^T P^T. A wave's products and its other work follow one
 // another unless they are of different tiles: the scores of tile t + 1 are made beside the weights of t, and
-// tile t + 2 is turned to fp16 beside the output's products of t, with three copies of the tile in LDS.
+// tile t + 2 is turned to 16 bits beside the output's products of t, with three copies of the tile in LDS.
 // 2 x 8192 tokens, 12 heads of 128: 780 TFLOP/s; 8 of 256, whose sums and queries leave room for one wave on a SIMD: 650,
 // 1.6 us for 32 keys, of which loading the next tile is a fifth and turning it a sixth; before its first tile 5 us.
 DEV int bits23(int r) { return (r & ~12) | (r & 4) << 1 | (r & 8) >> 1; }
@@ -645,7 +650,8 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_kv_wide(KvAttnArgs a,
     const int dim = (tid + 256 * i) % D, b = (tid + 256 * i) / D * 2;
     uint4* to = j & 2 ? &t.v[dim * W::VC + b] : &t.k[key * W::KC + c];
     const uint4 x = j & 2 ? r.v[i] : r.k[i];
-    to[j & 1] = __builtin_bit_cast(uint4, j & 1 ? codes_f16(x.z, x.w) : codes_f16(x.x, x.y));
+    const uint32_t y = j & 1 ? x.z : x.x, z = j & 1 ? x.w : x.y;
+    to[j & 1] = j & 2 ? codes_bf16(y, z) : __builtin_bit_cast(uint4, codes_f16(y, z));
   };
   auto store_scales = [&](W& t, const Raw& r) {
     if (sc_mine) t.sc[sc_b] = r.ok ? make_float2(usable(r.sc.x), usable(r.sc.y)) : make_float2(NAN, NAN);
@@ -678,7 +684,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_kv_wide(KvAttnArgs a,
 #pragma unroll
     for (int i = 0; i < 16; ++i) acc[d][i] = 0.f;
   const Seen see = keys_seen(pos, a.window);
-  float m = -FLT_MAX, l = 0.f, ref = 1.f, inv_ref = 1.f, top = 0.f;
+  float m = -FLT_MAX, l = 0.f, ref = kSmallRef;  // (the row's sums of values are in units of ref)
 
   auto scores = [&](const W& t, f32x16 (&sa)[NU], auto&& other) {
 #pragma unroll
@@ -700,7 +706,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_kv_wide(KvAttnArgs a,
   int tile = k0, at = 0;
   float x[NU][16], f[NB], sv[NB];
   bool masked;
-  // scores and scales of the tile, and whether a reference has to move for it
+  // scores and scales of the tile, and whether m or ref has to move for it
   auto look = [&] {
     const W& t = buf[at];
     float most = 0.f;
@@ -712,7 +718,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_kv_wide(KvAttnArgs a,
       // (0 where the row sees none of the block's keys; NaN else makes the weights of all of them NaN)
       const int first = tile * KT + 16 * b - see.lo;
       sv[b] = masked && (first + 16 <= 0 || first > (int)see.span) ? 0.f : sc.y;
-      most = fmaxf(most, sv[b] < INFINITY ? sv[b] : 0.f);
+      most = fmaxf(most, sv[b]);
     }
 #pragma unroll
     for (int u = 0; u < NU; ++u)
@@ -732,18 +738,14 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_kv_wide(KvAttnArgs a,
     for (int u = 0; u < NU; ++u)
 #pragma unroll
       for (int i = 0; i < 16; ++i) mx = fmaxf(mx, x[u][i]);
-    // (a reference has a reciprocal: 2^-126 at least)
-    const bool far = most > ref * kRefUp || (most > 0.f && most < ref * kRefDown && ref > FLT_MIN);
-    if (!__ballot(mx > m + kLift || far)) return false;
-    if (tile > k0) top = fmaxf(top, ref);
-    const float nr = far ? fmaxf(ldexpf(1.f, ilogbf(most)), fmaxf(FLT_MIN, top * kRefLeast)) : ref;
+    const bool grow = ref < 1.f && most > kSmall;
+    if (!__ballot(mx > m || grow)) return false;
     mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-    const float nm = fmaxf(m, mx), down = exp2_fast(m - nm);
+    const float nm = mx > m ? mx + kLift : m, down = exp2_fast(m - nm);
     m = nm;
     l *= down;
-    by = down * (ref / nr);
-    ref = nr;
-    inv_ref = 1.f / nr;
+    by = grow ? down * kSmallRef : down;
+    ref = grow ? 1.f : ref;
     return true;
   };
   look();
@@ -752,19 +754,18 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_kv_wide(KvAttnArgs a,
     for (int d = 0; d < NO; ++d) acc[d] *= by;
     do {
       const int at1 = at == 2 ? 0 : at + 1, at2 = at == 0 ? 2 : at - 1;
-      const float lift = kBias - m;
-      uint32_t pw[NU * 8];
+      TwoParts pw[NU * 8];
       float up[NB], p0;
 #pragma unroll
-      for (int b = 0; b < NB; ++b) up[b] = sv[b] * inv_ref;
+      for (int b = 0; b < NB; ++b) up[b] = ref < 1.f ? sv[b] * (1.f / kSmallRef) : sv[b];
       constexpr int PS = 16 / NF > 1 ? 16 / NF : 1;  // weights to a product
       scores(buf[at1], sn, [&](int j) {
 #pragma unroll
         for (int i = j * PS; i < min((j + 1) * PS, NU * 16); ++i) {
-          const float p = exp2_fast(x[i >> 4][i & 15] + lift);
+          const float p = exp2_fast(x[i >> 4][i & 15] - m);
           l += p;
           if (i & 1)
-            pw[i >> 1] = pack_f16x2(p0 * up[i >> 3], p * up[i >> 3]);
+            pw[i >> 1] = two_parts(p0 * up[i >> 3], p * up[i >> 3]);
           else
             p0 = p;
         }
@@ -774,8 +775,9 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_kv_wide(KvAttnArgs a,
       streamed<NO * NB>(
           [&](int i) { return t.v[(i % NO * 32 + c32) * W::VC + 2 * (i / NO) + hi]; },
           [&](int i, uint4 v) {
-            const int u = 4 * (i / NO);
-            acc[i % NO] = mfma32<OpF16>(v, make_uint4(pw[u], pw[u + 1], pw[u + 2], pw[u + 3]), acc[i % NO]);
+            const TwoParts* w = &pw[4 * (i / NO)];
+            acc[i % NO] = mfma32<OpBF16>(v, make_uint4(w[0].hi, w[1].hi, w[2].hi, w[3].hi), acc[i % NO]);
+            acc[i % NO] = mfma32<OpBF16>(v, make_uint4(w[0].lo, w[1].lo, w[2].lo, w[3].lo), acc[i % NO]);
           },
           [&](int i) {
             if (i % EV == 0) store(buf[at2], raw, i / EV);
@@ -822,7 +824,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_kv_wide(KvAttnArgs a,
       }
   }
   if (mine && hi == 0 && a.lse)
-    a.lse[(int64_t)(sq.row + tok) * a.q_heads + hq] = beyond ? NAN : (m - kBias + log2f(l)) * 0.6931471805599453f;
+    a.lse[(int64_t)(sq.row + tok) * a.q_heads + hq] = beyond ? NAN : (m + log2f(l)) * 0.6931471805599453f;
 }
 
 // Joins the parts of each row with W waves a row, 4 or 1: D / 4 lanes a part, the lanes of the others meeting by
@@ -927,7 +929,7 @@ __global__ __launch_bounds__(256) void k_kv_join(KvAttnArgs a, bool vec) {
     for (int d = 0; d < 4; ++d) to[d] = (T)x[d];
   }
   if (lane == 0 && a.lse)
-    a.lse[(int64_t)(sq.row + i) * a.q_heads + h * a.group + g] = beyond ? NAN : (m - kBias + log2f(l)) * 0.6931471805599453f;
+    a.lse[(int64_t)(sq.row + i) * a.q_heads + h * a.group + g] = beyond ? NAN : (m + log2f(l)) * 0.6931471805599453f;
 }
 
 template <class T, int D>

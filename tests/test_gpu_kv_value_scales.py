@@ -58,3 +58,50 @@ def test_rows_do_not_depend_on_blocks_that_they_do_not_see(built_lib, gpu, room,
             _value_scales(t, size)
             q = t.heads_of(hq, dtype, 0.5)
             _check_rows(t, q, _run(t, q, window), window)
+
+
+def _check_to_rounding(t, q, out, window=0):
+    """Every output within the roundings of fp32 and its type's, relative to its own terms sum w |v| alone: of a weight
+    2^-17 (two bf16) and 2^-22 (its exponential), of its score and its row's sum of weights the same again, (dim + 6)
+    half steps of sum |q k|, and half a step for each addition (a wave adds a quarter of the keys at least)."""
+    (past,), (new,) = t.past, t.new
+    k, v = (x.repeat_interleave(q.shape[1] // t.heads, 1).permute(1, 0, 2) for x in t.ref.read(t.table[0], 0, past + new))
+    qd, length, scale = q.double().permute(1, 0, 2), past + new, t.dim ** -0.5
+    i, j = torch.arange(past, length)[:, None], torch.arange(length)[None, :]
+    hide = (j > i) | ((j <= i - window) if window else torch.zeros_like(j > i))
+    w = torch.softmax((qd @ k.transpose(1, 2) * scale).masked_fill(hide, -math.inf), 2)
+    o, terms = w @ v, w @ v.abs()
+    size = (qd.abs() @ k.abs().transpose(1, 2) * scale).masked_fill(hide, 0).amax(2, keepdim=True)
+    delta = (t.dim + 6) * R.EPS * size
+    bound = terms * (2.0 ** -17 + 2 * (2 * delta + 2.0 ** -22 + (64 + length / 4) * R.EPS))
+    half, least = R.HALF_STEP[q.dtype], 2.0 ** -25 if q.dtype is F16 else 2.0 ** -134
+    R.check(out.permute(1, 0, 2), o, bound * (1 + half) + o.abs() * half + least, "out")
+
+
+@pytest.mark.parametrize("dim,hq,past,new,room", [
+    (64, 4, 3000, 1, 0), (64, 8, 2000, 4, 0), (64, 2, 2000, 70, 1 << 20), (128, 4, 3000, 1, 0), (128, 2, 2000, 100, 1 << 20), (256, 4, 3000, 1, 0),
+    (256, 2, 2000, 70, 1 << 20),
+])
+def test_many_small_weights_beside_a_sure_key(built_lib, gpu, dim, hq, past, new, room):
+    """One key takes all but a small part of the softmax, in a block of large scale whose values are 0 where the others'
+    many small ones are looked for."""
+    say("sure key", dim, hq, past, new, room)
+    for at in (3, past // 2 + 5, past):
+        for dtype, low, ratio in ((F16, 60.0, 255.0), (F16, 60.0, 500.0), (BF16, 1.0, 255.0), (BF16, 1.0, 2.0 ** 30), (BF16, 2.0 ** -60, 2.0 ** 90),
+                                  (BF16, 2.0 ** -110, 2.0 ** 30)):
+            t = Setup(gpu, 1, dim, 64, [past], [new], seed=at, max_len=room or None)
+            keys = t.ref.pages[:, :, :, 0].view(*t.ref.pages.shape[:3], 16, dim)
+            keys.zero_()
+            keys[..., 0] = torch.randint(0, 26, keys.shape[:-1], generator=t.gen, dtype=torch.int8)
+            t.ref.scales[..., 0] = 1 / 127
+            t.ref.scales[..., 1] *= low / 0.02
+            p, b = t.ref.where(t.table[0], at)
+            t.ref.scales[p, :, b, 1] = low * ratio
+            k, v = t.ref.codes(p, b)
+            k[:, at % 16, 0] = 127
+            v[..., : dim if dtype is F16 else dim // 2] = 0
+            t.cache.pages.copy_(t.ref.pages)
+            t.cache.scales.copy_(t.ref.scales)
+            q = torch.zeros(new, hq, dim, dtype=dtype)
+            q[..., 0] = dim ** 0.5 * torch.linspace(12, 22, hq).to(dtype)
+            _check_to_rounding(t, q, _run(t, q, 0))
