@@ -405,7 +405,7 @@ __global__ __launch_bounds__(256, 2) void k_kv_rows(KvAttnArgs a, bool vec) {
         }
 #pragma unroll
         for (int k = 0; k < KL; ++k) mx[n] = fmaxf(mx[n], sa[n][k >> 2][k & 3]);
-        large[n] = __ballot(ref[n] < 1.f && sv[n] > kSmall);
+        large[n] = __ballot(ref[n] < 1.f && fabsf(sv[n]) > kSmall);
         move |= large[n] || __ballot(mx[n] > m[n]) != 0;
       }
       if (move && !moved) {
@@ -718,7 +718,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_kv_wide(KvAttnArgs a,
       // (0 where the row sees none of the block's keys; NaN else makes the weights of all of them NaN)
       const int first = tile * KT + 16 * b - see.lo;
       sv[b] = masked && (first + 16 <= 0 || first > (int)see.span) ? 0.f : sc.y;
-      most = fmaxf(most, sv[b]);
+      most = fmaxf(most, fabsf(sv[b]));
     }
 #pragma unroll
     for (int u = 0; u < NU; ++u)

@@ -105,3 +105,21 @@ def test_many_small_weights_beside_a_sure_key(built_lib, gpu, dim, hq, past, new
             q = torch.zeros(new, hq, dim, dtype=dtype)
             q[..., 0] = dim ** 0.5 * torch.linspace(12, 22, hq).to(dtype)
             _check_to_rounding(t, q, _run(t, q, 0))
+
+
+@pytest.mark.parametrize("dim,hq,past,new,room", [
+    (64, 4, 700, 1, 0), (64, 8, 300, 4, 0), (64, 2, 300, 70, 1 << 20), (128, 4, 700, 1, 0), (128, 2, 300, 100, 1 << 20), (256, 4, 700, 1, 0),
+    (256, 2, 300, 70, 1 << 20),
+])
+def test_scales_below_zero(built_lib, gpu, dim, hq, past, new, room):
+    """Appending writes none, but a number is its code times its block's scale whatever that is."""
+    say("scales below zero", dim, hq, past, new, room)
+    for dtype, size in ((F16, 1.0), (F16, 100.0), (BF16, 1e9), (BF16, 1e30), (BF16, 1e-30)):
+        for every in (1, 2):
+            t = Setup(gpu, 1, dim, 64, [past], [new], seed=every, max_len=room or None)
+            flat = t.ref.scales.view(-1, 2)
+            flat[::every, 1] *= -size
+            flat[::every, 0] *= -1
+            t.cache.scales.copy_(t.ref.scales)
+            q = t.heads_of(hq, dtype, 0.5)
+            _check_to_rounding(t, q, _run(t, q, 0))
