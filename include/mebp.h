@@ -471,8 +471,8 @@ typedef struct {
 } mebp_kv_batch;
 
 /* Appends keys and values, the keys turned by their positions (rope NULL: as they are), and turns queries
- * beside them. A block's scale is max(scale before, max |x| / 127 in fp32), "before" 0 where the block's
- * first token is new; codes are round(x / scale) to nearest even, and where the scale rises the block's
+ * beside them. A block's scale is max(|scale before|, max |x| / 127 in fp32), "before" 0 where the block's
+ * first token is new; codes are round(x / scale) to nearest even, and where the scale changes the block's
  * earlier ones round(code before / after). Scales and codes are those of 64-bit arithmetic.
  *   k, v       of the cache's heads and dim, any dtype
  *   q, q_out   [tokens][any heads][dim] of that dtype, together or both NULL; q_out may be q

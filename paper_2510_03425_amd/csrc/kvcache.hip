@@ -1,8 +1,8 @@
 // Append to the paged 8-bit cache, with the rotation of keys and queries on the way, and its read back.
 //
 // A block of 16 tokens of one kv head has one fp32 scale for its keys and one for its values:
-//   scale = max(scale before, fp32(max |x| / 127)),  code = rint(x / scale),
-// "before" being 0 where the block's first token is new. A scale that rises has the block's earlier codes
+//   scale = max(|scale before|, fp32(max |x| / 127)),  code = rint(x / scale),
+// "before" being 0 where the block's first token is new. A scale that changes has the block's earlier codes
 // rounded again, rint(code before / after). Codes are the nearest ones of the definition in 64 bits (a
 // rotated key rounded to 32 bits first would land on the other side of a border now and then, and a code
 // is a whole step), so keys are turned, and their largest found, in 64 bits.
@@ -176,7 +176,7 @@ struct Pairs {
 };
 
 // A block's scale from the largest of the workgroup's x, and x's codes as bytes a[..], b[..]: of the block's new tokens
-// (`fresh`), or of earlier ones rounded again where the scale has risen. X: double for keys that are turned.
+// (`fresh`), or of earlier ones rounded again where the scale has changed. X: double for keys that are turned.
 template <class X, int E>
 struct Codes {
   float scale;
@@ -211,7 +211,7 @@ struct Codes {
     if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = m;
     __syncthreads();
     m = fmax(fmax(red[0], red[1]), fmax(red[2], red[3]));
-    scale = raised(old, m);
+    scale = raised(fabsf(old), m);
     write = fresh || (earlier && scale != old);
     // (a scale too small for its reciprocal, or none: every code by its definition)
     bool near = fresh && !(scale > 1e-37f);

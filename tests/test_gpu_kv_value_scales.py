@@ -123,3 +123,23 @@ def test_scales_below_zero(built_lib, gpu, dim, hq, past, new, room):
             t.cache.scales.copy_(t.ref.scales)
             q = t.heads_of(hq, dtype, 0.5)
             _check_to_rounding(t, q, _run(t, q, 0))
+
+
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("before", [0.5, -0.5, -1e-3, -40.0])
+def test_appending_to_a_block_of_a_scale_below_zero(built_lib, gpu, dim, before):
+    """Its scale is at least that large, and its earlier tokens stay what they were to half a code."""
+    t = Setup(gpu, 2, dim, 16, [5], [4], seed=1)
+    p = int(t.table[0, 0])
+    t.cache.scales[p] = t.ref.scales[p] = before
+    old_k, old_v = t.ref.read(t.table[0], 0, 5)
+    k, v = t.heads_of(2, BF16), t.heads_of(2, BF16)
+    D.kv_append(t.cache, t.batch, k.to(gpu), v.to(gpu))
+    ko, vo = (torch.zeros(9, 2, dim, device=gpu) for _ in range(2))
+    D.kv_read(t.cache, t.make_batch([0, 9], [0], 9), ko, vo)
+    scales = t.cache.scales[p].cpu()[:, 0]
+    for got, old, new, s in ((ko, old_k, k, scales[:, 0]), (vo, old_v, v, scales[:, 1])):
+        want = torch.maximum((new.double().abs().amax((0, 2)) / 127).float(), torch.full((2,), abs(before)))
+        assert torch.equal(s, want)
+        x = torch.cat([old, new.double()])
+        assert bool(((got.cpu().double() - x).abs() <= s.double()[None, :, None] / 2 * (1 + 2.0 ** -20) + x.abs() * R.EPS).all())
