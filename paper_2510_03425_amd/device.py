@@ -568,12 +568,19 @@ class DeviceModel:
 
     def layer_forward_cached(self, l: int, x_in: torch.Tensor, x_out: torch.Tensor, cache: KvCache, batch: KvBatch, rope: Rope,
                              ws: torch.Tensor):
-        rows = x_in.shape[0]
+        if x_in.is_cuda and x_in.get_device() != _current_device():
+            with torch.cuda.device(x_in.device):
+                return self.layer_forward_cached(l, x_in, x_out, cache, batch, rope, ws)
+        rows, dev = x_in.shape[0], self.ws.get_device()
         _with(x_in, cache, batch)
+        if rope.table.get_device() != dev:
+            raise ValueError(f"the rope's table must be on {self.ws.device}")
+        if ws.get_device() != dev or not ws.is_contiguous():
+            raise ValueError(f"workspace must be contiguous on {self.ws.device}")
         L.mebp_layer_forward_cached(self.ccfg, l, self.base[l], self.lora[l],
                                     _operand(x_in, torch.float32, (rows, self.cfg.hidden), self.ws, "x_in"),
                                     _operand(x_out, torch.float32, (rows, self.cfg.hidden), self.ws, "x_out"), rows, cache.struct,
-                                    batch.struct, rope.struct, ptr(ws), ws.numel(), stream_handle())
+                                    batch.struct, rope.struct, ptr(ws), ws.nbytes, stream_handle())
 
     def cached_ws(self, rows: int, batch: KvBatch) -> torch.Tensor:
         """A workspace of ``forward_cached`` for so many rows and such a batch."""
