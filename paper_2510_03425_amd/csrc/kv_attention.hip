@@ -13,6 +13,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "device_common.h"
 #include "heads.h"
@@ -46,7 +47,7 @@ DEV uint4 stream16(const int8_t* p) {
 }
 
 // 8 codes in 2 dwords -> 8 fp16: code + 128 below the bits of 1024, less 1152; exact.
-DEV f16x8 codes_f16(uint32_t lo, uint32_t hi) {
+DEV uint4 codes_f16(uint32_t lo, uint32_t hi) {
   const uint32_t a = lo ^ 0x80808080u, b = hi ^ 0x80808080u;
   const f16x2 off = {(f16)1152.0f, (f16)1152.0f};
   uint4 r;
@@ -54,7 +55,7 @@ DEV f16x8 codes_f16(uint32_t lo, uint32_t hi) {
   r.y = __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, a, 0x04030402u)) - off);
   r.z = __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, b, 0x04010400u)) - off);
   r.w = __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, b, 0x04030402u)) - off);
-  return __builtin_bit_cast(f16x8, r);
+  return r;
 }
 
 // The same as bf16, the upper halves of their fp32.
@@ -64,6 +65,16 @@ DEV uint32_t codes_bf16x2(uint32_t w, int j) {
 }
 DEV uint4 codes_bf16(uint32_t lo, uint32_t hi) {
   return make_uint4(codes_bf16x2(lo, 0), codes_bf16x2(lo, 2), codes_bf16x2(hi, 0), codes_bf16x2(hi, 2));
+}
+// Operands of a type T.
+template <class T>
+using OpOf = typename std::conditional<__is_same(T, f16), OpF16, OpBF16>::type;
+template <class T>
+DEV uint4 codes_as(uint32_t lo, uint32_t hi) {
+  if constexpr (__is_same(T, f16))
+    return codes_f16(lo, hi);
+  else
+    return codes_bf16(lo, hi);
 }
 // Two numbers as bf16, and what that leaves out of them.
 struct TwoParts {
@@ -92,9 +103,9 @@ DEV Seen keys_seen(int pos, int window) {
   return Seen{lo, (unsigned)(pos - lo)};
 }
 
-// A row's queries as fp16 operands, scaled by a power of two to just below fp16's end (exact but for
-// elements 2^-28 of the largest) and by the sign of `scale`, and what a score is to be multiplied by for it,
-// not negative: NaN where the row has a NaN or an infinity.
+// A row's queries as operands of their type, scaled by a power of two to just below fp16's end (exact but for elements
+// 2^-140 of a bf16 row's largest) and by the sign of `scale`, and what a score is to be
+// multiplied by for it, not negative: NaN where the row has a NaN or an infinity.
 // at(m): the lane's first element of operand m; LANES: of one row, this many apart.
 template <class T>
 struct Eight {
@@ -114,7 +125,7 @@ DEV void load_queries(const T* p, bool vec, typename Eight<T>::run (&x)[NF], At&
   }
 }
 template <class T, int NF, int LANES>
-DEV float queries(const typename Eight<T>::run (&raw)[NF], float scale, f16x8 (&f)[NF]) {
+DEV float queries(const typename Eight<T>::run (&raw)[NF], float scale, uint4 (&f)[NF]) {
   float x[NF][8];
 #pragma unroll
   for (int m = 0; m < NF; ++m)
@@ -129,15 +140,18 @@ DEV float queries(const typename Eight<T>::run (&raw)[NF], float scale, f16x8 (&
 #pragma unroll
   for (int o = LANES; o < 64; o *= 2) most = max(most, (uint32_t)__shfl_xor((int)most, o, 64));
   const bool bad = most >= 0x7f800000u;
-  const int up = most && !bad ? 14 - ilogbf(__builtin_bit_cast(float, most)) : 0;
+  const int up = most && !bad ? 15 - ilogbf(__builtin_bit_cast(float, most)) : 0;
 #pragma unroll
-  for (int m = 0; m < NF; ++m)
+  for (int m = 0; m < NF; ++m) {
+    typename Eight<T>::run r;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) f[m][i] = (f16)__builtin_amdgcn_ldexpf(scale < 0.f ? -x[m][i] : x[m][i], up);
+    for (int i = 0; i < 8; ++i) r[i] = (T)__builtin_amdgcn_ldexpf(scale < 0.f ? -x[m][i] : x[m][i], up);
+    f[m] = __builtin_bit_cast(uint4, r);
+  }
   return bad ? NAN : __builtin_amdgcn_ldexpf(fabsf(scale), -up);
 }
 template <class T, int NF>
-DEV float row_queries(const T* p, bool vec, float scale, f16x8 (&f)[NF], int g4) {
+DEV float row_queries(const T* p, bool vec, float scale, uint4 (&f)[NF], int g4) {
   typename Eight<T>::run x[NF];
   load_queries<T, NF>(p, vec, x, [&](int m) { return 64 * (m / 2) + 16 * g4 + 8 * (m & 1); });
   return queries<T, NF, 16>(x, scale, f);
@@ -305,7 +319,7 @@ __global__ __launch_bounds__(256, 2) void k_kv_rows(KvAttnArgs a, bool vec) {
   load_keys(tile);
   look_up(tile + 4);
 
-  f16x8 qf[NR][QL ? 1 : NF];
+  uint4 qf[NR][QL ? 1 : NF];
   float qs[NR];
   Seen see[NR];
 #pragma unroll
@@ -314,12 +328,12 @@ __global__ __launch_bounds__(256, 2) void k_kv_rows(KvAttnArgs a, bool vec) {
     see[n] = keys_seen(sq.past + i, a.window);
     const T* p = (const T*)a.q.p + (int64_t)(sq.row + i) * a.q.ld + (int64_t)(h * a.group + g) * a.q.hld;
     if constexpr (QL) {
-      f16x8 f[NF];
+      uint4 f[NF];
       qs[n] = row_queries(p, vec, a.scale, f, g4);
       // (every wave has made the same ones)
       if (wave == 0) {
 #pragma unroll
-        for (int i = 0; i < NF; ++i) q_lds[(n * NF + i) * 64 + lane] = __builtin_bit_cast(uint4, f[i]);
+        for (int i = 0; i < NF; ++i) q_lds[(n * NF + i) * 64 + lane] = f[i];
       }
     } else {
       qs[n] = row_queries(p, vec, a.scale, qf[n], g4);
@@ -328,7 +342,7 @@ __global__ __launch_bounds__(256, 2) void k_kv_rows(KvAttnArgs a, bool vec) {
   if (QL) __syncthreads();
   auto query = [&](int n, int i) {
     if constexpr (QL)
-      return __builtin_bit_cast(f16x8, q_lds[(n * NF + i) * 64 + lane]);
+      return q_lds[(n * NF + i) * 64 + lane];
     else
       return qf[n][i];
   };
@@ -364,7 +378,7 @@ __global__ __launch_bounds__(256, 2) void k_kv_rows(KvAttnArgs a, bool vec) {
         for (int n = 0; n < NR; ++n) sa[n][t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int j = 0; j < D / 64; ++j) {
-        f16x8 q[NR][2];
+        uint4 q[NR][2];
 #pragma unroll
         for (int n = 0; n < NR; ++n) {
           q[n][0] = query(n, 2 * j);
@@ -373,11 +387,11 @@ __global__ __launch_bounds__(256, 2) void k_kv_rows(KvAttnArgs a, bool vec) {
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
           const uint4 c = kr[t * (D / 64) + j];
-          const f16x8 c0 = codes_f16(c.x, c.y), c1 = codes_f16(c.z, c.w);
+          const uint4 c0 = codes_as<T>(c.x, c.y), c1 = codes_as<T>(c.z, c.w);
 #pragma unroll
           for (int n = 0; n < NR; ++n) {
-            sa[n][t] = mfma16(c0, q[n][0], sa[n][t]);
-            sa[n][t] = mfma16(c1, q[n][1], sa[n][t]);
+            sa[n][t] = mfma16_raw<OpOf<T>>(c0, q[n][0], sa[n][t]);
+            sa[n][t] = mfma16_raw<OpOf<T>>(c1, q[n][1], sa[n][t]);
           }
         }
       }
@@ -651,7 +665,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_kv_wide(KvAttnArgs a,
     uint4* to = j & 2 ? &t.v[dim * W::VC + b] : &t.k[key * W::KC + c];
     const uint4 x = j & 2 ? r.v[i] : r.k[i];
     const uint32_t y = j & 1 ? x.z : x.x, z = j & 1 ? x.w : x.y;
-    to[j & 1] = j & 2 ? codes_bf16(y, z) : __builtin_bit_cast(uint4, codes_f16(y, z));
+    to[j & 1] = j & 2 ? codes_bf16(y, z) : codes_as<T>(y, z);
   };
   auto store_scales = [&](W& t, const Raw& r) {
     if (sc_mine) t.sc[sc_b] = r.ok ? make_float2(usable(r.sc.x), usable(r.sc.y)) : make_float2(NAN, NAN);
@@ -674,7 +688,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_kv_wide(KvAttnArgs a,
   load(first, e0, k0);
   load(second, e1, tile_at(k0 + 1));
   load(raw, e2, tile_at(k0 + 2));
-  f16x8 qf[NF];
+  uint4 qf[NF];
   const float qs = queries<T, NF, 32>(qr, a.scale, qf);
   store_all(buf[0], first);
   store_all(buf[1], second);
@@ -693,7 +707,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_kv_wide(KvAttnArgs a,
       for (int i = 0; i < 16; ++i) sa[u][i] = 0.f;
     streamed<NU * NF>(
         [&](int i) { return t.k[(i % NU * 32 + bits23(c32)) * W::KC + 2 * (i / NU) + hi]; },
-        [&](int i, uint4 x) { sa[i % NU] = mfma32<OpF16>(x, __builtin_bit_cast(uint4, qf[i / NU]), sa[i % NU]); }, other);
+        [&](int i, uint4 x) { sa[i % NU] = mfma32<OpOf<T>>(x, qf[i / NU], sa[i % NU]); }, other);
   };
   f32x16 sn[NU];
   __syncthreads();

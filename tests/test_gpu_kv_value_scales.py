@@ -143,3 +143,19 @@ def test_appending_to_a_block_of_a_scale_below_zero(built_lib, gpu, dim, before)
         assert torch.equal(s, want)
         x = torch.cat([old, new.double()])
         assert bool(((got.cpu().double() - x).abs() <= s.double()[None, :, None] / 2 * (1 + 2.0 ** -20) + x.abs() * R.EPS).all())
+
+
+@pytest.mark.parametrize("dim,hq,past,new,room", [
+    (64, 4, 700, 1, 0), (64, 8, 300, 4, 0), (64, 2, 300, 70, 1 << 20), (128, 4, 700, 1, 0), (128, 2, 300, 100, 1 << 20), (256, 4, 700, 1, 0),
+    (256, 2, 300, 70, 1 << 20),
+])
+def test_one_element_of_a_query_far_above_the_others(built_lib, gpu, dim, hq, past, new, room):
+    """Where keys have nothing for it the others make the scores."""
+    say("large element", dim, hq, past, new, room)
+    for dtype, large in ((F16, 60000.0), (BF16, 2.0 ** 30), (BF16, 2.0 ** 60), (BF16, 2.0 ** 120)):
+        t = Setup(gpu, 1, dim, 64, [past], [new], seed=5, max_len=room or None)
+        t.ref.pages[:, :, :, 0].view(*t.ref.pages.shape[:3], 16, dim)[..., 7] = 0
+        t.cache.pages.copy_(t.ref.pages)
+        q = t.heads_of(hq, dtype, 0.5)
+        q[..., 7] = large
+        _check_to_rounding(t, q, _run(t, q, 0))
