@@ -398,7 +398,8 @@ int mebp_train_step_distill(const mebp_config* cfg, const mebp_q4* emb, const me
  * What a trained model answers with: rotary positions by themselves, a paged cache of keys and values
  * in 8 bits, attention of new tokens over it, and a layer's forward pass with them in the place of
  * mebp_layer_forward_ckpt's attention. Numbers of sequences, lengths and pages are read on the
- * device, so that a captured call serves as they change. rows = 0 and tokens = 0 enqueue nothing. */
+ * device, so that a captured call serves as they change. tokens = 0 and seqs = 0 enqueue nothing; the layer's
+ * call refuses rows = 0 and seqs = 0. */
 
 /* Heads of some tokens (queries, keys, values or their gradients). */
 typedef struct {
@@ -467,7 +468,8 @@ typedef struct {
   int32_t seqs;          /* 0 .. 65534                                                      */
   int32_t max_new;       /* no sequence has more new tokens (rows beyond are left as they were) */
   int32_t max_len;       /* none is longer with them (rows from there on are NaN in an attention); up to */
-                         /* 2^30. The call's launches are laid out for these two             */
+                         /* 2^30. The call's launches are laid out for these two, for all sequences alike: */
+                         /* single tokens behind long texts are quicker in a call without long prompts */
 } mebp_kv_batch;
 
 /* Appends keys and values, the keys turned by their positions (rope NULL: as they are), and turns queries
@@ -475,7 +477,7 @@ typedef struct {
  * first token is new; codes are round(x / scale) to nearest even, and where the scale changes the block's
  * earlier ones round(code before / after). Scales and codes are those of 64-bit arithmetic.
  *   k, v       of the cache's heads and dim, any dtype
- *   q, q_out   [tokens][any heads][dim] of that dtype, together or both NULL; q_out may be q
+ *   q, q_out   [tokens][any heads][dim] of that dtype, together and with a rope, or both NULL; q_out may be q
  * A NaN or an infinity makes its block's scale NaN. Where the table has no page of the pool (an id outside
  * 0 .. n_pages - 1, a column beyond max_pages) nothing is stored. Blocks that are written belong to one
  * sequence of the call; whole ones before them may be shared.                               */

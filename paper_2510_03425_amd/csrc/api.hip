@@ -2586,7 +2586,7 @@ int check_grid(int64_t groups) {
   return MEBP_OK;
 }
 
-int check_append(const mebp_kv_cache* c, const mebp_kv_batch* b, const mebp_rope* rope, int rows, int q_heads) {
+int check_append(const mebp_kv_cache* c, const mebp_kv_batch* b, const mebp_rope* rope, int q_heads) {
   int e;
   if ((e = check_cache(c)) || (e = check_batch(b)) || (rope && (e = check_rope_for(rope, c->dim))) ||
       (e = check_grid((int64_t)touched_blocks(b->max_new) * (2 * c->heads + q_heads))))
@@ -2595,7 +2595,6 @@ int check_append(const mebp_kv_cache* c, const mebp_kv_batch* b, const mebp_rope
   if ((e = check_batch_apart(b, pg)) || (e = check_batch_apart(b, sc)) || (e = check_apart(pg, {sc, table_span(rope)})) ||
       (e = check_apart(sc, {table_span(rope)})))
     return e;
-  (void)rows;
   return MEBP_OK;
 }
 KvAppendArgs append_args(const mebp_kv_cache* c, const mebp_kv_batch* b, const mebp_rope* rope, int rows) {
@@ -2729,7 +2728,7 @@ int mebp_kv_append(const mebp_kv_cache* cache, const mebp_kv_batch* batch, const
                    const mebp_heads* v, const mebp_heads* q, const mebp_heads* q_out, mebp_stream_t stream) {
   int e;
   if ((e = check_heads(k, "k", false)) || (e = check_heads(v, "v", false)) ||
-      (e = check_append(cache, batch, rope, k->tokens, q ? q->heads : 0)) ||
+      (e = check_append(cache, batch, rope, q ? q->heads : 0)) ||
       (e = check_like(k, "k", k->tokens, cache->heads, cache->dim, k->dtype)) ||
       (e = check_like(v, "v", k->tokens, cache->heads, cache->dim, k->dtype)))
     return e;
@@ -2847,7 +2846,7 @@ int mebp_layer_forward_cached(const mebp_config* cfg, int32_t layer, const mebp_
   int e;
   if ((e = check_config(cfg)) || (e = check_shape(1, rows)) || (e = check_layer(cfg, layer, base, lora)) ||
       (e = check_act(x_in, "x_in")) || (e = check_act(x_out, "x_out")) ||
-      (e = check_append(cache, batch, rope, rows, cfg->n_heads)) || (e = check_rope(rope)) ||
+      (e = check_append(cache, batch, rope, cfg->n_heads)) || (e = check_rope(rope)) ||
       (e = check_cached_shape(cfg, rows, batch->seqs, batch->max_new, batch->max_len)))
     return e;
   if (cache->heads != cfg->n_kv_heads || cache->dim != cfg->head_dim)

@@ -19,8 +19,6 @@
 #include "heads.h"
 #include "kv_device.h"
 
-#define DEVM __device__ __forceinline__
-
 namespace mebp {
 namespace {
 
