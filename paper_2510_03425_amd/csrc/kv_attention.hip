@@ -26,7 +26,7 @@ namespace {
 // Those below 2^-126 are 0.
 constexpr float kLift = 6.f;
 // A weight times its block's scale of values goes into the products as two bf16, the second what the first leaves out:
-// 2^-18 of it at any size, so that many small ones beside a large one of small values are all there (in fp16 those
+// 2^-17 of it at any size, so that many small ones beside a large one of small values are all there (in fp16 those
 // below 2^-22 of the largest are not). fp32's range takes them and their sums as they are; a row whose scales so far are
 // all below kSmall has them over kSmallRef, where theirs have their bits too. (The second products are what bounds
 // k_kv_wide: 8 x 2048 tokens, 8 heads of 256, 261 us instead of 249, 12 of 128, 176 instead of 146, 14 of 64, 134 instead
