@@ -1,8 +1,8 @@
 // Attention of new tokens over the paged 8-bit cache on gfx950: causal, grouped heads, optional window.
 //
 // With the codes k, v of a block and its scales sk, sv:  s = scale sk (q . k),  p = exp(s - m),
-// out = (sum p sv v) / (sum p): codes go into the matrix instructions as they are, exact in fp16 (keys) and bf16
-// (values), and the scales into the scores and the weights. One pass over the cache with the running maximum and sum of a
+// out = (sum p sv v) / (sum p): codes go into the matrix instructions as they are, exact in the queries' type (keys) and
+// bf16 (values), and the scales into the scores and the weights. One pass over the cache with the running maximum and sum of a
 // softmax; statistics and sums in fp32.
 //
 // k_kv_rows keeps a whole 64-key tile in one wave's registers, without LDS: with S^T = K Q^T and
@@ -102,9 +102,9 @@ DEV Seen keys_seen(int pos, int window) {
   return Seen{lo, (unsigned)(pos - lo)};
 }
 
-// A row's queries as operands of their type, scaled by a power of two to just below fp16's end (exact but for elements
-// 2^-140 of a bf16 row's largest) and by the sign of `scale`, and what a score is to be
-// multiplied by for it, not negative: NaN where the row has a NaN or an infinity.
+// A row's queries as operands of their type, scaled by a power of two towards fp16's end (exact but for elements 2^-140 of
+// a bf16 row's largest) and by the sign of `scale`, and what a score is to be multiplied by for it, not negative: NaN
+// where the row has a NaN or an infinity.
 // at(m): the lane's first element of operand m; LANES: of one row, this many apart.
 template <class T>
 struct Eight {
@@ -139,7 +139,8 @@ DEV float queries(const typename Eight<T>::run (&raw)[NF], float scale, uint4 (&
 #pragma unroll
   for (int o = LANES; o < 64; o *= 2) most = max(most, (uint32_t)__shfl_xor((int)most, o, 64));
   const bool bad = most >= 0x7f800000u;
-  const int up = most && !bad ? 15 - ilogbf(__builtin_bit_cast(float, most)) : 0;
+  // (by 2^100 at most, so that what takes it back has its bits)
+  const int up = most && !bad ? min(15 - ilogbf(__builtin_bit_cast(float, most)), 100) : 0;
 #pragma unroll
   for (int m = 0; m < NF; ++m) {
     typename Eight<T>::run r;
@@ -530,7 +531,7 @@ __global__ __launch_bounds__(256, 2) void k_kv_rows(KvAttnArgs a, bool vec) {
 }
 
 // Many rows: one workgroup of 4 waves takes 128 rows, 32 a wave, whose queries and sums stay in registers; the
-// waves share tiles of KT keys [KT][D] in fp16 and values [D][KT] in bf16 in LDS, turned to them once. Products on
+// waves share tiles of KT keys [KT][D] in the queries' type and values [D][KT] in bf16 in LDS, turned to them once. Products on
 // 32x32x16: S^T = K Q^T with row r of 32 as key r with bits 2 and 3 exchanged, so that a lane's 8 results
 // are 8 successive keys, the other operand of O^T += V^T P^T. A wave's products and its other work follow one
 // another unless they are of different tiles: the scores of tile t + 1 are made beside the weights of t, and

@@ -159,3 +159,18 @@ def test_one_element_of_a_query_far_above_the_others(built_lib, gpu, dim, hq, pa
         q = t.heads_of(hq, dtype, 0.5)
         q[..., 7] = large
         _check_to_rounding(t, q, _run(t, q, 0))
+
+
+@pytest.mark.parametrize("dim,hq,past,new,room", [
+    (64, 4, 700, 1, 0), (64, 8, 300, 4, 0), (64, 2, 300, 70, 1 << 20), (128, 4, 700, 1, 0), (128, 2, 300, 100, 1 << 20), (256, 4, 700, 1, 0),
+    (256, 2, 300, 70, 1 << 20),
+])
+def test_queries_and_scales_of_keys_at_opposite_ends(built_lib, gpu, dim, hq, past, new, room):
+    """Scores of ordinary size from queries at bf16's lower end and keys' scales at fp32's upper one, and the other way round."""
+    say("opposite ends", dim, hq, past, new, room)
+    for by in (125, 100, -60, -120):
+        t = Setup(gpu, 1, dim, 64, [past], [new], seed=9, max_len=room or None)
+        t.ref.scales[..., 0] *= 2.0 ** by
+        t.cache.scales.copy_(t.ref.scales)
+        q = (t.heads_of(hq, torch.float32) * 2.0 ** -by).to(BF16)
+        _check_to_rounding(t, q, _run(t, q, 0))
