@@ -495,9 +495,10 @@ int mebp_kv_read(const mebp_kv_cache* cache, const mebp_kv_batch* batch, const m
  *   q, out  fp16 or bf16 [tokens][a multiple of the cache's heads][dim]; out apart from q
  *   lse     [tokens][q heads] fp32 log-sum-exp of the scaled scores, or NULL
  * Scores by products in the queries' type (exact there, as codes are), outputs by products in bf16 (codes are
- * exact there too; weights times their block's scale go in as two of them, off by 2^-17 at most); sums and softmax in fp32. A row depends on the blocks that it sees alone: one whose
- * scale is NaN or infinite, or whose page the table does not have, makes it NaN. Sums of values beyond 10^33
- * may overflow, and beside values' scales above 10^-6 those below 10^-27 lose bits.            */
+ * exact there too; weights times their block's scale go in as two of them, off by 2^-17 at most); sums and
+ * softmax in fp32. A row depends on the blocks that it sees alone: one whose scale is NaN or infinite, or
+ * whose page the table does not have, makes it NaN. Sums of values beyond 10^33 may overflow, and beside
+ * values' scales above 10^-6 those below 10^-27 lose bits.                                  */
 int mebp_kv_attention(const mebp_kv_cache* cache, const mebp_kv_batch* batch, const mebp_heads* q, const mebp_heads* out,
                       float* lse, float scale, int32_t window, void* ws, size_t ws_bytes, mebp_stream_t stream);
 
