@@ -989,7 +989,7 @@ KvPlan kv_plan(int seqs, int max_new, int max_len, int q_heads, int heads, int d
   // Few rows by k_kv_rows, and as many as it has workgroups for in a round and a half of the chip, with up to 1536
   // times four tiles to do: it starts sooner than k_kv_wide, but each row tile reads the cache again. (Of heads of 128,
   // groups of 6, in us: one sequence of 1256 tokens, 256 of them new, 192 workgroups of 20 tiles, 18 and 30; of 8064,
-  // 64 new, 1536 fours, 29 and 32; of 8128, 128 new, 3072 fours, 41 and 38; 4 sequences of 256 new tokens, 768
+  // 64 new, 1536 fours, 29 and 32; of 8128, 128 new, twice as many, 41 and 38; 4 sequences of 256 new tokens, 768
   // workgroups, 18 and 18; 40 of 68, 60 new, 1840 workgroups, 35 and 13.)
   // The longest sequences decide for all: a single token beside a prompt of 2048 walks all its keys in one workgroup (7
   // behind 8192, 12 heads of 128: 417 us, the prompt alone 66 and they 16; behind 65536, 8 of 256: 3580, 85 and 160).
